@@ -371,6 +371,63 @@ MEZO_API int mezo_nf4_quantize(const void* src, uint32_t src_dtype, uint64_t n, 
 MEZO_API int mezo_nf4_dequantize(const void* codes, const float* absmax, uint64_t n, void* dst,
                                  uint32_t dst_dtype, void* stream);
 
+/* ---- the forward pass -------------------------------------------------- */
+
+/* Operators of the two forward passes that Algorithm 1 evaluates a sample
+ * with. All of them are plain kernel launches on stream: they allocate
+ * nothing, may be captured into a HIP graph, and give equal outputs for equal
+ * inputs, bit for bit. There is no backward pass: the method takes no
+ * derivative. Scratch memory is the caller's: *_workspace gives the bytes a
+ * call of these sizes needs (0: none, the pointer may be NULL), 16-byte
+ * aligned device memory that no other call uses until the work is done. */
+
+/* 8-bit storage of a [rows, cols] matrix. A row is cut into blocks of 128
+ * elements (the last may be shorter); a block is stored as e4m3 codes and one
+ * scale 2^e, e the least exponent in [-127, 127] with max|w| <= 448 * 2^e over
+ * the block's finite elements (e = 0 for a block of zeros): a code is
+ * w * 2^-e rounded to the nearest e4m3 value, ties to even. inf and NaN are
+ * coded NaN. `codes` holds rows * B * 128 bytes, B = ceil(cols / 128), the
+ * row's end padded with zeros; `scales` holds rows * S bytes, S = B rounded up
+ * to a multiple of 4, the bytes e + 127, the row's end padded with zeros. */
+#define MEZO_F8_BLOCK 128u
+#define MEZO_F8_MAX_ROWS (1ull << 30)
+#define MEZO_F8_MAX_COLS (1ull << 30)
+
+/* Quantize a [rows, cols] matrix of storage src_dtype (MEZO_F32 or MEZO_BF16),
+ * rows ld elements apart, into codes (16-byte aligned) and scales (4-byte
+ * aligned). 1 <= rows <= MEZO_F8_MAX_ROWS, 1 <= cols <= MEZO_F8_MAX_COLS,
+ * rows * B * 128 <= MEZO_MAX_NUMEL, ld >= cols (MEZO_EINVAL); the three buffers
+ * must not overlap (MEZO_EOVERLAP). Asynchronous on stream. */
+MEZO_API int mezo_f8_quantize(const void* src, uint32_t src_dtype, uint64_t rows, uint64_t cols, uint64_t ld,
+                              void* codes, uint8_t* scales, void* stream);
+
+/* c = x w^T: x [m, k] and w [n, k] (a layer's weights, one row per output) in
+ * 8-bit storage, c [m, n] of storage c_dtype (MEZO_F32 or MEZO_BF16), rows ldc
+ * elements apart. The values of both are multiplied exactly. For MEZO_F32 they
+ * are summed in fp32; for MEZO_BF16 the matrix instruction sums a block's 128
+ * products to about 16 bits, the blocks in fp32, and the sum is rounded once.
+ * Sizes as in mezo_f8_quantize, m * n <= MEZO_MAX_NUMEL, ldc >= n (MEZO_EINVAL); c and the workspace
+ * must not overlap the operands (MEZO_EOVERLAP). */
+MEZO_API uint64_t mezo_f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t c_dtype);
+MEZO_API int mezo_f8_matmul(const void* x_codes, const uint8_t* x_scales, const void* w_codes,
+                            const uint8_t* w_scales, uint64_t m, uint64_t n, uint64_t k, void* c, uint32_t c_dtype,
+                            uint64_t ldc, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* The loss of a forward pass: for each of `rows` tokens with target y =
+ * targets[t] >= 0, losses[t] = ln sum_v exp(x_tv) - x_ty over the token's
+ * `vocab` logits (storage dtype, rows ld elements apart); tokens with a
+ * negative target are not counted, their losses are 0 and their logits are not
+ * read. *mean (may be NULL) = the mean over the counted tokens, summed in fp64,
+ * 0 if there are none. A row that holds NaN or +inf, or only -inf, and a target
+ * >= vocab give NaN; a target of logit -inf gives +inf. 1 <= rows <=
+ * MEZO_LOSS_MAX_ROWS, vocab >= 1, ld >= vocab (MEZO_EINVAL); what is written
+ * must not overlap anything else (MEZO_EOVERLAP). */
+#define MEZO_LOSS_MAX_ROWS (1ull << 23)
+MEZO_API uint64_t mezo_token_loss_workspace(uint64_t rows, uint64_t vocab);
+MEZO_API int mezo_token_loss(const void* logits, uint32_t dtype, uint64_t rows, uint64_t vocab, uint64_t ld,
+                             const int64_t* targets, float* losses, float* mean, void* workspace,
+                             uint64_t workspace_bytes, void* stream);
+
 /* ---- the one-byte gradient (host, pure) ------------------------------- */
 
 /* Projected gradient g = (l+ - l-) / (2 eps) -> q (Section 3). ±inf clip to

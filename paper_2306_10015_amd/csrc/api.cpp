@@ -7,18 +7,15 @@
 #include <atomic>
 #include <cmath>
 #include <cstdint>
-#include <cstdio>
 #include <cstring>
-#include <exception>
 #include <memory>
 #include <mutex>
-#include <new>
-#include <stdexcept>
 #include <vector>
 
 #include "../../include/mezo.h"
 #include "checksum_launch.hpp"
 #include "engine_launch.hpp"
+#include "host.hpp"
 #include "inspect.hpp"
 #include "nf4_launch.hpp"
 #include "noalloc_launch.hpp"
@@ -26,48 +23,9 @@
 
 namespace {
 
-// The last failure's message on this thread (a fixed buffer: reporting an
-// error allocates nothing).
-thread_local char t_last_error[256];
-
-void set_error(const char* what, const char* detail = nullptr)
-{
-    std::snprintf(t_last_error, sizeof(t_last_error), detail ? "%s: %s" : "%s", what, detail);
-}
-
-int hip_fail(hipError_t e, const char* where)
-{
-    set_error(where, hipGetErrorString(e));
-    return MEZO_EHIP;
-}
-
-// Runs the body of a C entry point: no C++ exception crosses the C ABI. The
-// only ones the bodies can raise are host allocation failures (record lists,
-// tables) and, in principle, a failing mutex.
-template <class F>
-int guarded(const char* what, F&& body) noexcept
-{
-    try {
-        return body();
-    } catch (const std::bad_alloc&) {
-        set_error(what, "host allocation failed");
-    } catch (const std::length_error&) {
-        set_error(what, "host allocation failed");
-    } catch (const std::exception& e) {
-        set_error(what, e.what());
-        return MEZO_EINVAL;
-    } catch (...) {
-        set_error(what, "unexpected exception");
-        return MEZO_EINVAL;
-    }
-    return MEZO_ENOMEM;
-}
-
-#define MEZO_HIP(call)                                  \
-    do {                                                \
-        hipError_t err_ = (call);                       \
-        if (err_ != hipSuccess) return hip_fail(err_, #call); \
-    } while (0)
+using mezo::guarded;
+using mezo::hip_fail;
+using mezo::set_error;
 
 // ---- codec (Section 3: the projected gradient in one byte) -------------------
 
@@ -1012,8 +970,8 @@ const char* mezo_strerror(int code)
     }
 }
 
-const char* mezo_last_error(void) { return t_last_error; }
+const char* mezo_last_error(void) { return mezo::t_last_error; }
 
-int mezo_version(void) { return 500; }
+int mezo_version(void) { return 600; }
 
 }  // extern "C"

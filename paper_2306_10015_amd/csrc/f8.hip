@@ -1,0 +1,463 @@
+// f8.hip — 8-bit floating point storage and its product: what a forward pass
+// over weights that were perturbed just before computes with.
+//
+// A row is stored in blocks of 128 elements, each e4m3 codes and one scale 2^e:
+// the least power of two with max|w| <= 448 * 2^e. A power of two scales exactly,
+// so a code is w rounded once, and it is what the matrix instructions take as a
+// block's scale, so the product needs no multiply of its own for it:
+//   c_mn = sum_b 2^(ex_mb + ew_nb) sum_{k in b} x_mk w_nk.
+//
+// Two arithmetics, chosen by the output's type:
+//  bf16: v_mfma_scale_f32_16x16x128_f8f6f4. One instruction covers a block. Its
+//        inner sum of 128 products keeps about 16 bits (2-norm error of a product
+//        of normal rows 1.5e-5, with a few loud channels 5e-5, the same from 1 to
+//        128 blocks; measured), far below bf16's own rounding of 1.7e-3.
+//  fp32: the codes are widened to bf16 in registers, exactly, their scales
+//        applied, and v_mfma_f32_16x16x32_bf16 sums the exact products in fp32
+//        (error 1e-8 to 2e-7, as a chain of fp32 additions), at half the rate.
+#include <type_traits>
+
+#include "f8_launch.hpp"
+#include "records.hpp"
+#include "stream_io.hpp"
+
+namespace mezo {
+
+typedef int v8i_t __attribute__((ext_vector_type(8)));
+typedef float v4f_t __attribute__((ext_vector_type(4)));
+typedef __bf16 v2bf_t __attribute__((ext_vector_type(2)));
+typedef __bf16 v8bf_t __attribute__((ext_vector_type(8)));
+typedef MEZO_GLOBAL uint8_t gu8_t;
+typedef MEZO_GLOBAL uint32_t gu32_t;
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef MEZO_GLOBAL u32x2_t gu32x2_t;
+
+// ---- quantization --------------------------------------------------------------
+//
+// Bound by memory (fp32: 5 bytes an element, bf16: 3). A lane takes 16 bytes of a
+// row, so that loads and stores are whole lines; a block is 16 (bf16) or 32 (fp32)
+// lanes, which find its maximum by DPP. A lane starts kQuantLoads loads before it
+// uses any.
+constexpr uint32_t kQuantThreads = 256;
+constexpr uint32_t kQuantLoads = 4;
+
+template <int kCtrl>
+__device__ __forceinline__ float dpp_max(float x)
+{
+    const int y = __builtin_amdgcn_update_dpp(0, __float_as_int(x), kCtrl, 0xF, 0xF, false);
+    return fmaxf(x, __int_as_float(y));
+}
+
+// The maximum over the 16 lanes of a row of lanes.
+__device__ __forceinline__ float max16(float x)
+{
+    x = dpp_max<0xB1>(x);   // lanes 1 apart
+    x = dpp_max<0x4E>(x);   // 2 apart
+    x = dpp_max<0x141>(x);  // half a row mirrored
+    return dpp_max<0x140>(x);
+}
+
+template <uint32_t kDtype, bool kAligned>
+__global__ void __launch_bounds__(kQuantThreads) f8_quantize_kernel(F8QuantArgs a)
+{
+    constexpr uint32_t kBytes = kDtype == kF32 ? 4 : 2;
+    constexpr uint32_t kPer = 16 / kBytes;        // elements of a lane
+    constexpr uint32_t kLanes = kF8Block / kPer;  // lanes of a block
+    const uint32_t blocks = uint32_t(f8_blocks(a.cols)), per_row = blocks * kLanes;
+    const uint64_t total = uint64_t(a.rows) * per_row;
+    const uint64_t u0 = (uint64_t(blockIdx.x) * kQuantLoads) * kQuantThreads + threadIdx.x;
+    uint32_t row[kQuantLoads], col[kQuantLoads];  // col: the lane's first element
+    float w[kQuantLoads][kPer];
+#pragma unroll
+    for (uint32_t i = 0; i < kQuantLoads; ++i) {
+        const uint64_t u = u0 + i * kQuantThreads;
+        // (rows * blocks < 2^27: 32 bits hold every unit)
+        row[i] = uint32_t(u) / per_row;
+        col[i] = (uint32_t(u) - row[i] * per_row) * kPer;
+        const uint64_t at = a.values + (row[i] * a.ld + col[i]) * kBytes;
+        if (u >= total) col[i] = a.cols + kPer;  // nothing to read
+        if (kAligned && col[i] + kPer <= a.cols) {
+            const uint4 v = load_stream(at);
+            const uint32_t p[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                if constexpr (kDtype == kF32) {
+                    w[i][j] = __uint_as_float(p[j]);
+                } else {
+                    w[i][2 * j] = __uint_as_float(p[j] << 16);
+                    w[i][2 * j + 1] = __uint_as_float(p[j] & 0xFFFF0000u);
+                }
+            }
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < kPer; ++j) {
+                w[i][j] = 0.0f;
+                if (col[i] + j < a.cols) {
+                    if constexpr (kDtype == kF32)
+                        w[i][j] = reinterpret_cast<const gfloat_t*>(at)[j];
+                    else
+                        w[i][j] = __uint_as_float(uint32_t(reinterpret_cast<const gu16_t*>(at)[j]) << 16);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kQuantLoads; ++i) {
+        float top = 0.0f;  // of the finite values: inf and NaN are coded NaN and scale nothing
+#pragma unroll
+        for (uint32_t j = 0; j < kPer; ++j) {
+            const float m = fabsf(w[i][j]);
+            top = fmaxf(top, m < __builtin_inff() ? m : 0.0f);
+        }
+        top = max16(top);
+        if constexpr (kLanes == 32) top = fmaxf(top, __shfl_xor(top, 16));
+        // top = (1 + f) 2^x: e = x - 8, one more where 1 + f > 1.75 = 448 / 2^8
+        const uint32_t bits = __float_as_uint(top);
+        int e = int(bits >> 23) - 127 - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+        e = bits == 0 ? 0 : (e < -127 ? -127 : e);
+        const float inv = __uint_as_float(uint32_t(127 - e) << 23);
+        uint32_t code[kPer / 4];
+#pragma unroll
+        for (uint32_t j = 0; j < kPer; j += 4) {
+            int c = __builtin_amdgcn_cvt_pk_fp8_f32(w[i][j] * inv, w[i][j + 1] * inv, 0, false);
+            c = __builtin_amdgcn_cvt_pk_fp8_f32(w[i][j + 2] * inv, w[i][j + 3] * inv, c, true);
+            code[j / 4] = uint32_t(c);
+        }
+        if (u0 + i * kQuantThreads >= total) continue;
+        const uint32_t block = col[i] / kF8Block;
+        const uint64_t at = a.codes + uint64_t(row[i]) * blocks * kF8Block + col[i];
+        if constexpr (kPer == 8)
+            *reinterpret_cast<gu32x2_t*>(at) = u32x2_t{code[0], code[1]};
+        else
+            *reinterpret_cast<gu32_t*>(at) = code[0];
+        // the block's scale, and after the last one's the row's padding
+        const uint32_t stride = uint32_t(f8_scale_stride(a.cols)), lane = col[i] % kF8Block / kPer;
+        gu8_t* s = reinterpret_cast<gu8_t*>(a.scales) + uint64_t(row[i]) * stride;
+        if (lane == 0) s[block] = uint8_t(e + 127);
+        if (block == blocks - 1 && lane > 0 && block + lane < stride) s[block + lane] = 0;
+    }
+}
+
+hipError_t launch_f8_quantize(const F8QuantArgs& args, hipStream_t stream)
+{
+    const uint32_t bytes = args.dtype == kF32 ? 4 : 2;
+    const bool aligned = ((args.values | (args.ld * bytes)) & 15u) == 0;
+    const uint64_t units = uint64_t(args.rows) * f8_blocks(args.cols) * (kF8Block * bytes / 16);
+    const uint64_t per = kQuantThreads * kQuantLoads;
+    F8QuantArgs a = args;
+    void* params[] = {&a};
+    const void* f;
+    if (args.dtype == kF32)
+        f = aligned ? reinterpret_cast<const void*>(f8_quantize_kernel<kF32, true>)
+                    : reinterpret_cast<const void*>(f8_quantize_kernel<kF32, false>);
+    else
+        f = aligned ? reinterpret_cast<const void*>(f8_quantize_kernel<kBF16, true>)
+                    : reinterpret_cast<const void*>(f8_quantize_kernel<kBF16, false>);
+    return hipLaunchKernel(f, dim3(uint32_t((units + per - 1) / per)), dim3(kQuantThreads), params, 0, stream);
+}
+
+// ---- the product ----------------------------------------------------------------
+
+// A lane's 32 codes of a row's block, ready for the matrix instructions. Which 32
+// of the 128 a lane holds does not matter as long as both operands agree: a block
+// has one scale and the sum over it has no order.
+template <bool kWide>
+struct Operand;
+
+template <>
+struct Operand<false> {
+    v8i_t v;
+    int scale;  // the biased exponent in the low byte
+    __device__ __forceinline__ void set(uint4 lo, uint4 hi, uint32_t s)
+    {
+        v = v8i_t{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
+        scale = int(s);
+    }
+};
+
+template <>
+struct Operand<true> {
+    v8bf_t v[4];
+    __device__ __forceinline__ void set(uint4 lo, uint4 hi, uint32_t s)
+    {
+        const float scale = __uint_as_float((s & 0xFFu) << 23);  // (the exponent is all the conversion reads)
+        const uint32_t d[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const v2bf_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d[2 * q + h], scale, false);
+                const v2bf_t b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d[2 * q + h], scale, true);
+                v[q][4 * h] = a.x;
+                v[q][4 * h + 1] = a.y;
+                v[q][4 * h + 2] = b.x;
+                v[q][4 * h + 3] = b.y;
+            }
+        }
+    }
+};
+
+__device__ __forceinline__ v4f_t mma(const Operand<false>& a, const Operand<false>& b, v4f_t c)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, c, 0, 0, 0, a.scale, 0, b.scale);
+}
+
+__device__ __forceinline__ v4f_t mma(const Operand<true>& a, const Operand<true>& b, v4f_t c)
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[q], b.v[q], c, 0, 0, 0);
+    return c;
+}
+
+// A lane's four results, columns col .. col + 3 of a row of c.
+__device__ __forceinline__ void store4(const F8MatmulArgs& a, uint32_t row, uint32_t col, v4f_t v)
+{
+    const uint64_t e = row * a.ldc + col;
+    if (a.out_dtype == kF32) {
+        gfloat_t* p = reinterpret_cast<gfloat_t*>(a.c) + e;
+        if (col + 4 <= a.n && ((a.c | (a.ldc * 4)) & 15u) == 0) {
+            *reinterpret_cast<MEZO_GLOBAL v4f_t*>(p) = v;
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i)
+                if (col + i < a.n) p[i] = v[i];
+        }
+        return;
+    }
+    typedef __bf16 v4bf_t __attribute__((ext_vector_type(4)));
+    const v4bf_t b = __builtin_convertvector(v, v4bf_t);
+    MEZO_GLOBAL __bf16* p = reinterpret_cast<MEZO_GLOBAL __bf16*>(a.c) + e;
+    if (col + 4 <= a.n && ((a.c | (a.ldc * 2)) & 7u) == 0) {
+        *reinterpret_cast<MEZO_GLOBAL v4bf_t*>(p) = b;
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            if (col + i < a.n) p[i] = b[i];
+    }
+}
+
+// 16 bytes that other workgroups read too.
+__device__ __forceinline__ uint4 load_shared(uint64_t addr)
+{
+    const u32x4_t v = *reinterpret_cast<const gu32x4_t*>(addr);
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+
+// 16 bytes from global memory straight into LDS: lane l's go to lds + 16 l.
+__device__ __forceinline__ void load_to_lds(uint64_t addr, const void* lds)
+{
+    __builtin_amdgcn_global_load_lds(reinterpret_cast<const MEZO_GLOBAL void*>(addr),
+                                     (__attribute__((address_space(3))) void*)(lds), 16, 0, 0);
+}
+
+// Tiles of kBM activations x kBN weights, kWM x kWN waves. Weights are the matrix
+// instruction's rows and activations its columns, so that a lane's four results
+// lie next to each other in a row of c.
+//
+// A stage is one block of 128 of every row of the tile, loaded straight into LDS;
+// two stages, one computed on while the other loads. A row's eight 16-byte chunks
+// are stored at chunk ^ (row & 7): the 16 rows of a fragment then spread over all
+// banks.
+template <uint32_t kBM, uint32_t kBN, uint32_t kWM, uint32_t kWN, bool kWide>
+__global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a)
+{
+    constexpr uint32_t kWaves = kWM * kWN, kRows = kBM + kBN;
+    constexpr uint32_t kFM = kBM / kWM / 16, kFN = kBN / kWN / 16;  // fragments of a wave
+    constexpr uint32_t kLoads = kRows / 8 / kWaves;                 // 8 rows a load
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][kRows * 128];
+
+    const uint32_t l = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // workgroups go round the 8 XCDs: give each XCD a compact part of c (its L2 then
+    // holds the rows its workgroups share), in groups of 8 tile rows
+    const uint32_t tm = (a.m + kBM - 1) / kBM, tn = (a.n + kBN - 1) / kBN, tiles = tm * tn;
+    const uint32_t xcd = blockIdx.x % 8, each = tiles / 8, rest = tiles % 8;
+    const uint32_t id = blockIdx.x / 8 + xcd * each + (xcd < rest ? xcd : rest);
+    const uint32_t band = id / (8 * tn), height = tm - band * 8 < 8 ? tm - band * 8 : 8;
+    const uint32_t in = id - band * 8 * tn;
+    const uint32_t m0 = (band * 8 + in % height) * kBM, n0 = in / height * kBN;
+
+    const uint32_t blocks = uint32_t(f8_blocks(a.k));
+    const uint64_t stride = f8_code_stride(a.k);
+    // this lane's 16 bytes of each of its rows (past the end: the last row's again)
+    uint64_t src[kLoads];
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) {
+        const uint32_t r = (wave * kLoads + i) * 8 + (l >> 3);
+        const uint32_t chunk = (l & 7u) ^ (l >> 3);
+        const uint32_t xr = m0 + r < a.m ? m0 + r : a.m - 1;
+        const uint32_t wr = n0 + r - kBM < a.n ? n0 + r - kBM : a.n - 1;
+        src[i] = (r < kBM ? a.x + xr * stride : a.w + wr * stride) + chunk * 16;
+    }
+    const uint32_t fr = l & 15u, fg = l >> 4;
+    const uint32_t wm = (wave / kWN) * kFM * 16, wn = (wave % kWN) * kFN * 16;
+    const uint64_t sstride = f8_scale_stride(a.k);
+    uint64_t xs[kFM], ws[kFN];
+#pragma unroll
+    for (uint32_t i = 0; i < kFM; ++i) {
+        const uint32_t r = m0 + wm + i * 16 + fr;
+        xs[i] = a.xs + (r < a.m ? r : a.m - 1) * sstride;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kFN; ++i) {
+        const uint32_t r = n0 + wn + i * 16 + fr;
+        ws[i] = a.ws + (r < a.n ? r : a.n - 1) * sstride;
+    }
+    v4f_t acc[kFM][kFN] = {};
+    auto stage = [&](uint32_t kb) {
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i)
+            load_to_lds(src[i] + uint64_t(kb) * 128, &lds[kb & 1][(wave * kLoads + i) * 1024]);
+    };
+    uint32_t sx[kFM], sw[kFN], nx[kFM], nw[kFN];  // the scales of four blocks, and of the next four
+    auto scales = [&](uint32_t kb) {
+#pragma unroll
+        for (uint32_t i = 0; i < kFM; ++i) nx[i] = *reinterpret_cast<const gu32_t*>(xs[i] + kb);
+#pragma unroll
+        for (uint32_t i = 0; i < kFN; ++i) nw[i] = *reinterpret_cast<const gu32_t*>(ws[i] + kb);
+    };
+    scales(0);
+    stage(0);
+    for (uint32_t kb = 0; kb < blocks; ++kb) {
+        __syncthreads();  // stage kb is there, and nobody reads the other one any more
+        if ((kb & 3u) == 0) {
+#pragma unroll
+            for (uint32_t i = 0; i < kFM; ++i) sx[i] = nx[i];
+#pragma unroll
+            for (uint32_t i = 0; i < kFN; ++i) sw[i] = nw[i];
+            if (kb + 4 < blocks) scales(kb + 4);
+        }
+        if (kb + 1 < blocks) stage(kb + 1);
+        const uint8_t* t = lds[kb & 1];
+        const uint32_t shift = (kb & 3u) * 8;
+        auto fragment = [&](uint32_t row) {
+            const uint32_t r = row + fr;
+            struct {
+                uint4 lo, hi;
+            } f;
+            f.lo = *reinterpret_cast<const uint4*>(t + r * 128 + ((fg ^ (fr & 7u)) * 16));
+            f.hi = *reinterpret_cast<const uint4*>(t + r * 128 + (((fg + 4) ^ (fr & 7u)) * 16));
+            return f;
+        };
+        Operand<kWide> w[kFN];
+#pragma unroll
+        for (uint32_t j = 0; j < kFN; ++j) {
+            const auto f = fragment(kBM + wn + j * 16);
+            w[j].set(f.lo, f.hi, sw[j] >> shift);
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kFM; ++i) {
+            const auto f = fragment(wm + i * 16);
+            Operand<kWide> x;
+            x.set(f.lo, f.hi, sx[i] >> shift);
+#pragma unroll
+            for (uint32_t j = 0; j < kFN; ++j) acc[i][j] = mma(w[j], x, acc[i][j]);
+        }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kFM; ++i) {
+        const uint32_t row = m0 + wm + i * 16 + fr;
+        if (row < a.m) {
+#pragma unroll
+            for (uint32_t j = 0; j < kFN; ++j) store4(a, row, n0 + wn + j * 16 + fg * 4, acc[i][j]);
+        }
+    }
+}
+
+// A product of few activations: bound by the weights' bytes. A workgroup takes 16
+// weights' rows and all m <= 16 kFM activations; its waves share out the blocks of
+// k and load both operands from global memory straight into registers, a few
+// blocks ahead; their sums join through LDS in the order of the waves.
+constexpr uint32_t kThinAhead = 4;
+
+template <uint32_t kFM, uint32_t kWaves, bool kWide>
+__global__ void __launch_bounds__(kWaves * 64) f8_thin_kernel(F8MatmulArgs a)
+{
+    const uint32_t l = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t fr = l & 15u, fg = l >> 4, n0 = blockIdx.x * 16;
+    const uint32_t blocks = uint32_t(f8_blocks(a.k));
+    const uint64_t stride = f8_code_stride(a.k), sstride = f8_scale_stride(a.k);
+    const uint32_t b0 = blocks * wave / kWaves, b1 = blocks * (wave + 1) / kWaves;
+    const uint64_t wr = n0 + fr < a.n ? n0 + fr : a.n - 1;
+    const uint64_t w = a.w + wr * stride + fg * 16, ws = a.ws + wr * sstride;
+    uint64_t x[kFM], xs[kFM];
+#pragma unroll
+    for (uint32_t i = 0; i < kFM; ++i) {
+        const uint64_t r = i * 16 + fr < a.m ? i * 16 + fr : a.m - 1;
+        x[i] = a.x + r * stride + fg * 16;
+        xs[i] = a.xs + r * sstride;
+    }
+    v4f_t acc[kFM] = {};
+    auto run = [&](auto ahead, uint32_t kb) {
+        constexpr uint32_t kN = decltype(ahead)::value;
+        uint4 lo[kN], hi[kN], xlo[kN][kFM], xhi[kN][kFM];
+        uint32_t s[kN], sx[kN][kFM];
+#pragma unroll
+        for (uint32_t d = 0; d < kN; ++d) {
+            const uint64_t b = kb + d;
+            lo[d] = load_stream(w + b * 128);
+            hi[d] = load_stream(w + b * 128 + 64);
+            s[d] = reinterpret_cast<const gu8_t*>(ws)[b];
+#pragma unroll
+            for (uint32_t i = 0; i < kFM; ++i) {
+                xlo[d][i] = load_shared(x[i] + b * 128);
+                xhi[d][i] = load_shared(x[i] + b * 128 + 64);
+                sx[d][i] = reinterpret_cast<const gu8_t*>(xs[i])[b];
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);  // all loads before the first use
+#pragma unroll
+        for (uint32_t d = 0; d < kN; ++d) {
+            Operand<kWide> wo;
+            wo.set(lo[d], hi[d], s[d]);
+#pragma unroll
+            for (uint32_t i = 0; i < kFM; ++i) {
+                Operand<kWide> xo;
+                xo.set(xlo[d][i], xhi[d][i], sx[d][i]);
+                acc[i] = mma(wo, xo, acc[i]);
+            }
+        }
+    };
+    uint32_t kb = b0;
+    for (; kb + kThinAhead <= b1; kb += kThinAhead) run(std::integral_constant<uint32_t, kThinAhead>{}, kb);
+    for (; kb < b1; ++kb) run(std::integral_constant<uint32_t, 1>{}, kb);
+    __shared__ v4f_t part[kWaves][kFM][64];
+#pragma unroll
+    for (uint32_t i = 0; i < kFM; ++i) part[wave][i][l] = acc[i];
+    __syncthreads();
+    for (uint32_t i = wave; i < kFM; i += kWaves) {
+        v4f_t sum = part[0][i][l];
+#pragma unroll
+        for (uint32_t v = 1; v < kWaves; ++v) sum += part[v][i][l];
+        if (i * 16 + fr < a.m) store4(a, i * 16 + fr, n0 + fg * 4, sum);
+    }
+}
+
+uint64_t f8_matmul_workspace(uint64_t, uint64_t, uint64_t, uint32_t) { return 0; }
+
+template <bool kWide>
+hipError_t launch_product(F8MatmulArgs a, hipStream_t stream)
+{
+    void* params[] = {&a};
+    auto go = [&](const void* f, uint32_t groups, uint32_t lanes) {
+        return hipLaunchKernel(f, dim3(groups), dim3(lanes), params, 0, stream);
+    };
+    if (a.m <= 64) {
+        const uint32_t groups = (a.n + 15) / 16;
+        if (a.m <= 16) return go(reinterpret_cast<const void*>(f8_thin_kernel<1, 4, kWide>), groups, 256);
+        if (a.m <= 32) return go(reinterpret_cast<const void*>(f8_thin_kernel<2, 4, kWide>), groups, 256);
+        return go(reinterpret_cast<const void*>(f8_thin_kernel<4, 4, kWide>), groups, 256);
+    }
+    auto tiles = [&](uint32_t bm, uint32_t bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
+    if constexpr (!kWide) {
+        if (tiles(256, 256) >= 256)
+            return go(reinterpret_cast<const void*>(f8_matmul_kernel<256, 256, 2, 4, false>), tiles(256, 256), 512);
+    }
+    return go(reinterpret_cast<const void*>(f8_matmul_kernel<128, 128, 2, 2, kWide>), tiles(128, 128), 256);
+}
+
+hipError_t launch_f8_matmul(const F8MatmulArgs& args, hipStream_t stream)
+{
+    return args.out_dtype == kF32 ? launch_product<true>(args, stream) : launch_product<false>(args, stream);
+}
+
+}  // namespace mezo

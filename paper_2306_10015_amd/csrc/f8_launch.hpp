@@ -1,0 +1,42 @@
+// f8_launch.hpp — interface between the C-ABI host code (forward.cpp) and the
+// 8-bit storage kernels (f8.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace mezo {
+
+// Elements of a row that share a scale, and the bytes of a stored row.
+constexpr uint64_t kF8Block = 128;
+constexpr uint64_t f8_blocks(uint64_t cols) { return (cols + kF8Block - 1) / kF8Block; }
+constexpr uint64_t f8_code_stride(uint64_t cols) { return f8_blocks(cols) * kF8Block; }
+constexpr uint64_t f8_scale_stride(uint64_t cols) { return (f8_blocks(cols) + 3) / 4 * 4; }
+
+struct F8QuantArgs {
+    uint64_t values;  // device address, fp32 or bf16
+    uint64_t ld;      // elements from one row to the next
+    uint64_t codes;
+    uint64_t scales;
+    uint32_t rows;
+    uint32_t cols;
+    uint32_t dtype;
+};
+
+struct F8MatmulArgs {
+    uint64_t x, xs;  // codes and scales of the m activations' rows
+    uint64_t w, ws;  // and of the n weights' rows
+    uint64_t c;      // [m, n] of out_dtype
+    uint64_t ldc;    // elements from one row of c to the next
+    uint64_t partial;  // fp32 [splits, m, n] of a split product
+    uint32_t m, n, k;
+    uint32_t out_dtype;
+};
+
+hipError_t launch_f8_quantize(const F8QuantArgs& args, hipStream_t stream);
+
+// Bytes of `partial` a product of these sizes needs (0: not split).
+uint64_t f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t out_dtype);
+hipError_t launch_f8_matmul(const F8MatmulArgs& args, hipStream_t stream);
+
+}  // namespace mezo

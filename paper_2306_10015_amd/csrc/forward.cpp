@@ -1,0 +1,202 @@
+// forward.cpp — the C ABI of the forward pass's operators (include/mezo.h):
+// argument checks and launches on the caller's stream. Nothing here allocates;
+// scratch memory is the caller's.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/mezo.h"
+#include "f8_launch.hpp"
+#include "host.hpp"
+#include "token_loss_launch.hpp"
+
+namespace {
+
+using mezo::guarded;
+
+uint64_t address(const void* p) { return reinterpret_cast<uint64_t>(p); }
+
+bool aligned(const void* p, uint64_t bytes) { return (address(p) & (bytes - 1)) == 0; }
+
+bool dense(uint32_t dtype) { return dtype == MEZO_F32 || dtype == MEZO_BF16; }
+
+uint64_t element_bytes(uint32_t dtype) { return dtype == MEZO_F32 ? 4 : 2; }
+
+// The bytes of rows rows of cols elements, ld apart (false: past 64 bits).
+bool matrix_bytes(uint64_t rows, uint64_t cols, uint64_t ld, uint64_t element, uint64_t& bytes)
+{
+    return !__builtin_mul_overflow(rows - 1, ld, &bytes) && !__builtin_add_overflow(bytes, cols, &bytes) &&
+           !__builtin_mul_overflow(bytes, element, &bytes);
+}
+
+struct Range {
+    uint64_t at, bytes;
+};
+
+bool overlap(Range a, Range b) { return a.at < b.at + b.bytes && b.at < a.at + a.bytes; }
+
+// Whether a buffer that is written shares memory with one of n others.
+bool clashes(Range out, const Range* others, int n)
+{
+    for (int i = 0; i < n; ++i)
+        if (overlap(out, others[i])) return true;
+    return false;
+}
+
+// ---- 8-bit storage -----------------------------------------------------------
+
+// Sizes of an 8-bit matrix.
+bool f8_sizes(uint64_t rows, uint64_t cols)
+{
+    return rows >= 1 && cols >= 1 && rows <= MEZO_F8_MAX_ROWS && cols <= MEZO_F8_MAX_COLS &&
+           rows <= MEZO_MAX_NUMEL / mezo::f8_code_stride(cols);
+}
+
+Range f8_codes(const void* codes, uint64_t rows, uint64_t cols)
+{
+    return {address(codes), rows * mezo::f8_code_stride(cols)};
+}
+
+Range f8_scales(const void* scales, uint64_t rows, uint64_t cols)
+{
+    return {address(scales), rows * mezo::f8_scale_stride(cols)};
+}
+
+int f8_quantize(const void* src, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ld, void* codes, uint8_t* scales,
+                void* stream)
+{
+    if (!dense(dtype)) return MEZO_EDTYPE;
+    if (!src || !codes || !scales || !f8_sizes(rows, cols) || (rows > 1 && ld < cols)) return MEZO_EINVAL;
+    if (!aligned(src, element_bytes(dtype)) || !aligned(codes, 16) || !aligned(scales, 4)) return MEZO_EINVAL;
+    uint64_t bytes;
+    if (!matrix_bytes(rows, cols, ld, element_bytes(dtype), bytes)) return MEZO_EINVAL;
+    const Range in = {address(src), bytes}, c = f8_codes(codes, rows, cols), s = f8_scales(scales, rows, cols);
+    const Range read[2] = {in, c};
+    if (clashes(c, &in, 1) || clashes(s, read, 2)) return MEZO_EOVERLAP;
+    mezo::F8QuantArgs a;
+    a.values = in.at;
+    a.ld = ld;
+    a.codes = c.at;
+    a.scales = s.at;
+    a.rows = static_cast<uint32_t>(rows);
+    a.cols = static_cast<uint32_t>(cols);
+    a.dtype = dtype;
+    MEZO_HIP(mezo::launch_f8_quantize(a, static_cast<hipStream_t>(stream)));
+    return MEZO_OK;
+}
+
+int f8_matmul(const void* x_codes, const uint8_t* x_scales, const void* w_codes, const uint8_t* w_scales, uint64_t m,
+              uint64_t n, uint64_t k, void* c, uint32_t c_dtype, uint64_t ldc, void* workspace,
+              uint64_t workspace_bytes, void* stream)
+{
+    if (!dense(c_dtype)) return MEZO_EDTYPE;
+    if (!x_codes || !x_scales || !w_codes || !w_scales || !c || !f8_sizes(m, k) || !f8_sizes(n, k) ||
+        m > MEZO_MAX_NUMEL / n || (m > 1 && ldc < n))
+        return MEZO_EINVAL;
+    if (!aligned(x_codes, 16) || !aligned(w_codes, 16) || !aligned(x_scales, 4) || !aligned(w_scales, 4) ||
+        !aligned(c, element_bytes(c_dtype)))
+        return MEZO_EINVAL;
+    const uint64_t need = mezo::f8_matmul_workspace(m, n, k, c_dtype);
+    if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return MEZO_EINVAL;
+    uint64_t bytes;
+    if (!matrix_bytes(m, n, ldc, element_bytes(c_dtype), bytes)) return MEZO_EINVAL;
+    const Range out = {address(c), bytes}, scratch = {address(workspace), need};
+    const Range read[5] = {f8_codes(x_codes, m, k), f8_scales(x_scales, m, k), f8_codes(w_codes, n, k),
+                           f8_scales(w_scales, n, k), out};
+    if (clashes(out, read, 4) || (need && clashes(scratch, read, 5))) return MEZO_EOVERLAP;
+    mezo::F8MatmulArgs a;
+    a.x = read[0].at;
+    a.xs = read[1].at;
+    a.w = read[2].at;
+    a.ws = read[3].at;
+    a.c = out.at;
+    a.ldc = ldc;
+    a.partial = scratch.at;
+    a.m = static_cast<uint32_t>(m);
+    a.n = static_cast<uint32_t>(n);
+    a.k = static_cast<uint32_t>(k);
+    a.out_dtype = c_dtype;
+    MEZO_HIP(mezo::launch_f8_matmul(a, static_cast<hipStream_t>(stream)));
+    return MEZO_OK;
+}
+
+// ---- the token loss ------------------------------------------------------------
+
+uint64_t loss_workspace(uint64_t rows, uint64_t vocab)
+{
+    if (rows == 0 || vocab == 0) return 0;
+    const uint64_t parts = mezo::loss_parts(rows, vocab);
+    return parts > 1 ? rows * parts * sizeof(float2) : 0;
+}
+
+int token_loss(const void* logits, uint32_t dtype, uint64_t rows, uint64_t vocab, uint64_t ld, const int64_t* targets,
+               float* losses, float* mean, void* workspace, uint64_t workspace_bytes, void* stream)
+{
+    if (!dense(dtype)) return MEZO_EDTYPE;
+    if (rows == 0) return MEZO_EINVAL;
+    if (!logits || !targets || !losses || vocab == 0 || rows > MEZO_LOSS_MAX_ROWS || (rows > 1 && ld < vocab))
+        return MEZO_EINVAL;
+    if (!aligned(logits, element_bytes(dtype)) || !aligned(targets, 8) || !aligned(losses, 4) || !aligned(mean, 4))
+        return MEZO_EINVAL;
+    uint64_t bytes;
+    if (!matrix_bytes(rows, vocab, ld, element_bytes(dtype), bytes)) return MEZO_EINVAL;
+    const uint64_t need = loss_workspace(rows, vocab);
+    if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return MEZO_EINVAL;
+    const Range read[5] = {{address(logits), bytes}, {address(targets), rows * 8}, {address(losses), rows * 4},
+                           {address(mean), mean ? 4u : 0u}, {address(workspace), need}};
+    if (clashes(read[2], read, 2) || (mean && clashes(read[3], read, 3)) || (need && clashes(read[4], read, 4)))
+        return MEZO_EOVERLAP;
+    mezo::LossArgs a;
+    a.logits = read[0].at;
+    a.ld = ld;
+    a.vocab = vocab;
+    a.targets = targets;
+    a.losses = losses;
+    a.mean = mean;
+    a.rows = static_cast<uint32_t>(rows);
+    a.parts = mezo::loss_parts(rows, vocab);
+    a.partial = need ? static_cast<float2*>(workspace) : nullptr;
+    a.dtype = dtype;
+    MEZO_HIP(mezo::launch_token_loss(a, static_cast<hipStream_t>(stream)));
+    return MEZO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int mezo_f8_quantize(const void* src, uint32_t src_dtype, uint64_t rows, uint64_t cols, uint64_t ld, void* codes,
+                     uint8_t* scales, void* stream)
+{
+    return guarded("mezo_f8_quantize",
+                   [&] { return f8_quantize(src, src_dtype, rows, cols, ld, codes, scales, stream); });
+}
+
+uint64_t mezo_f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t c_dtype)
+{
+    return dense(c_dtype) && f8_sizes(m, k) && f8_sizes(n, k) ? mezo::f8_matmul_workspace(m, n, k, c_dtype) : 0;
+}
+
+int mezo_f8_matmul(const void* x_codes, const uint8_t* x_scales, const void* w_codes, const uint8_t* w_scales,
+                   uint64_t m, uint64_t n, uint64_t k, void* c, uint32_t c_dtype, uint64_t ldc, void* workspace,
+                   uint64_t workspace_bytes, void* stream)
+{
+    return guarded("mezo_f8_matmul", [&] {
+        return f8_matmul(x_codes, x_scales, w_codes, w_scales, m, n, k, c, c_dtype, ldc, workspace, workspace_bytes,
+                         stream);
+    });
+}
+
+uint64_t mezo_token_loss_workspace(uint64_t rows, uint64_t vocab) { return loss_workspace(rows, vocab); }
+
+int mezo_token_loss(const void* logits, uint32_t dtype, uint64_t rows, uint64_t vocab, uint64_t ld,
+                    const int64_t* targets, float* losses, float* mean, void* workspace, uint64_t workspace_bytes,
+                    void* stream)
+{
+    return guarded("mezo_token_loss", [&] {
+        return token_loss(logits, dtype, rows, vocab, ld, targets, losses, mean, workspace, workspace_bytes, stream);
+    });
+}
+
+}  // extern "C"

@@ -29,6 +29,8 @@ OK, EINVAL, EDTYPE, EOVERLAP, EORDER, ERANGE, EHIP, ENOMEM = 0, -1, -2, -3, -4, 
 F32, BF16, NF4 = 0, 1, 2
 #: NF4 elements per absmax value.
 NF4_BLOCK = 64
+#: 8-bit storage: elements of a row that share a scale.
+F8_BLOCK = 128
 GAUSS_FAST, GAUSS_PORTABLE = 0, 1
 LINEAR, SIGNED_LOG = 0, 1
 #: Signed-log slope of a base-2 log: code 127 decodes just inside fp32.
@@ -65,7 +67,9 @@ EXPORTS = ("mezo_paramset_create", "mezo_paramset_destroy", "mezo_paramset_numel
            "mezo_perturb", "mezo_perturb_multi", "mezo_update_multi", "mezo_replay", "mezo_replay_noalloc",
            "mezo_perturb_from",
            "mezo_update_multi_from", "mezo_checksum", "quantize_projgrad",
-           "mezo_dequantize", "mezo_nf4_quantize", "mezo_nf4_dequantize", "mezo_debug_generate", "mezo_debug_box_muller",
+           "mezo_dequantize", "mezo_nf4_quantize", "mezo_nf4_dequantize",
+           "mezo_f8_quantize", "mezo_f8_matmul_workspace", "mezo_f8_matmul",
+           "mezo_token_loss_workspace", "mezo_token_loss", "mezo_debug_generate", "mezo_debug_box_muller",
            "mezo_strerror", "mezo_last_error", "mezo_version")
 
 
@@ -112,6 +116,16 @@ def _load() -> ctypes.CDLL:
     L.mezo_nf4_quantize.restype = i32
     L.mezo_nf4_dequantize.argtypes = [vp, vp, u64, vp, u32, vp]
     L.mezo_nf4_dequantize.restype = i32
+    L.mezo_f8_quantize.argtypes = [vp, u32, u64, u64, u64, vp, vp, vp]
+    L.mezo_f8_quantize.restype = i32
+    L.mezo_f8_matmul_workspace.argtypes = [u64, u64, u64, u32]
+    L.mezo_f8_matmul_workspace.restype = u64
+    L.mezo_f8_matmul.argtypes = [vp, vp, vp, vp, u64, u64, u64, vp, u32, u64, vp, u64, vp]
+    L.mezo_f8_matmul.restype = i32
+    L.mezo_token_loss_workspace.argtypes = [u64, u64]
+    L.mezo_token_loss_workspace.restype = u64
+    L.mezo_token_loss.argtypes = [vp, u32, u64, u64, u64, vp, vp, vp, vp, u64, vp]
+    L.mezo_token_loss.restype = i32
     L.mezo_debug_generate.argtypes = [Seed, u32, u64, u64, u32, vp, vp, vp]
     L.mezo_debug_generate.restype = i32
     L.mezo_debug_box_muller.argtypes = [vp, u64, u32, vp, vp]
@@ -244,6 +258,156 @@ def nf4_dequantize(t: NF4Tensor, dtype=None, out=None, stream=None):
         _check(lib.mezo_nf4_dequantize(t.codes.data_ptr(), t.absmax.data_ptr(), t.numel(), out.data_ptr(),
                                        _dtype_code(out), _stream_ptr(stream)), "mezo_nf4_dequantize")
     return out
+
+
+# ---- the forward pass ------------------------------------------------------
+
+def _on(device, stream):
+    """Run a call on `device`, its outputs and scratch allocated on the stream
+    it runs on (memory of another stream's pool could still be in use there)."""
+    import contextlib
+    import torch
+    stack = contextlib.ExitStack()
+    if torch.cuda.device_count() > 1:
+        stack.enter_context(torch.cuda.device(device))
+    if stream is not None:
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), device=device)
+        stack.enter_context(torch.cuda.stream(stream))
+    return stack
+
+
+def _rows_of(t, what: str):
+    """A 2-D CUDA tensor whose rows are contiguous, and the elements between them."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what}: a 2-D CUDA tensor")
+    rows, cols = t.shape
+    if rows == 0 or cols == 0:
+        raise ValueError(f"{what}: empty")
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        raise ValueError(f"{what}: the elements of a row must be contiguous")
+    return rows, cols, t.stride(0) if rows > 1 else cols
+
+
+def _same_device(*tensors):
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1:
+        raise ValueError(f"tensors on several devices: {sorted(map(str, devices))}")
+
+
+def _scratch(nbytes: int, device):
+    import torch
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+class F8Matrix:
+    """A [rows, cols] matrix in 8-bit storage: ``codes`` (uint8, [rows, B * 128]
+    with B = ceil(cols / 128) blocks a row, e4m3, zeros after the last column)
+    and ``scales`` (uint8, [rows, B rounded up to a multiple of 4], a block's
+    scale 2^(byte - 127)), both contiguous device tensors owned by torch."""
+
+    def __init__(self, codes, scales, rows: int, cols: int):
+        import torch
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+            raise TypeError("codes and scales must be uint8")
+        rows, cols = int(rows), int(cols)
+        blocks = (cols + F8_BLOCK - 1) // F8_BLOCK
+        if rows < 1 or cols < 1 or codes.shape != (rows, blocks * F8_BLOCK) \
+                or scales.shape != (rows, (blocks + 3) // 4 * 4):
+            raise ValueError("codes / scales do not have the sizes of a [rows, cols] matrix")
+        if not (codes.is_cuda and scales.is_cuda and codes.is_contiguous() and scales.is_contiguous()):
+            raise ValueError("codes and scales must be contiguous CUDA tensors")
+        _same_device(codes, scales)
+        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device="cuda") -> "F8Matrix":
+        import torch
+        blocks = (int(cols) + F8_BLOCK - 1) // F8_BLOCK
+        return cls(torch.empty(rows, blocks * F8_BLOCK, dtype=torch.uint8, device=device),
+                   torch.empty(rows, (blocks + 3) // 4 * 4, dtype=torch.uint8, device=device), rows, cols)
+
+    @property
+    def shape(self):
+        return self.rows, self.cols
+
+    @property
+    def device(self):
+        return self.codes.device
+
+
+def f8_quantize(values, out: F8Matrix | None = None, stream=None) -> F8Matrix:
+    """values (fp32/bf16 [rows, cols], contiguous rows) -> 8-bit storage."""
+    rows, cols, ld = _rows_of(values, "values")
+    dtype = _dtype_code(values)
+    if out is not None and out.shape != (rows, cols):
+        raise ValueError(f"out is {out.shape}, values {(rows, cols)}")
+    with _on(values.device, stream):
+        out = F8Matrix.empty(rows, cols, values.device) if out is None else out
+        _same_device(values, out.codes)
+        _check(lib.mezo_f8_quantize(values.data_ptr(), dtype, rows, cols, ld, out.codes.data_ptr(),
+                                    out.scales.data_ptr(), _stream_ptr(None)), "mezo_f8_quantize")
+    return out
+
+
+def f8_matmul(x: F8Matrix, w: F8Matrix, dtype=None, out=None, stream=None):
+    """x w^T of two 8-bit matrices, [m, k] and [n, k], as a [m, n] tensor of
+    dtype (torch.bfloat16, the default, or torch.float32: see mezo_f8_matmul)."""
+    import torch
+    if x.cols != w.cols:
+        raise ValueError(f"x has {x.cols} columns, w {w.cols}")
+    m, n, k = x.rows, w.rows, x.cols
+    with _on(x.device, stream):
+        if out is None:
+            out = torch.empty(m, n, dtype=dtype or torch.bfloat16, device=x.device)
+        elif dtype is not None and out.dtype != dtype:
+            raise TypeError(f"out is {out.dtype}, dtype {dtype}")
+        if out.shape != (m, n):
+            raise ValueError(f"out is {tuple(out.shape)}, the product {(m, n)}")
+        _same_device(x.codes, w.codes, out)
+        code, ldc = _dtype_code(out), _rows_of(out, "out")[2]
+        nbytes = lib.mezo_f8_matmul_workspace(m, n, k, code)
+        ws = _scratch(nbytes, x.device)
+        _check(lib.mezo_f8_matmul(x.codes.data_ptr(), x.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(),
+                                  m, n, k, out.data_ptr(), code, ldc, _ptr(ws), nbytes, _stream_ptr(None)),
+               "mezo_f8_matmul")
+    return out
+
+
+def f8_linear(x, w: F8Matrix, dtype=None, out=None, stream=None):
+    """A layer's product: the activations x (fp32/bf16 [m, k]) quantized, times
+    the weights w ([n, k]) in 8-bit storage: [m, n] of dtype (x's by default)."""
+    if dtype is None and out is None:
+        dtype = x.dtype
+    with _on(x.device, stream):
+        return f8_matmul(f8_quantize(x), w, dtype, out)
+
+
+def token_loss(logits, targets, stream=None):
+    """The cross entropy of each token and the mean over those that count:
+    logits fp32/bf16 [tokens, vocabulary] with contiguous rows, targets int64
+    [tokens], negative where a token does not count. Returns (losses, mean),
+    fp32 device tensors of [tokens] and of no dimension."""
+    import torch
+    rows, vocab, ld = _rows_of(logits, "logits")
+    dtype = _dtype_code(logits)
+    if targets.dtype != torch.int64:
+        raise TypeError(f"targets must be int64, got {targets.dtype}")
+    if targets.shape != (rows,) or not targets.is_contiguous():
+        raise ValueError(f"targets: a contiguous tensor of {rows}")
+    _same_device(logits, targets)
+    with _on(logits.device, stream):
+        losses = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        mean = torch.empty((), dtype=torch.float32, device=logits.device)
+        nbytes = lib.mezo_token_loss_workspace(rows, vocab)
+        ws = _scratch(nbytes, logits.device)
+        _check(lib.mezo_token_loss(logits.data_ptr(), dtype, rows, vocab, ld, targets.data_ptr(), losses.data_ptr(),
+                                   mean.data_ptr(), _ptr(ws), nbytes, _stream_ptr(None)), "mezo_token_loss")
+    return losses, mean
 
 
 def _tensor_struct(t, tid: int, first: int = 0) -> Tensor:
