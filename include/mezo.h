@@ -413,6 +413,56 @@ MEZO_API int mezo_f8_matmul(const void* x_codes, const uint8_t* x_scales, const 
                             const uint8_t* w_scales, uint64_t m, uint64_t n, uint64_t k, void* c, uint32_t c_dtype,
                             uint64_t ldc, void* workspace, uint64_t workspace_bytes, void* stream);
 
+/* Attention of a batch of documents. q [q_tokens, heads, dim], k and v
+ * [k_tokens, kv_heads, dim] and out, like q, are arrays of storage dtype
+ * (MEZO_F32 or MEZO_BF16) given by the elements from one token and from one
+ * head to the next; the dim elements of a head are contiguous. `docs` is a
+ * device array of n_docs rows of 5 int64,
+ *     q_first, nq, k_first, nk, prefix:
+ * the document's queries are the tokens q_first .. q_first + nq - 1 of q, its
+ * keys those from k_first of k and v (a cache may leave room between
+ * documents), and its queries are the last nq of its nk tokens: query i stands
+ * at position pos = i + nk - nq. For each query and head, over the document's
+ * keys j the query sees (all, or with `causal` those with j <= pos or
+ * j < prefix):
+ *     s_j = scale q . k_j, then cap tanh(s_j / cap) if softcap = cap > 0,
+ *           then s_j - slopes[head] |pos - j| if slopes is not NULL,
+ *     out = sum_j p_j v_j, p = softmax(s),   lse = ln sum_j exp(s_j).
+ * A query that sees no key has out = 0 and lse = -inf. A key that a query does
+ * not see takes no part in its result, whatever its values. Head h reads
+ * key/value head h / (heads / kv_heads). Tokens of no document keep their out
+ * and lse. lse (fp32 [q_tokens, heads]) may be NULL.
+ *
+ * max_q and max_k: no document has more queries or keys (queries past max_q
+ * are left out). The documents' queries must not overlap. Rows of docs that
+ * point outside the arrays are cut to them. Scores and sums are fp32; with
+ * MEZO_BF16 each probability is rounded to bf16 before it multiplies v.
+ *
+ * heads a multiple of kv_heads, heads <= MEZO_ATTENTION_MAX_HEADS, dim a
+ * multiple of 8 up to 128, pointers 16-byte aligned, strides multiples of 16
+ * bytes (MEZO_EINVAL); scale and softcap finite, softcap >= 0 (MEZO_ERANGE);
+ * out, lse and the workspace share no memory with each other or with anything
+ * read (MEZO_EOVERLAP). n_docs = 0, max_q = 0 and q_tokens = 0 enqueue nothing. */
+#define MEZO_ATTENTION_MAX_HEADS 65536u
+typedef struct {
+    const void* q;
+    const void* k;
+    const void* v;
+    void*       out;
+    float*      lse;
+    const int64_t* docs;
+    const float*   slopes; /* fp32 [heads], or NULL */
+    uint64_t q_tokens, k_tokens;
+    uint64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;
+    uint64_t max_q, max_k;
+    uint32_t n_docs, heads, kv_heads, dim;
+    uint32_t dtype, causal;
+    float    scale, softcap;
+} mezo_attention_t;
+
+MEZO_API uint64_t mezo_attention_workspace(const mezo_attention_t* a);
+MEZO_API int mezo_attention(const mezo_attention_t* a, void* workspace, uint64_t workspace_bytes, void* stream);
+
 /* The loss of a forward pass: for each of `rows` tokens with target y =
  * targets[t] >= 0, losses[t] = ln sum_v exp(x_tv) - x_ty over the token's
  * `vocab` logits (storage dtype, rows ld elements apart); tokens with a

@@ -82,7 +82,7 @@ KERNEL_UNITS = ["engine_dense.hip", "engine_nf4.hip", "nf4_convert.hip", "checks
 #: Those of the forward pass's operators. Their matrix tiles fill a wave's
 #: registers on purpose, so they are recorded apart from the engine's kernels,
 #: which keep to 128.
-FORWARD_UNITS = ["f8.hip", "token_loss.hip"]
+FORWARD_UNITS = ["attention.hip", "f8.hip", "token_loss.hip"]
 #: Host units.
 HOST_UNITS = ["api.cpp", "forward.cpp"]
 

@@ -1,0 +1,588 @@
+// attention.hip — attention of a packed batch of documents, the middle of a
+// decoder layer's forward pass. For query i of a document with nq queries and nk
+// keys (its queries are the last of its tokens, pos = i + nk - nq), per head:
+//   s_j = scale q_i . k_j,  s_j = cap tanh(s_j / cap) if capped,
+//   s_j = s_j - slope |pos - j| if biased,
+//   out = sum_j softmax_j(s) v_j over the visible keys j < limit,
+// limit = nk, or max(pos + 1, prefix) if causal: every mask this serves (documents,
+// causal, a prefix seen both ways, their mixtures) is "the first so many keys of the
+// own document", one number a row. A row that sees nothing gives 0 and lse -inf.
+//
+// One pass over the keys with a running reference m and l = sum 2^(s - m) (scores
+// in units of log 2). m need not be the maximum, any reference cancels: it moves
+// only when a row's maximum has passed it by kSlack, so that the accumulator is
+// seldom rescaled; a term is then at most 2^kSlack.
+//
+// Scores are computed transposed, keys x queries: a lane's 16 results of a 32x32
+// tile are then 16 keys of one query, the row's statistics are a lane's own (and
+// its partner's, 32 lanes away), and the probabilities are already where the second
+// product wants its operand, with the keys in an order that its other operand, the
+// values, follows: no exchange between lanes. The values' operand needs the columns
+// of the tile: ds_read_b64_tr_b16 transposes 4 keys x 16 columns at a time (bf16);
+// for fp32 the instruction takes one key a lane and a column read does.
+// All sums are fp32. bf16: probabilities are rounded to bf16 for the product with
+// the values (as large an error as the output's own rounding), l sums them
+// unrounded. fp32: v_mfma_f32_32x32x2_f32, exact products of fp32.
+//
+// The rows of a tile are (query, head) pairs of the heads that share a key/value
+// head, so these read it once. Two shapes of workgroup:
+//   rows: each wave has 32 rows of its own and all share stages of 64 keys;
+//   keys: at most 32 rows (single tokens): all waves have the same rows, each takes
+//         every kWaves-th stage of 32 keys through LDS of its own, without barriers,
+//         and they join at the end.
+// Where that gives too few workgroups for the GPU, a document's keys are split over
+// several, which leave (m, l, accumulator) and a second kernel joins them.
+//
+// A masked key takes no part whatever its value: its probability is 0, but 0 times
+// an infinite or NaN value is not. So a row whose result is not finite is computed
+// once more, from its visible keys alone (careful_row), slowly; finite inputs never
+// get there.
+#include "attention_launch.hpp"
+#include "lds_dma.hpp"
+#include "records.hpp"
+#include "stream_io.hpp"
+
+namespace mezo {
+
+typedef float v16f_t __attribute__((ext_vector_type(16)));
+typedef float v4f_t __attribute__((ext_vector_type(4)));
+typedef __bf16 v8bf_t __attribute__((ext_vector_type(8)));
+typedef __bf16 v4bf_t __attribute__((ext_vector_type(4)));
+typedef short v4s_t __attribute__((ext_vector_type(4)));
+typedef float v2f_t __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLn2 = 0.693147180559945309f;
+constexpr float kLowest = -3.0e38f;  // a reference below every score that counts
+constexpr float kSlack = 8.0f;
+
+// What a padded column of a narrower head is loaded from.
+__device__ const u32x4_t kZeros[1] = {};
+
+struct Document {
+    uint64_t q_first, k_first;
+    int64_t nq, nk, prefix;
+};
+
+// A document's row of the table, cut to the arrays it points into: no table makes
+// a kernel leave them.
+__device__ __forceinline__ Document read_document(const AttentionArgs& a, uint32_t d)
+{
+    const MEZO_GLOBAL int64_t* t = reinterpret_cast<const MEZO_GLOBAL int64_t*>(a.table) + uint64_t(d) * 5;
+    auto within = [](int64_t x, uint64_t top) { return x < 0 ? 0 : (uint64_t(x) > top ? int64_t(top) : x); };
+    Document r;
+    r.q_first = uint64_t(within(t[0], a.q_tokens));
+    r.nq = within(t[1], a.q_tokens - r.q_first);
+    r.k_first = uint64_t(within(t[2], a.k_tokens));
+    r.nk = within(t[3], a.k_tokens - r.k_first);
+    r.prefix = within(t[4], uint64_t(r.nk));
+    return r;
+}
+
+// How many of its document's keys query i sees.
+__device__ __forceinline__ int64_t visible(const AttentionArgs& a, const Document& d, int64_t i)
+{
+    const int64_t pos = i + d.nk - d.nq;
+    if (!a.causal) return d.nk;
+    return pos + 1 > d.prefix ? pos + 1 : d.prefix;  // pos < nk
+}
+
+// The score function's constants, for scores in units of log 2.
+struct Score {
+    float c;      // scale log2 e
+    float k, w;   // capped: x = w - 2 w / (1 + 2^(k s)), k = 2 scale log2 e / cap, w = cap log2 e
+    float cap, scale;
+    bool capped;
+};
+
+__device__ __forceinline__ Score score_of(const AttentionArgs& a)
+{
+    Score s;
+    s.scale = a.scale;
+    s.cap = a.softcap;
+    s.capped = a.softcap > 0.0f;
+    s.c = a.scale * kLog2e;
+    s.k = s.capped ? 2.0f * a.scale * kLog2e / a.softcap : 0.0f;
+    s.w = a.softcap * kLog2e;
+    return s;
+}
+
+// A capped score, before the bias. fp32 takes the library's tanh: the short form's
+// error, 2^-23 cap in the exponent, is for results of bf16.
+template <bool kF>
+__device__ __forceinline__ float capped(const Score& s, float x)
+{
+    if constexpr (kF) return s.w * tanhf(x * s.scale / s.cap);
+    return __builtin_fmaf(__builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * s.k)), -2.0f * s.w, s.w);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The larger of this lane's and its partner's value, 32 lanes away, and their sum.
+__device__ __forceinline__ float max_halves(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ float sum_halves(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+template <bool kF>
+__device__ __forceinline__ float load_element(uint64_t addr, uint32_t i)
+{
+    if constexpr (kF) return reinterpret_cast<const gfloat_t*>(addr)[i];
+    return __uint_as_float(uint32_t(reinterpret_cast<const gu16_t*>(addr)[i]) << 16);
+}
+
+template <bool kF>
+__device__ __forceinline__ void store_element(uint64_t addr, uint32_t i, float x)
+{
+    if constexpr (kF)
+        reinterpret_cast<gfloat_t*>(addr)[i] = x;
+    else
+        reinterpret_cast<MEZO_GLOBAL __bf16*>(addr)[i] = static_cast<__bf16>(x);
+}
+
+// Where row (i, h) of a document keeps what a split of its keys found: (m, l), and
+// the accumulator, dim floats.
+struct PartialRow {
+    uint64_t stats, acc;
+};
+__device__ __forceinline__ PartialRow partial_row(const AttentionArgs& a, uint32_t split, uint32_t doc, int64_t i,
+                                                  uint32_t h)
+{
+    const uint64_t rows = uint64_t(a.docs) * a.max_q * a.heads;
+    const uint64_t row = (uint64_t(doc) * a.max_q + uint64_t(i)) * a.heads + h;
+    const uint64_t at = split * rows + row;
+    return {a.partial + at * 8, a.partial + (a.splits * rows + 1) / 2 * 16 + at * a.dim * 4};
+}
+
+__device__ __forceinline__ void store_lse(const AttentionArgs& a, uint64_t token, uint32_t h, float m, float l)
+{
+    if (a.lse)
+        reinterpret_cast<gfloat_t*>(a.lse)[token * a.heads + h] =
+            l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// A row by its visible keys alone, k0 <= j < k1, one key after another; the whole
+// wave works on it. Lane l holds columns l and l + 64 of the accumulator.
+template <bool kF>
+__device__ __forceinline__ void careful_row(const AttentionArgs& a, const Document& d, uint32_t doc, uint32_t kvh,
+                                         uint32_t split, int64_t i, uint32_t h, int64_t k0, int64_t k1)
+{
+    const Score sc = score_of(a);
+    const uint32_t l = threadIdx.x & 63u;
+    const uint64_t q = a.q + (d.q_first + uint64_t(i)) * a.q_token + h * a.q_head;
+    const float slope = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
+    float q2[2], acc[2] = {0.0f, 0.0f}, m = kLowest, sum = 0.0f;
+    for (uint32_t c = 0; c < 2; ++c) q2[c] = l + 64 * c < a.dim ? load_element<kF>(q, l + 64 * c) : 0.0f;
+    for (int64_t j = k0; j < k1; ++j) {
+        const uint64_t key = d.k_first + uint64_t(j);
+        const uint64_t k = a.k + key * a.k_token + kvh * a.k_head, v = a.v + key * a.v_token + kvh * a.v_head;
+        float s = 0.0f;
+        for (uint32_t c = 0; c < 2; ++c)
+            if (l + 64 * c < a.dim) s += q2[c] * load_element<kF>(k, l + 64 * c);
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
+        s = sc.capped ? capped<kF>(sc, s) : s * sc.c;
+        if (a.slopes) s -= slope * fabsf(float(i + d.nk - d.nq - j));
+        const float top = fmaxf(m, s), old = exp2_fast(m - top), p = exp2_fast(s - top);
+        m = top;
+        sum = sum * old + p;
+        for (uint32_t c = 0; c < 2; ++c)
+            if (l + 64 * c < a.dim) acc[c] = acc[c] * old + p * load_element<kF>(v, l + 64 * c);
+    }
+    const uint64_t token = d.q_first + uint64_t(i);
+    if (a.splits > 1) {
+        const PartialRow p = partial_row(a, split, doc, i, h);
+        if (l == 0) *reinterpret_cast<MEZO_GLOBAL v2f_t*>(p.stats) = v2f_t{m, sum};
+        for (uint32_t c = 0; c < 2; ++c)
+            if (l + 64 * c < a.dim) reinterpret_cast<gfloat_t*>(p.acc)[l + 64 * c] = acc[c];
+        return;
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    for (uint32_t c = 0; c < 2; ++c)
+        if (l + 64 * c < a.dim) store_element<kF>(a.out + token * a.o_token + h * a.o_head, l + 64 * c, acc[c] * inv);
+    if (l == 0) store_lse(a, token, h, m, sum);
+}
+
+// The tile of one type and padded head size: how it lies in LDS and what the
+// matrix instructions take from it.
+template <bool kF, uint32_t kD>
+struct Tile {
+    static constexpr uint32_t kElement = kF ? 4 : 2;
+    static constexpr uint32_t kRow = kD * kElement;     // bytes of a key's row
+    static constexpr uint32_t kChunks = kRow / 16;
+    static constexpr uint32_t kLoadRows = 1024 / kRow;  // rows of one load of a wave
+    static constexpr uint32_t kQ = kD * kElement / 2 / 16;  // 16-byte operands of a lane's half row
+
+    // The order of a row's chunks in LDS, such that the lanes that read together
+    // read different banks: K 8 rows at one chunk, V (bf16) 4 rows at a pair of chunks.
+    static __device__ __forceinline__ uint32_t k_swizzle(uint32_t row) { return row & 7u; }
+    static __device__ __forceinline__ uint32_t v_swizzle(uint32_t row)
+    {
+        if constexpr (kF) return 0;
+        return (row & (kChunks >= 16 ? 7u : 3u)) << 1;
+    }
+
+    // scores += 32 keys (from row of K's stage) x 32 queries
+    static __device__ __forceinline__ v16f_t scores(const uint8_t* k, uint32_t row, const u32x4_t (&q)[kQ], uint32_t l)
+    {
+        v16f_t s = {};
+        const uint32_t r = row + (l & 31u);
+#pragma unroll
+        for (uint32_t c = 0; c < kQ; ++c) {
+            const u32x4_t w =
+                *reinterpret_cast<const u32x4_t*>(k + r * kRow + (((2 * c + (l >> 5)) ^ k_swizzle(r)) * 16));
+            if constexpr (kF) {
+                const v4f_t kv = __builtin_bit_cast(v4f_t, w), qv = __builtin_bit_cast(v4f_t, q[c]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[e], qv[e], s, 0, 0, 0);
+            } else {
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf_t, w),
+                                                            __builtin_bit_cast(v8bf_t, q[c]), s, 0, 0, 0);
+            }
+        }
+        return s;
+    }
+
+    // acc += values x probabilities of 32 keys (from row of V's stage)
+    static __device__ __forceinline__ void values(const uint8_t* v, uint32_t row, const v16f_t& p, v16f_t (&acc)[kD / 32],
+                                                  uint32_t l)
+    {
+        if constexpr (kF) {
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) {
+                const uint32_t r = row + 8 * (i >> 2) + 4 * (l >> 5) + (i & 3);
+#pragma unroll
+                for (uint32_t t = 0; t < kD / 32; ++t) {
+                    const float x = *reinterpret_cast<const float*>(v + r * kRow + (t * 32 + (l & 31u)) * 4);
+                    acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[i], acc[t], 0, 0, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (uint32_t u = 0; u < 2; ++u) {  // 16 keys an instruction
+                v8bf_t pb;
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) pb[j] = static_cast<__bf16>(p[8 * u + j]);
+#pragma unroll
+                for (uint32_t t = 0; t < kD / 32; ++t) {
+                    // columns t * 32 + l % 32; keys 4 h .. + 3 and 8 + 4 h .. + 3 of the 16, h = l / 32
+                    const uint32_t r = row + 16 * u + 4 * (l >> 5) + ((l & 15u) >> 2);
+                    const uint32_t chunk = t * 4 + ((l >> 4) & 1u) * 2 + ((l & 3u) >> 1);
+                    const uint32_t at = r * kRow + ((chunk ^ v_swizzle(r)) * 16) + (l & 1u) * 8;
+                    const uint32_t at8 = (r + 8) * kRow + ((chunk ^ v_swizzle(r + 8)) * 16) + (l & 1u) * 8;
+                    typedef __attribute__((address_space(3))) v4s_t lv4s_t;
+                    const v4s_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lv4s_t*)(v + at));
+                    const v4s_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lv4s_t*)(v + at8));
+                    const v8bf_t w = __builtin_bit_cast(
+                        v8bf_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, pb, acc[t], 0, 0, 0);
+                }
+            }
+        }
+    }
+};
+
+// kKeys: the workgroup's waves share out the keys; else the rows.
+template <bool kF, uint32_t kD, uint32_t kWaves, bool kKeys>
+__global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(AttentionArgs a)
+{
+    using T = Tile<kF, kD>;
+    constexpr uint32_t kStage = kKeys ? 32 : 64;  // keys of a stage
+    constexpr uint32_t kBytes = kStage * T::kRow;
+    constexpr uint32_t kSets = kKeys ? kWaves : 1;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kSets][2][2][kBytes];
+
+    const uint32_t l = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t kvh = blockIdx.x % a.kv_heads, doc = blockIdx.x / a.kv_heads;
+    const Document d = read_document(a, doc);
+    const uint64_t rows = uint64_t(d.nq < int64_t(a.max_q) ? d.nq : int64_t(a.max_q)) * a.group;
+    // the last tiles see the most keys: first
+    constexpr uint32_t kTileRows = kKeys ? 32 : 32 * kWaves;
+    const uint64_t tile0 = uint64_t(gridDim.y - 1 - blockIdx.y) * kTileRows;
+    if (tile0 >= rows) return;
+    const uint64_t tile1 = tile0 + kTileRows < rows ? tile0 + kTileRows : rows;
+
+    // this lane's row: a (query, head) pair; past the end the last one's again
+    const uint64_t first = tile0 + (kKeys ? 0 : wave * 32), row = first + (l & 31u);
+    auto query = [&](uint64_t r) { return int64_t((r < tile1 ? r : tile1 - 1) / a.group); };
+    const int64_t i = query(row);
+    const uint32_t h = kvh * a.group + uint32_t((row < tile1 ? row : tile1 - 1) % a.group);
+    const bool mine = row < tile1;
+    const int64_t limit = visible(a, d, i) > 0 ? visible(a, d, i) : 0;
+    // the wave's rows see all keys below low and none from high
+    const int64_t low0 = visible(a, d, query(first)), low = low0 > 0 ? low0 : 0;
+    const int64_t high0 = visible(a, d, query(first + 31)), high = high0 > 0 ? high0 : 0;
+    const int64_t last0 = visible(a, d, int64_t((tile1 - 1) / a.group)), last = last0 > 0 ? last0 : 0;
+
+    // the stages of this split of the workgroup's keys
+    const uint64_t stages = (uint64_t(last) + kStage - 1) / kStage;
+    const uint64_t s0 = stages * blockIdx.z / a.splits, s1 = stages * (blockIdx.z + 1) / a.splits;
+
+    u32x4_t q[T::kQ];
+    {
+        const uint64_t at = a.q + (d.q_first + uint64_t(i)) * a.q_token + h * a.q_head + (l >> 5) * 16;
+#pragma unroll
+        for (uint32_t c = 0; c < T::kQ; ++c) {
+            q[c] = u32x4_t{0, 0, 0, 0};
+            if (c * 32 + (l >> 5) * 16 < a.dim * T::kElement) q[c] = *reinterpret_cast<const gu32x4_t*>(at + c * 32);
+        }
+    }
+    const uint64_t kbase = a.k + d.k_first * a.k_token + kvh * a.k_head;
+    const uint64_t vbase = a.v + d.k_first * a.v_token + kvh * a.v_head;
+    const uint32_t lds0 = lds_offset(&lds[kKeys ? wave : 0][0][0][0]);
+    // stage s into buffer b; keys past the document's end: the last one again
+    auto load = [&](uint64_t s, uint32_t b) {
+        constexpr uint32_t kLoads = kBytes / 1024 / (kKeys ? 1 : kWaves);  // of K, and of V
+        const int64_t left = d.nk - int64_t(s * kStage) - 1;
+#pragma unroll
+        for (uint32_t n = 0; n < 2 * kLoads; ++n) {
+            const bool isv = n >= kLoads;
+            const uint32_t at = (kKeys ? 0 : wave * kLoads) + n % kLoads;
+            const uint32_t r = at * T::kLoadRows + l / T::kChunks;
+            const uint32_t chunk = (l % T::kChunks) ^ (isv ? T::v_swizzle(r) : T::k_swizzle(r));
+            const uint64_t key = s * kStage + (int64_t(r) < left ? r : uint32_t(left));
+            uint64_t addr = isv ? vbase + key * a.v_token : kbase + key * a.k_token;
+            addr += chunk * 16;
+            if (chunk * 16 >= a.dim * T::kElement) addr = reinterpret_cast<uint64_t>(&kZeros[0]);
+            dma_to_lds(addr, lds0 + (2 * b + (isv ? 1 : 0)) * kBytes + at * 1024);
+        }
+    };
+
+    const Score sc = score_of(a);
+    const float slope = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
+    const int64_t pos = i + d.nk - d.nq;
+    v16f_t acc[kD / 32] = {};
+    float m = kLowest, sum = 0.0f;
+
+    const uint64_t step = kKeys ? kWaves : 1, begin = s0 + (kKeys ? wave : 0);
+    if (begin < s1) load(begin, 0);
+    uint32_t b = 0;
+    for (uint64_t s = begin; s < s1; s += step, b ^= 1) {
+        dma_wait();
+        if constexpr (kKeys)
+            lds_wait();  // the other buffer is read
+        else
+            lds_barrier();  // everyone's part of this stage is there, and the other buffer is read
+        if (s + step < s1) load(s + step, b ^ 1);
+        const int64_t k0 = int64_t(s * kStage);
+        if (k0 >= high) continue;  // (of the wave)
+        const uint8_t* kt = lds[kKeys ? wave : 0][b][0];
+        const uint8_t* vt = lds[kKeys ? wave : 0][b][1];
+        v16f_t x[kStage / 32];
+        float top = kLowest;
+#pragma unroll
+        for (uint32_t t = 0; t < kStage / 32; ++t) {
+            x[t] = T::scores(kt, t * 32, q, l);
+if (sc.capped) {
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped<kF>(sc, x[t][e]);
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e) x[t][e] *= sc.c;
+            }
+            // this lane's keys: k0 + t * 32 + 4 (l / 32), and 8 (e / 4) + e % 4 more
+            const int64_t key = k0 + t * 32 + 4 * (l >> 5);
+            if (a.slopes) {
+                const float from = float(pos - key);
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e)
+                    x[t][e] = __builtin_fmaf(-slope, fabsf(from - float(8 * (e >> 2) + (e & 3))), x[t][e]);
+            }
+            if (k0 + kStage > low) {
+                const int64_t left = limit - key;
+                const int see = left < 0 ? 0 : (left < 32 ? int(left) : 32);
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e)
+                    if (int(8 * (e >> 2) + (e & 3)) >= see) x[t][e] = -__builtin_inff();
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < 16; ++e) top = fmaxf(top, x[t][e]);
+        }
+        top = max_halves(top);
+        if (__any(top > m + kSlack)) {
+            const float now = fmaxf(m, top), old = exp2_fast(m - now);
+            m = now;
+            sum *= old;
+#pragma unroll
+            for (uint32_t t = 0; t < kD / 32; ++t)
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e) acc[t][e] *= old;
+        }
+#pragma unroll
+        for (uint32_t t = 0; t < kStage / 32; ++t) {
+#pragma unroll
+            for (uint32_t e = 0; e < 16; ++e) {
+                x[t][e] = exp2_fast(x[t][e] - m);
+                sum += x[t][e];
+            }
+            T::values(vt, t * 32, x[t], acc, l);
+        }
+    }
+    sum = sum_halves(sum);
+
+    if constexpr (kKeys) {  // the waves' parts, joined in their order by the first
+        __shared__ float stats[kWaves][2][32];
+        float* room = reinterpret_cast<float*>(&lds[0][0][0][0]);  // [kWaves - 1][kD / 32][16][64]
+        if (l < 32) {
+            stats[wave][0][l] = m;
+            stats[wave][1][l] = sum;
+        }
+        __syncthreads();
+        float now = stats[0][0][l & 31u];
+#pragma unroll
+        for (uint32_t w = 1; w < kWaves; ++w) now = fmaxf(now, stats[w][0][l & 31u]);
+        const float old = exp2_fast(m - now);
+        if (wave > 0) {
+#pragma unroll
+            for (uint32_t t = 0; t < kD / 32; ++t)
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e)
+                    room[(((wave - 1) * (kD / 32) + t) * 16 + e) * 64 + l] = acc[t][e] * old;
+        }
+        __syncthreads();
+        if (wave > 0) return;
+        sum = 0.0f;
+#pragma unroll
+        for (uint32_t w = 0; w < kWaves; ++w) sum += stats[w][1][l & 31u] * exp2_fast(stats[w][0][l & 31u] - now);
+#pragma unroll
+        for (uint32_t t = 0; t < kD / 32; ++t)
+#pragma unroll
+            for (uint32_t e = 0; e < 16; ++e) {
+                float x = acc[t][e] * old;
+#pragma unroll
+                for (uint32_t w = 1; w < kWaves; ++w) x += room[(((w - 1) * (kD / 32) + t) * 16 + e) * 64 + l];
+                acc[t][e] = x;
+            }
+        m = now;
+    }
+
+    const bool split = a.splits > 1;
+    const float inv = split ? 1.0f : (sum == 0.0f ? 0.0f : 1.0f / sum);
+    bool finite = true;
+#pragma unroll
+    for (uint32_t t = 0; t < kD / 32; ++t)
+#pragma unroll
+        for (uint32_t e = 0; e < 16; ++e) {
+            acc[t][e] *= inv;
+            finite = finite && fabsf(acc[t][e]) < __builtin_inff();
+        }
+    const uint64_t token = d.q_first + uint64_t(i);
+    if (mine) {
+        const PartialRow p = partial_row(a, blockIdx.z, doc, i, h);
+        if (l < 32) {
+            if (split)
+                *reinterpret_cast<MEZO_GLOBAL v2f_t*>(p.stats) = v2f_t{m, sum};
+            else
+                store_lse(a, token, h, m, sum);
+        }
+        const uint64_t o = a.out + token * a.o_token + h * a.o_head;
+#pragma unroll
+        for (uint32_t t = 0; t < kD / 32; ++t)
+#pragma unroll
+            for (uint32_t e = 0; e < 16; e += 4) {
+                const uint32_t c = t * 32 + 8 * (e >> 2) + 4 * (l >> 5);
+                if (c >= a.dim) continue;
+                const v4f_t w = {acc[t][e], acc[t][e + 1], acc[t][e + 2], acc[t][e + 3]};
+                if (split)
+                    *reinterpret_cast<MEZO_GLOBAL v4f_t*>(p.acc + c * 4) = w;
+                else if constexpr (kF)
+                    *reinterpret_cast<MEZO_GLOBAL v4f_t*>(o + c * 4) = w;
+                else
+                    *reinterpret_cast<MEZO_GLOBAL v4bf_t*>(o + c * 2) = __builtin_convertvector(w, v4bf_t);
+            }
+    }
+    // rows that are not finite, once more
+    uint64_t again = __ballot(mine && !finite);
+    again = (again | (again >> 32)) & 0xFFFFFFFFull;
+    while (again) {
+        const uint32_t lane = uint32_t(__builtin_ctzll(again));
+        again &= again - 1;
+        const int64_t ri = query(first + lane);
+        const uint32_t rh = kvh * a.group + uint32_t((first + lane) % a.group);
+        const int64_t rlimit = visible(a, d, ri), end = int64_t(s1 * kStage);
+        careful_row<kF>(a, d, doc, kvh, blockIdx.z, ri, rh, int64_t(s0 * kStage), end < rlimit ? end : rlimit);
+    }
+}
+
+// The splits of a row, joined in their order: a wave a row.
+template <bool kF>
+__global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a)
+{
+    const uint32_t l = threadIdx.x & 63u;
+    const uint64_t row = uint64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (row >= uint64_t(a.docs) * a.max_q * a.heads) return;
+    const uint32_t h = uint32_t(row % a.heads);
+    const int64_t i = int64_t(row / a.heads % a.max_q);
+    const uint32_t doc = uint32_t(row / a.heads / a.max_q);
+    const Document d = read_document(a, doc);
+    if (i >= d.nq) return;
+    float m = kLowest;
+    for (uint32_t s = 0; s < a.splits; ++s)
+        m = fmaxf(m, reinterpret_cast<const gfloat_t*>(partial_row(a, s, doc, i, h).stats)[0]);
+    float sum = 0.0f, acc[2] = {0.0f, 0.0f};
+    for (uint32_t s = 0; s < a.splits; ++s) {
+        const PartialRow p = partial_row(a, s, doc, i, h);
+        const float pl = reinterpret_cast<const gfloat_t*>(p.stats)[1];
+        if (pl == 0.0f) continue;  // no key of this row in this split
+        const float w = exp2_fast(reinterpret_cast<const gfloat_t*>(p.stats)[0] - m);
+        sum += pl * w;
+        for (uint32_t c = 0; c < 2; ++c)
+            if (l + 64 * c < a.dim) acc[c] += reinterpret_cast<const gfloat_t*>(p.acc)[l + 64 * c] * w;
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const uint64_t token = d.q_first + uint64_t(i);
+    for (uint32_t c = 0; c < 2; ++c)
+        if (l + 64 * c < a.dim) store_element<kF>(a.out + token * a.o_token + h * a.o_head, l + 64 * c, acc[c] * inv);
+    if (l == 0) store_lse(a, token, h, m, sum);
+}
+
+// Few rows: the waves of a workgroup share out the keys.
+bool by_keys(uint64_t rows) { return rows <= 32; }
+
+AttentionPlan plan_attention(uint32_t docs, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t max_q,
+                             uint32_t max_k, uint32_t)
+{
+    const uint64_t rows = uint64_t(max_q) * (heads / kv_heads);
+    const uint64_t tiles = by_keys(rows) ? 1 : (rows + 127) / 128;
+    const uint64_t groups = uint64_t(docs) * kv_heads * tiles;
+    const uint64_t want = (1024 + groups - 1) / groups, most = max_k / 256;
+    uint64_t splits = want < most ? want : most;
+    splits = splits < 1 || groups >= 512 ? 1 : (splits > 64 ? 64 : splits);
+    AttentionPlan p;
+    p.splits = uint32_t(splits);
+    const uint64_t kept = splits * docs * max_q * heads;
+    p.workspace = splits > 1 ? (kept + 1) / 2 * 16 + kept * dim * 4 : 0;
+    return p;
+}
+
+template <bool kF, uint32_t kD>
+hipError_t launch(AttentionArgs a, hipStream_t stream)
+{
+    constexpr uint32_t kKeyWaves = kF && kD > 64 ? 2 : 4;
+    void* params[] = {&a};
+    const uint64_t rows = uint64_t(a.max_q) * a.group;
+    const bool keys = by_keys(rows);
+    const dim3 grid(a.docs * a.kv_heads, uint32_t(keys ? 1 : (rows + 127) / 128), a.splits);
+    const void* f = keys ? reinterpret_cast<const void*>(attention_kernel<kF, kD, kKeyWaves, true>)
+                         : reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false>);
+    const hipError_t e = hipLaunchKernel(f, grid, dim3(keys ? kKeyWaves * 64 : 256), params, 0, stream);
+    if (e != hipSuccess || a.splits == 1) return e;
+    const uint64_t all = uint64_t(a.docs) * a.max_q * a.heads;
+    return hipLaunchKernel(reinterpret_cast<const void*>(attention_join_kernel<kF>), dim3(uint32_t((all + 3) / 4)),
+                           dim3(256), params, 0, stream);
+}
+
+hipError_t launch_attention(const AttentionArgs& args, hipStream_t stream)
+{
+    if (args.dtype == kF32) return args.dim <= 64 ? launch<true, 64>(args, stream) : launch<true, 128>(args, stream);
+    return args.dim <= 64 ? launch<false, 64>(args, stream) : launch<false, 128>(args, stream);
+}
+
+}  // namespace mezo

@@ -7,6 +7,7 @@
 #include <cstdint>
 
 #include "../../include/mezo.h"
+#include "attention_launch.hpp"
 #include "f8_launch.hpp"
 #include "host.hpp"
 #include "token_loss_launch.hpp"
@@ -121,6 +122,112 @@ int f8_matmul(const void* x_codes, const uint8_t* x_scales, const void* w_codes,
     return MEZO_OK;
 }
 
+// ---- attention -------------------------------------------------------------------
+
+// The sizes of an attention call that do not depend on its pointers.
+bool attention_sizes(const mezo_attention_t& a)
+{
+    return a.heads >= 1 && a.kv_heads >= 1 && a.heads <= MEZO_ATTENTION_MAX_HEADS && a.heads % a.kv_heads == 0 &&
+           a.dim >= 8 && a.dim <= mezo::kMaxHeadDim && a.dim % 8 == 0 && a.q_tokens <= MEZO_MAX_NUMEL &&
+           a.k_tokens <= MEZO_MAX_NUMEL;
+}
+
+// Rows of work: what of max_q and max_k can be.
+uint64_t most_q(const mezo_attention_t& a) { return a.max_q < a.q_tokens ? a.max_q : a.q_tokens; }
+uint64_t most_k(const mezo_attention_t& a) { return a.max_k < a.k_tokens ? a.max_k : a.k_tokens; }
+
+bool attention_empty(const mezo_attention_t& a) { return a.n_docs == 0 || most_q(a) == 0; }
+
+// Whether the launch's grid holds the call.
+bool attention_fits(const mezo_attention_t& a)
+{
+    const uint64_t q = most_q(a), k = most_k(a);
+    return uint64_t(a.n_docs) * a.kv_heads < (1u << 24) && q * (a.heads / a.kv_heads) <= 65535ull * 128 &&
+           k < (1ull << 32) && uint64_t(a.n_docs) * q * a.heads < (1ull << 40);
+}
+
+mezo::AttentionPlan attention_plan(const mezo_attention_t& a)
+{
+    return mezo::plan_attention(a.n_docs, a.heads, a.kv_heads, a.dim, static_cast<uint32_t>(most_q(a)),
+                                static_cast<uint32_t>(most_k(a)), a.dtype);
+}
+
+int attention(const mezo_attention_t* p, void* workspace, uint64_t workspace_bytes, void* stream)
+{
+    if (!p) return MEZO_EINVAL;
+    const mezo_attention_t& a = *p;
+    if (!dense(a.dtype)) return MEZO_EDTYPE;
+    if (!attention_sizes(a)) return MEZO_EINVAL;
+    if (!std::isfinite(a.scale) || !std::isfinite(a.softcap) || a.softcap < 0.0f) return MEZO_ERANGE;
+    if (attention_empty(a)) return MEZO_OK;
+    if (!a.q || !a.out || !a.docs || (a.k_tokens && (!a.k || !a.v)) || !attention_fits(a)) return MEZO_EINVAL;
+    const uint64_t e = element_bytes(a.dtype), align = 16 / e;
+    if (!aligned(a.q, 16) || !aligned(a.k, 16) || !aligned(a.v, 16) || !aligned(a.out, 16) || !aligned(a.docs, 8) ||
+        !aligned(a.lse, 4) || !aligned(a.slopes, 4))
+        return MEZO_EINVAL;
+    const uint64_t strides[8] = {a.q_token, a.q_head, a.k_token, a.k_head, a.v_token, a.v_head, a.o_token, a.o_head};
+    for (uint64_t s : strides)
+        if (s % align) return MEZO_EINVAL;
+    // the bytes of each array; out's elements must not share memory with each other
+    Range r[4];
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t tokens = i == 1 || i == 2 ? a.k_tokens : a.q_tokens, heads = i == 1 || i == 2 ? a.kv_heads : a.heads;
+        const void* const at[4] = {a.q, a.k, a.v, a.out};
+        uint64_t n = 0, m = 0;
+        if (tokens && (__builtin_mul_overflow(tokens - 1, strides[2 * i], &n) ||
+                       __builtin_mul_overflow(heads - 1, strides[2 * i + 1], &m) || __builtin_add_overflow(n, m, &n) ||
+                       __builtin_add_overflow(n, a.dim, &n) || __builtin_mul_overflow(n, e, &n)))
+            return MEZO_EINVAL;
+        r[i] = {address(at[i]), n};
+    }
+    using wide = unsigned __int128;
+    const wide oh = a.o_head, ot = a.o_token, h1 = a.heads - 1, t1 = a.q_tokens - 1;
+    const bool by_token = (h1 == 0 || oh >= a.dim) && (t1 == 0 || ot >= h1 * oh + a.dim);  // [tokens, heads, dim]
+    const bool by_head = (t1 == 0 || ot >= a.dim) && (h1 == 0 || oh >= t1 * ot + a.dim);   // [heads, tokens, dim]
+    if (!by_token && !by_head) return MEZO_EOVERLAP;
+    const mezo::AttentionPlan plan = attention_plan(a);
+    if (plan.workspace && (!workspace || workspace_bytes < plan.workspace || !aligned(workspace, 16))) return MEZO_EINVAL;
+    const Range lse = {address(a.lse), a.lse ? a.q_tokens * a.heads * 4 : 0},
+                scratch = {address(workspace), plan.workspace};
+    const Range read[7] = {r[0], r[1], r[2], {address(a.docs), a.n_docs * 40ull},
+                           {address(a.slopes), a.slopes ? a.heads * 4ull : 0}, r[3], lse};
+    if (clashes(r[3], read, 5) || (a.lse && clashes(lse, read, 6)) || (plan.workspace && clashes(scratch, read, 7)))
+        return MEZO_EOVERLAP;
+    mezo::AttentionArgs g;
+    g.q = r[0].at;
+    g.k = r[1].at;
+    g.v = r[2].at;
+    g.out = r[3].at;
+    g.lse = lse.at;
+    g.table = address(a.docs);
+    g.partial = scratch.at;
+    g.slopes = a.slopes;
+    g.q_token = a.q_token * e;
+    g.q_head = a.q_head * e;
+    g.k_token = a.k_token * e;
+    g.k_head = a.k_head * e;
+    g.v_token = a.v_token * e;
+    g.v_head = a.v_head * e;
+    g.o_token = a.o_token * e;
+    g.o_head = a.o_head * e;
+    g.q_tokens = a.q_tokens;
+    g.k_tokens = a.k_tokens;
+    g.docs = a.n_docs;
+    g.heads = a.heads;
+    g.kv_heads = a.kv_heads;
+    g.group = a.heads / a.kv_heads;
+    g.dim = a.dim;
+    g.max_q = static_cast<uint32_t>(most_q(a));
+    g.max_k = static_cast<uint32_t>(most_k(a));
+    g.splits = plan.splits;
+    g.causal = a.causal ? 1u : 0u;
+    g.dtype = a.dtype;
+    g.scale = a.scale;
+    g.softcap = a.softcap;
+    MEZO_HIP(mezo::launch_attention(g, static_cast<hipStream_t>(stream)));
+    return MEZO_OK;
+}
+
 // ---- the token loss ------------------------------------------------------------
 
 uint64_t loss_workspace(uint64_t rows, uint64_t vocab)
@@ -186,6 +293,17 @@ int mezo_f8_matmul(const void* x_codes, const uint8_t* x_scales, const void* w_c
         return f8_matmul(x_codes, x_scales, w_codes, w_scales, m, n, k, c, c_dtype, ldc, workspace, workspace_bytes,
                          stream);
     });
+}
+
+uint64_t mezo_attention_workspace(const mezo_attention_t* a)
+{
+    if (!a || !dense(a->dtype) || !attention_sizes(*a) || attention_empty(*a) || !attention_fits(*a)) return 0;
+    return attention_plan(*a).workspace;
+}
+
+int mezo_attention(const mezo_attention_t* a, void* workspace, uint64_t workspace_bytes, void* stream)
+{
+    return guarded("mezo_attention", [&] { return attention(a, workspace, workspace_bytes, stream); });
 }
 
 uint64_t mezo_token_loss_workspace(uint64_t rows, uint64_t vocab) { return loss_workspace(rows, vocab); }

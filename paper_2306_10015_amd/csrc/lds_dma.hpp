@@ -1,0 +1,51 @@
+// lds_dma.hpp — loads from global memory straight into LDS, and the waits they
+// need.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace mezo {
+
+// The LDS byte offset of a __shared__ object.
+__device__ __forceinline__ uint32_t lds_offset(const void* p)
+{
+    return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)(p)));
+}
+
+// Start a load of 16 bytes a lane: lane l's go from its addr to LDS byte
+// lds + 16 l (lds is the wave's, uniform). The instruction is written out because
+// after the builtin the compiler waits for every such load before the next LDS
+// read of the kernel, also of another buffer, which undoes the overlap of loads
+// with the work on the stage before. It has no result register, so nothing but
+// the LDS bytes is in flight: dma_wait() before they are read. m0 is a reserved
+// register: the compiler sets it right before each use of its own and keeps
+// nothing in it.
+__device__ __forceinline__ void dma_to_lds(uint64_t addr, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %1\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %0, off"
+                 :
+                 : "v"(addr), "s"(lds)
+                 : "memory");
+}
+
+// Wait until at most kLeft of the wave's loads (the latest) are still in flight.
+template <int kLeft = 0>
+__device__ __forceinline__ void dma_wait()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLeft) : "memory");
+}
+
+// Wait for the wave's LDS accesses.
+__device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
+// A barrier of the workgroup that waits for the wave's LDS accesses but not for
+// its loads in flight.
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+}
+
+}  // namespace mezo

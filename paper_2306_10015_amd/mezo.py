@@ -56,6 +56,14 @@ class Codec(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_uint32), ("scale", ctypes.c_float), ("alpha", ctypes.c_float)]
 
 
+class Attention(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "k", "v", "out", "lse", "docs", "slopes")]
+                + [(n, ctypes.c_uint64) for n in ("q_tokens", "k_tokens", "q_token", "q_head", "k_token", "k_head",
+                                                  "v_token", "v_head", "o_token", "o_head", "max_q", "max_k")]
+                + [(n, ctypes.c_uint32) for n in ("n_docs", "heads", "kv_heads", "dim", "dtype", "causal")]
+                + [("scale", ctypes.c_float), ("softcap", ctypes.c_float)])
+
+
 class Step(ctypes.Structure):
     _fields_ = [("seeds", ctypes.c_void_p), ("q", ctypes.c_void_p), ("K", ctypes.c_uint32),
                 ("lr", ctypes.c_float)]
@@ -69,6 +77,7 @@ EXPORTS = ("mezo_paramset_create", "mezo_paramset_destroy", "mezo_paramset_numel
            "mezo_update_multi_from", "mezo_checksum", "quantize_projgrad",
            "mezo_dequantize", "mezo_nf4_quantize", "mezo_nf4_dequantize",
            "mezo_f8_quantize", "mezo_f8_matmul_workspace", "mezo_f8_matmul",
+           "mezo_attention_workspace", "mezo_attention",
            "mezo_token_loss_workspace", "mezo_token_loss", "mezo_debug_generate", "mezo_debug_box_muller",
            "mezo_strerror", "mezo_last_error", "mezo_version")
 
@@ -122,6 +131,10 @@ def _load() -> ctypes.CDLL:
     L.mezo_f8_matmul_workspace.restype = u64
     L.mezo_f8_matmul.argtypes = [vp, vp, vp, vp, u64, u64, u64, vp, u32, u64, vp, u64, vp]
     L.mezo_f8_matmul.restype = i32
+    L.mezo_attention_workspace.argtypes = [ctypes.POINTER(Attention)]
+    L.mezo_attention_workspace.restype = u64
+    L.mezo_attention.argtypes = [ctypes.POINTER(Attention), vp, u64, vp]
+    L.mezo_attention.restype = i32
     L.mezo_token_loss_workspace.argtypes = [u64, u64]
     L.mezo_token_loss_workspace.restype = u64
     L.mezo_token_loss.argtypes = [vp, u32, u64, u64, u64, vp, vp, vp, vp, u64, vp]
@@ -385,6 +398,107 @@ def f8_linear(x, w: F8Matrix, dtype=None, out=None, stream=None):
         dtype = x.dtype
     with _on(x.device, stream):
         return f8_matmul(f8_quantize(x), w, dtype, out)
+
+
+class Documents:
+    """The documents of an attention call: ``table``, a device tensor int64
+    [documents, 5] of (q_first, q_len, k_first, k_len, prefix) as in mezo.h, and
+    the most queries and keys a document has. Use ``Documents.of`` to make one
+    from lengths, checked."""
+
+    def __init__(self, table, max_q: int, max_k: int):
+        import torch
+        if table.dtype != torch.int64:
+            raise TypeError(f"table must be int64, got {table.dtype}")
+        if not table.is_cuda or table.dim() != 2 or table.shape[1] != 5 or not table.is_contiguous():
+            raise ValueError("table: a contiguous CUDA tensor [documents, 5]")
+        if max_q < 0 or max_k < 0:
+            raise ValueError("max_q and max_k must not be negative")
+        self.table, self.max_q, self.max_k = table, int(max_q), int(max_k)
+
+    @classmethod
+    def of(cls, q_lens, k_lens=None, prefix=None, q_first=None, k_first=None, device="cuda") -> "Documents":
+        """From sequences of lengths: q_lens queries and k_lens keys a document
+        (q_lens by default), the visible prefix (0), and where each begins
+        (packed one after another by default)."""
+        import torch
+
+        def ints(x, default):
+            out = [int(v) for v in (default if x is None else x)]
+            if len(out) != len(q_lens) or any(v < 0 for v in out):
+                raise ValueError("one value that is not negative for each document")
+            return out
+
+        def packed(lens):
+            at, out = 0, []
+            for n in lens:
+                out.append(at)
+                at += n
+            return out
+
+        q_lens = list(q_lens)
+        q_lens = ints(q_lens, q_lens)
+        k_lens = ints(k_lens, q_lens)
+        q_first, k_first = ints(q_first, packed(q_lens)), ints(k_first, packed(k_lens))
+        spans = sorted((a, a + n) for a, n in zip(q_first, q_lens) if n)
+        if any(b > c for (_, b), (c, _) in zip(spans, spans[1:])):
+            raise ValueError("the documents' queries overlap")
+        rows = list(zip(q_first, q_lens, k_first, k_lens, ints(prefix, [0] * len(q_lens))))
+        table = torch.tensor(rows, dtype=torch.int64, device=device).reshape(len(rows), 5)
+        return cls(table, max(q_lens, default=0), max(k_lens, default=0))
+
+
+def _heads_of(t, what: str):
+    """(tokens, heads, dim) of a 3-D CUDA tensor with contiguous heads, and the
+    elements from one token and from one head to the next."""
+    if t.dim() != 3 or not t.is_cuda:
+        raise ValueError(f"{what}: a CUDA tensor [tokens, heads, dim]")
+    tokens, heads, dim = t.shape
+    st, sh, sd = t.stride()
+    if dim > 1 and sd != 1:
+        raise ValueError(f"{what}: the elements of a head must be contiguous")
+    if st < 0 or sh < 0:
+        raise ValueError(f"{what}: negative strides")
+    return tokens, heads, dim, st if tokens > 1 else heads * dim, sh if heads > 1 else dim
+
+
+def attention(q, k, v, docs: Documents, causal: bool = True, scale: float | None = None, softcap: float = 0.0,
+              slopes=None, out=None, return_lse: bool = False, stream=None):
+    """Attention of a batch of documents (mezo_attention): q [tokens, heads,
+    dim], k and v [tokens, kv_heads, dim] of fp32 or bf16, each with any token
+    and head strides that are multiples of 16 bytes. scale is 1 / sqrt(dim) by
+    default; slopes, fp32 [heads], biases scores by -slope * distance. Returns
+    out, like q, and with return_lse the pair (out, lse), lse fp32 [tokens, heads].
+    Tokens of no document are not written."""
+    import torch
+    tq, heads, dim, q_token, q_head = _heads_of(q, "q")
+    tk, kv_heads, k_dim, k_token, k_head = _heads_of(k, "k")
+    tv, v_heads, v_dim, v_token, v_head = _heads_of(v, "v")
+    if (tk, kv_heads) != (tv, v_heads) or not dim == k_dim == v_dim:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not fit together")
+    if kv_heads == 0 or heads % kv_heads:
+        raise ValueError(f"{heads} heads over {kv_heads} key/value heads")
+    dtype = _dtype_code(q)
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise TypeError(f"q, k and v are {q.dtype}, {k.dtype} and {v.dtype}")
+    if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (heads,) or not slopes.is_contiguous()):
+        raise ValueError(f"slopes: a contiguous float32 tensor of {heads}")
+    with _on(q.device, stream):
+        if out is None:
+            out = torch.empty(tq, heads, dim, dtype=q.dtype, device=q.device)
+        elif out.dtype != q.dtype or out.shape != q.shape:
+            raise ValueError("out must be like q")
+        _same_device(q, k, v, out, slopes, docs.table)
+        lse = torch.empty(tq, heads, dtype=torch.float32, device=q.device) if return_lse else None
+        _, _, _, o_token, o_head = _heads_of(out, "out")
+        a = Attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), docs.table.data_ptr(),
+                      _ptr(slopes), tq, tk, q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head,
+                      docs.max_q, docs.max_k, docs.table.shape[0], heads, kv_heads, dim, dtype, int(causal),
+                      1.0 / math.sqrt(dim) if scale is None else float(scale), float(softcap))
+        nbytes = lib.mezo_attention_workspace(ctypes.byref(a))
+        ws = _scratch(nbytes, q.device)
+        _check(lib.mezo_attention(ctypes.byref(a), _ptr(ws), nbytes, _stream_ptr(None)), "mezo_attention")
+    return (out, lse) if return_lse else out
 
 
 def token_loss(logits, targets, stream=None):

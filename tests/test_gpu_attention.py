@@ -1,0 +1,357 @@
+"""Attention on the GPU, through the binding, against a plain reference in 64
+bits (attention_ref.py), at the sizes, masks and layouts where it can go wrong.
+The bars come from the arithmetic (attention_ref.bounds)."""
+import math
+
+import numpy as np
+import pytest
+
+import attention_ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mz():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a visible GPU"
+    from paper_2306_10015_amd import mezo
+    return mezo
+
+
+def tensors(tq, tk, heads, kv_heads, dim, dtype, seed=0):
+    import torch
+    g = torch.Generator()
+    g.manual_seed(seed + 7 * tq + tk)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    return tuple(torch.randn(t, n, dim, generator=g).mul(s).to(dt).cuda()
+                 for t, n, s in ((tq, heads, 1.5), (tk, kv_heads, 1.5), (tk, kv_heads, 1.0)))
+
+
+def table(q_lens, k_lens=None, prefix=None, q_first=None, k_first=None):
+    k_lens = list(q_lens) if k_lens is None else list(k_lens)
+    q_first = [int(x) for x in np.cumsum([0, *q_lens])[:-1]] if q_first is None else q_first
+    k_first = [int(x) for x in np.cumsum([0, *k_lens])[:-1]] if k_first is None else k_first
+    return list(zip(q_first, q_lens, k_first, k_lens, prefix or [0] * len(q_lens)))
+
+
+def check(mz, q, k, v, rows, **kw):
+    import torch
+    docs = mz.Documents.of([r[1] for r in rows], [r[3] for r in rows], [r[4] for r in rows],
+                           [r[0] for r in rows], [r[2] for r in rows])
+    out, lse = mz.attention(q, k, v, docs, return_lse=True, **kw)
+    assert out.dtype == q.dtype and out.shape == q.shape and lse.shape == q.shape[:2]
+    kw.pop("out", None)
+    want, want_lse, weight = attention_ref.attention(q, k, v, rows, **kw)
+    kw.pop("causal", None)
+    ob, lb = attention_ref.bounds(want, want_lse, weight, q.float(), k.float(), q.dtype,
+                                  max([r[3] for r in rows], default=0), **kw)
+    mine = torch.zeros(q.shape[0], dtype=torch.bool)
+    for r in rows:
+        mine[r[0]:r[0] + r[1]] = True
+    off = (out.cpu().double() - want).abs()[mine]
+    assert bool((off <= ob[mine]).all()), float((off / ob[mine]).max())
+    got, ref = lse.cpu().double()[mine], want_lse[mine]
+    empty = torch.isinf(ref)
+    assert bool((got[empty] == -math.inf).all())
+    assert bool(((got - ref).abs()[~empty] <= lb[mine][~empty]).all())
+    return out, lse
+
+
+DTYPES = ["f32", "bf16"]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dim", [8, 40, 64, 72, 80, 128])
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 64, 65, 129, 200])
+def test_one_document(mz, n, dim, dtype):
+    q, k, v = tensors(n, n, 2, 2, dim, dtype)
+    check(mz, q, k, v, table([n]))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (4, 1), (6, 2), (12, 4), (5, 5), (40, 1)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_ragged_documents_and_grouped_heads(mz, heads, kv_heads, causal, dtype):
+    lens = [1, 37, 0, 64, 3, 100]
+    q, k, v = tensors(sum(lens), sum(lens), heads, kv_heads, 64, dtype)
+    check(mz, q, k, v, table(lens, prefix=[0, 5, 0, 64, 2, 33]), causal=causal)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("prefix", [0, 1, 31, 32, 63, 64, 65, 149, 150])
+def test_prefix(mz, prefix, dtype):
+    q, k, v = tensors(150, 150, 2, 1, 64, dtype)
+    check(mz, q, k, v, table([150], prefix=[prefix]))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("softcap,bias", [(30.0, False), (0.0, True), (5.0, True), (50.0, False)])
+def test_capped_and_biased_scores(mz, softcap, bias, dim, dtype):
+    import torch
+    lens = [70, 150]
+    q, k, v = tensors(sum(lens), sum(lens), 4, 2, dim, dtype)
+    q = q * 3
+    slopes = torch.tensor([0.5, 0.03, 0.0, -0.01], device="cuda") if bias else None
+    check(mz, q, k, v, table(lens, prefix=[10, 0]), softcap=softcap, slopes=slopes)
+    check(mz, q[:3], k[:150], v[:150], table([1, 2], [70, 80], [0, 0]), softcap=softcap, slopes=slopes)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [0.5, -0.2, 0.0])
+def test_scale(mz, scale, dtype):
+    q, k, v = tensors(90, 90, 2, 2, 64, dtype)
+    check(mz, q, k, v, table([90]), scale=scale)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nq", [1, 2, 5, 16, 17, 70])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(8, 2, 128), (3, 3, 64), (8, 1, 40)])
+def test_new_tokens_over_a_cache(mz, nq, heads, kv_heads, dim, dtype):
+    """Caches with room between the documents, lengths around every stage's end."""
+    k_lens = [70, 128, 129, 400, 95]
+    cap = 410
+    q, k, v = tensors(nq * 5, cap * 5, heads, kv_heads, dim, dtype)
+    rows = table([nq] * 5, k_lens, k_first=[cap * d for d in range(5)])
+    nan = k.new_full((), float("nan"))
+    for d, n in enumerate(k_lens):  # what lies past a document's end is never used
+        k[cap * d + n:cap * (d + 1)] = nan
+        v[cap * d + n:cap * (d + 1)] = nan
+    import torch
+    out, _ = check_finite_ref(mz, q, k, v, rows)
+    assert bool(torch.isfinite(out.float()).all())
+
+
+def check_finite_ref(mz, q, k, v, rows, **kw):
+    """check(), for caches that hold NaN outside the documents."""
+    import torch
+    docs = mz.Documents.of([r[1] for r in rows], [r[3] for r in rows], [r[4] for r in rows],
+                           [r[0] for r in rows], [r[2] for r in rows])
+    out, lse = mz.attention(q, k, v, docs, return_lse=True, **kw)
+    kf, vf = torch.nan_to_num(k), torch.nan_to_num(v)
+    want, want_lse, weight = attention_ref.attention(q, kf, vf, rows, **kw)
+    ob, lb = attention_ref.bounds(want, want_lse, weight, q.float(), kf.float(), q.dtype, max(r[3] for r in rows))
+    off = (out.cpu().double() - want).abs()
+    assert bool((off <= ob).all()), float((off / ob).max())
+    assert bool(((lse.cpu().double() - want_lse).abs() <= lb).all())
+    return out, lse
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,nq", [(3000, 1), (5000, 4), (2600, 40), (4096, 129)])
+def test_long_caches_are_split(mz, n, nq, dtype):
+    q, k, v = tensors(nq, n, 4, 2, 64, dtype)
+    rows = table([nq], [n])
+    check(mz, q, k, v, rows)
+    # documents of very different length in one call: some splits are empty
+    q, k, v = tensors(3 * nq, n + 500, 4, 2, 64, dtype, seed=1)
+    check(mz, q, k, v, table([nq] * 3, [n, 300, nq], k_first=[0, n, n + 300]))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_more_queries_than_keys(mz, dtype):
+    """Queries before the first key see nothing: 0 and -inf."""
+    import torch
+    q, k, v = tensors(200, 60, 2, 2, 64, dtype)
+    out, lse = check(mz, q, k, v, table([120, 50, 30], [20, 40, 0]))
+    assert bool((out[:100] == 0).all()) and bool((lse[:100] == -math.inf).all())
+    assert bool((out[170:] == 0).all()) and bool((lse[170:] == -math.inf).all())
+    out, lse = check(mz, q[:5], k, v, table([3, 2], [2, 0]))
+    assert bool((out[0] == 0).all()) and bool((out[3:] == 0).all())
+    out, lse = check(mz, q[:5], k[:0], v[:0], table([5], [0]), causal=False)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    check(mz, q, k, v, table([120], [20], [7]))  # a prefix that all of them see
+    assert torch.isfinite(out.float()).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dim", [64, 128, 80])
+def test_strided_arrays(mz, dim, dtype):
+    """Parts of one projection's output, heads before tokens, a padded head."""
+    import torch
+    t, h, hk = 90, 4, 2
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    qkv = torch.randn(t, h + 2 * hk, dim, generator=g, device="cuda").to(dt)
+    check(mz, qkv[:, :h], qkv[:, h:h + hk], qkv[:, h + hk:], table([40, 50]))
+    heads_first = torch.randn(h + 2 * hk, t, dim, generator=g, device="cuda").to(dt).transpose(0, 1)
+    out = torch.empty(h, t, dim, dtype=dt, device="cuda").transpose(0, 1)
+    check(mz, heads_first[:, :h], heads_first[:, h:h + hk], heads_first[:, h + hk:], table([40, 50]), out=out)
+    wide = torch.randn(t, h + 2 * hk, dim + 16, generator=g, device="cuda").to(dt)[:, :, :dim]
+    out = torch.full((t, h, dim + 8), 7.0, dtype=dt, device="cuda")
+    check(mz, wide[:, :h], wide[:, h:h + hk], wide[:, h + hk:], table([40, 50]), out=out[:, :, :dim])
+    assert bool((out[:, :, dim:] == 7).all())
+    one = torch.randn(1, 1, dim, generator=g, device="cuda").to(dt).expand(t, hk, dim)  # the same key for all
+    check(mz, qkv[:, :h], one, qkv[:, h + hk:], table([40, 50]))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_tokens_of_no_document_keep_their_output(mz, dtype):
+    import torch
+    q, k, v = tensors(100, 100, 2, 2, 64, dtype)
+    out = torch.full_like(q, 3.0)
+    rows = table([20, 30], [20, 30], q_first=[10, 60], k_first=[50, 0])
+    check(mz, q, k, v, rows, out=out)
+    for a, b in ((0, 10), (30, 60), (90, 100)):
+        assert bool((out[a:b] == 3).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("nq,nk", [(150, 150), (4, 600), (3, 5000), (100, 3000)])
+def test_a_bad_token_reaches_only_those_that_see_it(mz, nq, nk, bad, dtype):
+    """A value (then a key) that is not finite, in the middle of the queries'
+    stretch: rows before it are as if it were not there."""
+    import torch
+    at = nk - nq + nq // 2
+    for which in ("v", "k", "q"):
+        q, k, v = tensors(nq, nk, 4, 2, 64, dtype)
+        docs = mz.Documents.of([nq], [nk])
+        clean, clean_lse = mz.attention(q, k, v, docs, return_lse=True)
+        if which == "q":
+            q[nq // 2, 1, 3] = bad
+            rows = torch.zeros(nq, 4, dtype=torch.bool)
+            rows[nq // 2, 1] = True
+        else:
+            (v if which == "v" else k)[at, 0, 3] = bad
+            rows = torch.zeros(nq, 4, dtype=torch.bool)
+            rows[nq // 2:, :2] = True  # the heads that read key/value head 0
+        out, lse = mz.attention(q, k, v, docs, return_lse=True)
+        same = ~rows.cuda()
+        tol = 2.0 ** -6 if dtype == "bf16" else 1e-4
+        assert bool(((out.float() - clean.float()).abs()[same] <= tol).all())
+        assert bool(((lse - clean_lse).abs()[same] <= 1e-4).all())
+        if which == "v":  # that column of those rows, and only it
+            assert not bool(torch.isfinite(out[~same][:, 3].float()).any())
+            others = [c for c in range(64) if c != 3]
+            assert bool(((out.float() - clean.float()).abs()[~same][:, others] <= tol).all())
+        elif math.isnan(bad):
+            assert bool(torch.isnan(out[~same].float()).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_lowest_and_largest_scores(mz, dtype):
+    """Scores near the ends of the type's range, and rows of equal huge scores."""
+    import torch
+    q, k, v = tensors(70, 70, 2, 2, 64, dtype)
+    docs = mz.Documents.of([70])
+    for scale in (1e30, -1e30):
+        out, lse = mz.attention(q, k, v, docs, scale=scale, return_lse=True)
+        want, _, _ = attention_ref.attention(q, k, v, table([70]), scale=scale)
+        assert float((out.cpu().double() - want).abs().max()) <= 2.0 ** -6
+    k[:] = 0
+    q[:] = 1
+    k[:, :, 0] = 3e30
+    out, lse = mz.attention(q, k, v, docs, scale=1e7, return_lse=True)
+    want = torch.cumsum(v.double(), 0) / torch.arange(1, 71, device="cuda")[:, None, None]
+    assert float((out.double() - want).abs().max()) <= 2.0 ** -5
+
+
+def test_a_table_that_points_outside_is_cut(mz):
+    """Rows past the arrays' ends and negative ones read and write inside them."""
+    import torch
+    q, k, v = tensors(50, 80, 2, 2, 64, "bf16")
+    raw = torch.tensor([[0, 10, 0, 10, 0], [10, 1 << 40, 60, 1 << 41, 1 << 62], [-5, -7, -9, 4, -3],
+                        [1 << 50, 6, 1 << 51, 6, 0]], dtype=torch.int64, device="cuda")
+    out, lse = mz.attention(q, k, v, mz.Documents(raw, 50, 80), return_lse=True)
+    want, _, _ = attention_ref.attention(q, k, v, [(0, 10, 0, 10, 0), (10, 40, 60, 20, 20)])
+    assert float((out.cpu().double() - want).abs().max()) <= 2.0 ** -5
+    torch.cuda.synchronize()
+
+
+def test_fewer_than_the_documents_queries(mz):
+    """max_q below a document's length: the queries past it are left out."""
+    import torch
+    q, k, v = tensors(200, 200, 2, 2, 64, "bf16")
+    rows = torch.tensor([[0, 200, 0, 200, 0]], dtype=torch.int64, device="cuda")
+    full = mz.attention(q, k, v, mz.Documents(rows, 200, 200))
+    out = torch.full_like(q, 5.0)
+    mz.attention(q, k, v, mz.Documents(rows, 70, 200), out=out)
+    assert torch.equal(out[:70], full[:70]) and bool((out[70:] == 5).all())
+
+
+def test_offsets_past_32_bits(mz):
+    """A cache of more than 2^32 elements: documents at its far end."""
+    import torch
+    tokens, hk, dim = (1 << 32) // (8 * 128) + 4096, 8, 128
+    k = torch.zeros(tokens, hk, dim, dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    q, ks, vs = tensors(2, 600, 16, hk, dim, "bf16")
+    at = tokens - 700
+    k[at:at + 600], v[at:at + 600] = ks, vs
+    rows = [(0, 1, at, 600, 0), (1, 1, at + 100, 500, 0)]
+    docs = mz.Documents.of([1, 1], [600, 500], k_first=[at, at + 100])
+    out = mz.attention(q, k, v, docs)
+    want, _, _ = attention_ref.attention(q, ks, vs, [(0, 1, 0, 600, 0), (1, 1, 100, 500, 0)])
+    assert float((out.cpu().double() - want).abs().max()) <= 2.0 ** -5
+    del rows
+
+
+def test_equal_inputs_equal_bits_on_any_stream_and_in_graphs(mz):
+    import torch
+    for nq, nk, heads in [(100, 100, 4), (1, 5000, 8), (3, 300, 2), (200, 4000, 2)]:
+        q, k, v = tensors(nq, nk, heads, 2, 64, "bf16")
+        docs = mz.Documents.of([nq], [nk])
+        want = mz.attention(q, k, v, docs, return_lse=True)
+        torch.cuda.synchronize()
+        s = torch.cuda.Stream()
+        got = mz.attention(q, k, v, docs, return_lse=True, stream=s)
+        s.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = mz.attention(q, k, v, docs, return_lse=True)
+        for i in range(3):
+            q.copy_(tensors(nq, nk, heads, 2, 64, "bf16", seed=i + 1)[0])
+            eager = mz.attention(q, k, v, docs, return_lse=True)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out[0], eager[0]) and torch.equal(out[1], eager[1])
+
+
+def test_refusals(mz):
+    import torch
+    q, k, v = tensors(10, 10, 4, 2, 64, "bf16")
+    docs = mz.Documents.of([10])
+    with pytest.raises(ValueError):
+        mz.attention(q, k, v[:, :1], docs)
+    with pytest.raises(ValueError):
+        mz.attention(q, k.repeat(1, 2, 1)[:, :3], v.repeat(1, 2, 1)[:, :3], docs)
+    with pytest.raises(TypeError):
+        mz.attention(q, k.float(), v, docs)
+    with pytest.raises(TypeError):
+        mz.attention(q.half(), k.half(), v.half(), docs)
+    with pytest.raises(ValueError):
+        mz.attention(q, k, v, docs, slopes=torch.zeros(3, device="cuda"))
+    with pytest.raises(ValueError):
+        mz.attention(q.transpose(1, 2), k, v, docs)
+    for bad in (dict(softcap=-1.0), dict(softcap=float("nan")), dict(scale=float("inf"))):
+        with pytest.raises(mz.MezoError) as e:
+            mz.attention(q, k, v, docs, **bad)
+        assert e.value.code == mz.ERANGE
+    for out in (q, torch.empty(10, 1, 64, dtype=torch.bfloat16, device="cuda").expand(10, 4, 64)):
+        with pytest.raises(mz.MezoError) as e:
+            mz.attention(q, k, v, docs, out=out)
+        assert e.value.code == mz.EOVERLAP
+    for dim in (4, 60, 136):
+        x = torch.zeros(10, 2, dim, dtype=torch.bfloat16, device="cuda")
+        with pytest.raises(mz.MezoError) as e:
+            mz.attention(x, x, x, docs)
+        assert e.value.code == mz.EINVAL
+    odd = torch.zeros(10, 2, 68, dtype=torch.bfloat16, device="cuda")[:, :, :64]  # heads 136 bytes apart
+    with pytest.raises(mz.MezoError) as e:
+        mz.attention(odd, odd, odd, docs)
+    assert e.value.code == mz.EINVAL
+    with pytest.raises(ValueError):
+        mz.Documents.of([3, 4], [5])
+    with pytest.raises(ValueError):
+        mz.Documents.of([3, -4])
+    with pytest.raises(ValueError):
+        mz.Documents.of([3, 4], q_first=[0, 2])
+    with pytest.raises(TypeError):
+        mz.Documents(docs.table.int(), 10, 10)
+    empty = mz.attention(q[:0], k, v, mz.Documents.of([]))
+    assert empty.shape == (0, 4, 64)
