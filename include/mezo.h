@@ -391,7 +391,7 @@ MEZO_API int mezo_nf4_dequantize(const void* codes, const float* absmax, uint64_
  * to a multiple of 4, the bytes e + 127, the row's end padded with zeros. */
 #define MEZO_F8_BLOCK 128u
 #define MEZO_F8_MAX_ROWS (1ull << 30)
-#define MEZO_F8_MAX_COLS (1ull << 30)
+#define MEZO_F8_MAX_COLS (1ull << 23)
 
 /* Quantize a [rows, cols] matrix of storage src_dtype (MEZO_F32 or MEZO_BF16),
  * rows ld elements apart, into codes (16-byte aligned) and scales (4-byte
@@ -410,6 +410,14 @@ MEZO_API int mezo_f8_quantize(const void* src, uint32_t src_dtype, uint64_t rows
  * must not overlap the operands (MEZO_EOVERLAP). */
 MEZO_API uint64_t mezo_f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t c_dtype);
 MEZO_API int mezo_f8_matmul(const void* x_codes, const uint8_t* x_scales, const void* w_codes,
+                            const uint8_t* w_scales, uint64_t m, uint64_t n, uint64_t k, void* c, uint32_t c_dtype,
+                            uint64_t ldc, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* A layer's product in one call: x [m, k] of storage x_dtype, rows ldx elements
+ * apart, quantized into the workspace as mezo_f8_quantize does, then
+ * mezo_f8_matmul with the weights w. Always needs its workspace. */
+MEZO_API uint64_t mezo_f8_linear_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t c_dtype);
+MEZO_API int mezo_f8_linear(const void* x, uint32_t x_dtype, uint64_t ldx, const void* w_codes,
                             const uint8_t* w_scales, uint64_t m, uint64_t n, uint64_t k, void* c, uint32_t c_dtype,
                             uint64_t ldc, void* workspace, uint64_t workspace_bytes, void* stream);
 

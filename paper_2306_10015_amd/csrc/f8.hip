@@ -18,6 +18,7 @@
 #include <type_traits>
 
 #include "f8_launch.hpp"
+#include "lds_dma.hpp"
 #include "records.hpp"
 #include "stream_io.hpp"
 
@@ -209,31 +210,41 @@ __device__ __forceinline__ v4f_t mma(const Operand<true>& a, const Operand<true>
     return c;
 }
 
-// A lane's four results, columns col .. col + 3 of a row of c.
-__device__ __forceinline__ void store4(const F8MatmulArgs& a, uint32_t row, uint32_t col, v4f_t v)
+typedef __bf16 v4bf_t __attribute__((ext_vector_type(4)));
+
+// A lane's four results, columns col .. col + 3 of a row of c: fp32 if kWide, else
+// bf16. `whole`: every group of four columns lies on 4 elements' alignment.
+template <bool kWide>
+__device__ __forceinline__ void store4(const F8MatmulArgs& a, bool whole, uint32_t row, uint32_t col, v4f_t v)
 {
     const uint64_t e = row * a.ldc + col;
-    if (a.out_dtype == kF32) {
+    if constexpr (kWide) {
         gfloat_t* p = reinterpret_cast<gfloat_t*>(a.c) + e;
-        if (col + 4 <= a.n && ((a.c | (a.ldc * 4)) & 15u) == 0) {
+        if (whole && col + 4 <= a.n) {
             *reinterpret_cast<MEZO_GLOBAL v4f_t*>(p) = v;
         } else {
 #pragma unroll
             for (uint32_t i = 0; i < 4; ++i)
                 if (col + i < a.n) p[i] = v[i];
         }
-        return;
-    }
-    typedef __bf16 v4bf_t __attribute__((ext_vector_type(4)));
-    const v4bf_t b = __builtin_convertvector(v, v4bf_t);
-    MEZO_GLOBAL __bf16* p = reinterpret_cast<MEZO_GLOBAL __bf16*>(a.c) + e;
-    if (col + 4 <= a.n && ((a.c | (a.ldc * 2)) & 7u) == 0) {
-        *reinterpret_cast<MEZO_GLOBAL v4bf_t*>(p) = b;
     } else {
+        const v4bf_t b = __builtin_convertvector(v, v4bf_t);
+        MEZO_GLOBAL __bf16* p = reinterpret_cast<MEZO_GLOBAL __bf16*>(a.c) + e;
+        if (whole && col + 4 <= a.n) {
+            *reinterpret_cast<MEZO_GLOBAL v4bf_t*>(p) = b;
+        } else {
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i)
-            if (col + i < a.n) p[i] = b[i];
+            for (uint32_t i = 0; i < 4; ++i)
+                if (col + i < a.n) p[i] = b[i];
+        }
     }
+}
+
+template <bool kWide>
+__device__ __forceinline__ bool whole_groups(const F8MatmulArgs& a)
+{
+    constexpr uint64_t kBytes = kWide ? 4 : 2;
+    return ((a.c | (a.ldc * kBytes)) & (4 * kBytes - 1)) == 0;
 }
 
 // 16 bytes that other workgroups read too.
@@ -243,13 +254,6 @@ __device__ __forceinline__ uint4 load_shared(uint64_t addr)
     return make_uint4(v.x, v.y, v.z, v.w);
 }
 
-// 16 bytes from global memory straight into LDS: lane l's go to lds + 16 l.
-__device__ __forceinline__ void load_to_lds(uint64_t addr, const void* lds)
-{
-    __builtin_amdgcn_global_load_lds(reinterpret_cast<const MEZO_GLOBAL void*>(addr),
-                                     (__attribute__((address_space(3))) void*)(lds), 16, 0, 0);
-}
-
 // Tiles of kBM activations x kBN weights, kWM x kWN waves. Weights are the matrix
 // instruction's rows and activations its columns, so that a lane's four results
 // lie next to each other in a row of c.
@@ -257,14 +261,17 @@ __device__ __forceinline__ void load_to_lds(uint64_t addr, const void* lds)
 // A stage is one block of 128 of every row of the tile, loaded straight into LDS;
 // two stages, one computed on while the other loads. A row's eight 16-byte chunks
 // are stored at chunk ^ (row & 7): the 16 rows of a fragment then spread over all
-// banks.
+// banks. The scales of four blocks are a word of a row; they come the same way,
+// every fourth stage.
 template <uint32_t kBM, uint32_t kBN, uint32_t kWM, uint32_t kWN, bool kWide>
 __global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a)
 {
     constexpr uint32_t kWaves = kWM * kWN, kRows = kBM + kBN;
     constexpr uint32_t kFM = kBM / kWM / 16, kFN = kBN / kWN / 16;  // fragments of a wave
     constexpr uint32_t kLoads = kRows / 8 / kWaves;                 // 8 rows a load
+    static_assert(kRows == kWaves * 64, "a word of scales a lane");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2][kRows * 128];
+    __shared__ __attribute__((aligned(256))) uint32_t scales[2][kRows];
 
     const uint32_t l = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // workgroups go round the 8 XCDs: give each XCD a compact part of c (its L2 then
@@ -277,88 +284,90 @@ __global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a
     const uint32_t m0 = (band * 8 + in % height) * kBM, n0 = in / height * kBN;
 
     const uint32_t blocks = uint32_t(f8_blocks(a.k));
-    const uint64_t stride = f8_code_stride(a.k);
-    // this lane's 16 bytes of each of its rows (past the end: the last row's again)
-    uint64_t src[kLoads];
+    const uint32_t stride = uint32_t(f8_code_stride(a.k)), sstride = uint32_t(f8_scale_stride(a.k));
+    // a wave's loads are all of x's rows or all of w's; rows past the end: the last
+    // one's again
+    static_assert(kBM % (8 * kLoads) == 0 && kBM % 64 == 0, "a wave loads rows of one operand");
+    const bool ofx = wave * kLoads * 8 < kBM, sofx = wave * 64 < kBM;
+    const uint64_t codes = ofx ? a.x + uint64_t(m0) * stride : a.w + uint64_t(n0) * stride;
+    const uint64_t words = sofx ? a.xs + uint64_t(m0) * sstride : a.ws + uint64_t(n0) * sstride;
+    uint32_t src[kLoads];  // this lane's 16 bytes of each of its rows
 #pragma unroll
     for (uint32_t i = 0; i < kLoads; ++i) {
-        const uint32_t r = (wave * kLoads + i) * 8 + (l >> 3);
-        const uint32_t chunk = (l & 7u) ^ (l >> 3);
-        const uint32_t xr = m0 + r < a.m ? m0 + r : a.m - 1;
-        const uint32_t wr = n0 + r - kBM < a.n ? n0 + r - kBM : a.n - 1;
-        src[i] = (r < kBM ? a.x + xr * stride : a.w + wr * stride) + chunk * 16;
+        const uint32_t r = (wave * kLoads + i) * 8 + (l >> 3) - (ofx ? 0 : kBM);
+        const uint32_t end = (ofx ? a.m - m0 : a.n - n0) - 1;
+        src[i] = (r < end ? r : end) * stride + ((l & 7u) ^ (l >> 3)) * 16;
     }
-    const uint32_t fr = l & 15u, fg = l >> 4;
-    const uint32_t wm = (wave / kWN) * kFM * 16, wn = (wave % kWN) * kFN * 16;
-    const uint64_t sstride = f8_scale_stride(a.k);
-    uint64_t xs[kFM], ws[kFN];
-#pragma unroll
-    for (uint32_t i = 0; i < kFM; ++i) {
-        const uint32_t r = m0 + wm + i * 16 + fr;
-        xs[i] = a.xs + (r < a.m ? r : a.m - 1) * sstride;
+    uint32_t word;
+    {
+        const uint32_t r = wave * 64 + l - (sofx ? 0 : kBM), end = (sofx ? a.m - m0 : a.n - n0) - 1;
+        word = (r < end ? r : end) * sstride;
     }
-#pragma unroll
-    for (uint32_t i = 0; i < kFN; ++i) {
-        const uint32_t r = n0 + wn + i * 16 + fr;
-        ws[i] = a.ws + (r < a.n ? r : a.n - 1) * sstride;
-    }
-    v4f_t acc[kFM][kFN] = {};
+    const uint32_t lds0 = lds_offset(&lds[0][0]) + wave * kLoads * 1024;
+    const uint32_t sc0 = lds_offset(&scales[0][0]) + wave * 256;
     auto stage = [&](uint32_t kb) {
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; ++i)
-            load_to_lds(src[i] + uint64_t(kb) * 128, &lds[kb & 1][(wave * kLoads + i) * 1024]);
+            dma_to_lds(codes + uint64_t(kb) * 128, src[i], lds0 + (kb & 1) * kRows * 128 + i * 1024);
     };
-    uint32_t sx[kFM], sw[kFN], nx[kFM], nw[kFN];  // the scales of four blocks, and of the next four
-    auto scales = [&](uint32_t kb) {
-#pragma unroll
-        for (uint32_t i = 0; i < kFM; ++i) nx[i] = *reinterpret_cast<const gu32_t*>(xs[i] + kb);
-#pragma unroll
-        for (uint32_t i = 0; i < kFN; ++i) nw[i] = *reinterpret_cast<const gu32_t*>(ws[i] + kb);
+    auto scale_words = [&](uint32_t group) {
+        dma_word_to_lds(words + uint64_t(group) * 4, word, sc0 + (group & 1) * kRows * 4);
     };
-    scales(0);
+
+    const uint32_t fr = l & 15u, fg = l >> 4;
+    const uint32_t wm = (wave / kWN) * kFM * 16, wn = (wave % kWN) * kFN * 16;
+    v4f_t acc[kFM][kFN] = {};
+    uint32_t sx[kFM], sw[kFN];  // the scales of four blocks
+    struct Fragment {
+        uint4 lo, hi;
+    };
+    scale_words(0);
     stage(0);
     for (uint32_t kb = 0; kb < blocks; ++kb) {
-        __syncthreads();  // stage kb is there, and nobody reads the other one any more
-        if ((kb & 3u) == 0) {
-#pragma unroll
-            for (uint32_t i = 0; i < kFM; ++i) sx[i] = nx[i];
-#pragma unroll
-            for (uint32_t i = 0; i < kFN; ++i) sw[i] = nw[i];
-            if (kb + 4 < blocks) scales(kb + 4);
-        }
+        dma_wait();
+        lds_barrier();  // stage kb is there, and nobody reads the other one any more
         if (kb + 1 < blocks) stage(kb + 1);
+        if ((kb & 3u) == 0) {
+            const uint32_t* s = scales[(kb >> 2) & 1];
+#pragma unroll
+            for (uint32_t i = 0; i < kFM; ++i) sx[i] = s[wm + i * 16 + fr];
+#pragma unroll
+            for (uint32_t i = 0; i < kFN; ++i) sw[i] = s[kBM + wn + i * 16 + fr];
+            if (kb + 4 < blocks) scale_words((kb >> 2) + 1);
+        }
         const uint8_t* t = lds[kb & 1];
         const uint32_t shift = (kb & 3u) * 8;
         auto fragment = [&](uint32_t row) {
             const uint32_t r = row + fr;
-            struct {
-                uint4 lo, hi;
-            } f;
+            Fragment f;
             f.lo = *reinterpret_cast<const uint4*>(t + r * 128 + ((fg ^ (fr & 7u)) * 16));
             f.hi = *reinterpret_cast<const uint4*>(t + r * 128 + (((fg + 4) ^ (fr & 7u)) * 16));
             return f;
         };
         Operand<kWide> w[kFN];
+        Fragment next = fragment(wm);
 #pragma unroll
         for (uint32_t j = 0; j < kFN; ++j) {
-            const auto f = fragment(kBM + wn + j * 16);
+            const Fragment f = fragment(kBM + wn + j * 16);
             w[j].set(f.lo, f.hi, sw[j] >> shift);
         }
 #pragma unroll
         for (uint32_t i = 0; i < kFM; ++i) {
-            const auto f = fragment(wm + i * 16);
+            const Fragment f = next;
+            if (i + 1 < kFM) next = fragment(wm + (i + 1) * 16);
             Operand<kWide> x;
             x.set(f.lo, f.hi, sx[i] >> shift);
 #pragma unroll
             for (uint32_t j = 0; j < kFN; ++j) acc[i][j] = mma(w[j], x, acc[i][j]);
         }
     }
+    const bool whole = whole_groups<kWide>(a);
 #pragma unroll
     for (uint32_t i = 0; i < kFM; ++i) {
         const uint32_t row = m0 + wm + i * 16 + fr;
         if (row < a.m) {
 #pragma unroll
-            for (uint32_t j = 0; j < kFN; ++j) store4(a, row, n0 + wn + j * 16 + fg * 4, acc[i][j]);
+            for (uint32_t j = 0; j < kFN; ++j) store4<kWide>(a, whole, row, n0 + wn + j * 16 + fg * 4, acc[i][j]);
         }
     }
 }
@@ -428,7 +437,7 @@ __global__ void __launch_bounds__(kWaves * 64) f8_thin_kernel(F8MatmulArgs a)
         v4f_t sum = part[0][i][l];
 #pragma unroll
         for (uint32_t v = 1; v < kWaves; ++v) sum += part[v][i][l];
-        if (i * 16 + fr < a.m) store4(a, i * 16 + fr, n0 + fg * 4, sum);
+        if (i * 16 + fr < a.m) store4<kWide>(a, whole_groups<kWide>(a), i * 16 + fr, n0 + fg * 4, sum);
     }
 }
 

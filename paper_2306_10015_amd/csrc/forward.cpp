@@ -64,8 +64,9 @@ Range f8_scales(const void* scales, uint64_t rows, uint64_t cols)
     return {address(scales), rows * mezo::f8_scale_stride(cols)};
 }
 
-int f8_quantize(const void* src, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ld, void* codes, uint8_t* scales,
-                void* stream)
+// The checks of a quantization, and its kernel's arguments.
+int check_quantize(const void* src, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ld, void* codes,
+                   void* scales, mezo::F8QuantArgs& a)
 {
     if (!dense(dtype)) return MEZO_EDTYPE;
     if (!src || !codes || !scales || !f8_sizes(rows, cols) || (rows > 1 && ld < cols)) return MEZO_EINVAL;
@@ -75,7 +76,6 @@ int f8_quantize(const void* src, uint32_t dtype, uint64_t rows, uint64_t cols, u
     const Range in = {address(src), bytes}, c = f8_codes(codes, rows, cols), s = f8_scales(scales, rows, cols);
     const Range read[2] = {in, c};
     if (clashes(c, &in, 1) || clashes(s, read, 2)) return MEZO_EOVERLAP;
-    mezo::F8QuantArgs a;
     a.values = in.at;
     a.ld = ld;
     a.codes = c.at;
@@ -83,13 +83,13 @@ int f8_quantize(const void* src, uint32_t dtype, uint64_t rows, uint64_t cols, u
     a.rows = static_cast<uint32_t>(rows);
     a.cols = static_cast<uint32_t>(cols);
     a.dtype = dtype;
-    MEZO_HIP(mezo::launch_f8_quantize(a, static_cast<hipStream_t>(stream)));
     return MEZO_OK;
 }
 
-int f8_matmul(const void* x_codes, const uint8_t* x_scales, const void* w_codes, const uint8_t* w_scales, uint64_t m,
-              uint64_t n, uint64_t k, void* c, uint32_t c_dtype, uint64_t ldc, void* workspace,
-              uint64_t workspace_bytes, void* stream)
+// The checks of a product, and its kernel's arguments.
+int check_matmul(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, uint64_t m,
+                 uint64_t n, uint64_t k, void* c, uint32_t c_dtype, uint64_t ldc, void* workspace,
+                 uint64_t workspace_bytes, mezo::F8MatmulArgs& a)
 {
     if (!dense(c_dtype)) return MEZO_EDTYPE;
     if (!x_codes || !x_scales || !w_codes || !w_scales || !c || !f8_sizes(m, k) || !f8_sizes(n, k) ||
@@ -106,7 +106,6 @@ int f8_matmul(const void* x_codes, const uint8_t* x_scales, const void* w_codes,
     const Range read[5] = {f8_codes(x_codes, m, k), f8_scales(x_scales, m, k), f8_codes(w_codes, n, k),
                            f8_scales(w_scales, n, k), out};
     if (clashes(out, read, 4) || (need && clashes(scratch, read, 5))) return MEZO_EOVERLAP;
-    mezo::F8MatmulArgs a;
     a.x = read[0].at;
     a.xs = read[1].at;
     a.w = read[2].at;
@@ -118,7 +117,48 @@ int f8_matmul(const void* x_codes, const uint8_t* x_scales, const void* w_codes,
     a.n = static_cast<uint32_t>(n);
     a.k = static_cast<uint32_t>(k);
     a.out_dtype = c_dtype;
-    MEZO_HIP(mezo::launch_f8_matmul(a, static_cast<hipStream_t>(stream)));
+    return MEZO_OK;
+}
+
+// The layout of a linear call's workspace: x's codes, its scales, the product's.
+struct LinearSpace {
+    uint64_t scales, product, bytes;
+};
+
+LinearSpace linear_space(uint64_t m, uint64_t n, uint64_t k, uint32_t c_dtype)
+{
+    LinearSpace s;
+    s.scales = m * mezo::f8_code_stride(k);
+    s.product = s.scales + (m * mezo::f8_scale_stride(k) + 15) / 16 * 16;
+    s.bytes = s.product + mezo::f8_matmul_workspace(m, n, k, c_dtype);
+    return s;
+}
+
+int f8_linear(const void* x, uint32_t x_dtype, uint64_t ldx, const void* w_codes, const uint8_t* w_scales, uint64_t m,
+              uint64_t n, uint64_t k, void* c, uint32_t c_dtype, uint64_t ldc, void* workspace,
+              uint64_t workspace_bytes, void* stream)
+{
+    if (!dense(x_dtype) || !dense(c_dtype)) return MEZO_EDTYPE;
+    if (!workspace || !aligned(workspace, 16) || !f8_sizes(m, k) || !f8_sizes(n, k)) return MEZO_EINVAL;
+    const LinearSpace s = linear_space(m, n, k, c_dtype);
+    if (workspace_bytes < s.bytes) return MEZO_EINVAL;
+    char* const codes = static_cast<char*>(workspace);
+    mezo::F8QuantArgs q;
+    mezo::F8MatmulArgs a;
+    int rc = check_quantize(x, x_dtype, m, k, ldx, codes, codes + s.scales, q);
+    if (rc == MEZO_OK)
+        rc = check_matmul(codes, codes + s.scales, w_codes, w_scales, m, n, k, c, c_dtype, ldc, codes + s.product,
+                          workspace_bytes - s.product, a);
+    if (rc != MEZO_OK) return rc;
+    uint64_t in = 0, out = 0;  // (both checked to fit)
+    matrix_bytes(m, k, ldx, element_bytes(x_dtype), in);
+    matrix_bytes(m, n, ldc, element_bytes(c_dtype), out);
+    const Range scratch = {address(workspace), s.bytes};
+    const Range others[4] = {{address(x), in}, {address(c), out}, f8_codes(w_codes, n, k), f8_scales(w_scales, n, k)};
+    if (overlap(others[0], others[1]) || clashes(scratch, others, 4)) return MEZO_EOVERLAP;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    MEZO_HIP(mezo::launch_f8_quantize(q, st));
+    MEZO_HIP(mezo::launch_f8_matmul(a, st));
     return MEZO_OK;
 }
 
@@ -276,8 +316,13 @@ extern "C" {
 int mezo_f8_quantize(const void* src, uint32_t src_dtype, uint64_t rows, uint64_t cols, uint64_t ld, void* codes,
                      uint8_t* scales, void* stream)
 {
-    return guarded("mezo_f8_quantize",
-                   [&] { return f8_quantize(src, src_dtype, rows, cols, ld, codes, scales, stream); });
+    return guarded("mezo_f8_quantize", [&]() -> int {
+        mezo::F8QuantArgs a;
+        const int rc = check_quantize(src, src_dtype, rows, cols, ld, codes, scales, a);
+        if (rc != MEZO_OK) return rc;
+        MEZO_HIP(mezo::launch_f8_quantize(a, static_cast<hipStream_t>(stream)));
+        return MEZO_OK;
+    });
 }
 
 uint64_t mezo_f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t c_dtype)
@@ -289,8 +334,27 @@ int mezo_f8_matmul(const void* x_codes, const uint8_t* x_scales, const void* w_c
                    uint64_t m, uint64_t n, uint64_t k, void* c, uint32_t c_dtype, uint64_t ldc, void* workspace,
                    uint64_t workspace_bytes, void* stream)
 {
-    return guarded("mezo_f8_matmul", [&] {
-        return f8_matmul(x_codes, x_scales, w_codes, w_scales, m, n, k, c, c_dtype, ldc, workspace, workspace_bytes,
+    return guarded("mezo_f8_matmul", [&]() -> int {
+        mezo::F8MatmulArgs a;
+        const int rc = check_matmul(x_codes, x_scales, w_codes, w_scales, m, n, k, c, c_dtype, ldc, workspace,
+                                    workspace_bytes, a);
+        if (rc != MEZO_OK) return rc;
+        MEZO_HIP(mezo::launch_f8_matmul(a, static_cast<hipStream_t>(stream)));
+        return MEZO_OK;
+    });
+}
+
+uint64_t mezo_f8_linear_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t c_dtype)
+{
+    return dense(c_dtype) && f8_sizes(m, k) && f8_sizes(n, k) ? linear_space(m, n, k, c_dtype).bytes : 0;
+}
+
+int mezo_f8_linear(const void* x, uint32_t x_dtype, uint64_t ldx, const void* w_codes, const uint8_t* w_scales,
+                   uint64_t m, uint64_t n, uint64_t k, void* c, uint32_t c_dtype, uint64_t ldc, void* workspace,
+                   uint64_t workspace_bytes, void* stream)
+{
+    return guarded("mezo_f8_linear", [&] {
+        return f8_linear(x, x_dtype, ldx, w_codes, w_scales, m, n, k, c, c_dtype, ldc, workspace, workspace_bytes,
                          stream);
     });
 }

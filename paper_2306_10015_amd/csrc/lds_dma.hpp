@@ -31,6 +31,28 @@ __device__ __forceinline__ void dma_to_lds(uint64_t addr, uint32_t lds)
                  : "memory");
 }
 
+// The same with the address as a uniform base and a lane's 32-bit offset.
+__device__ __forceinline__ void dma_to_lds(uint64_t base, uint32_t offset, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %0, %1"
+                 :
+                 : "v"(offset), "s"(base), "s"(lds)
+                 : "memory");
+}
+
+// 4 bytes a lane: lane l's go to LDS byte lds + 4 l.
+__device__ __forceinline__ void dma_word_to_lds(uint64_t base, uint32_t offset, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dword %0, %1"
+                 :
+                 : "v"(offset), "s"(base), "s"(lds)
+                 : "memory");
+}
+
 // Wait until at most kLeft of the wave's loads (the latest) are still in flight.
 template <int kLeft = 0>
 __device__ __forceinline__ void dma_wait()

@@ -16,6 +16,7 @@ with ``python -m paper_2306_10015_amd.build``); there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 from pathlib import Path
@@ -77,6 +78,7 @@ EXPORTS = ("mezo_paramset_create", "mezo_paramset_destroy", "mezo_paramset_numel
            "mezo_update_multi_from", "mezo_checksum", "quantize_projgrad",
            "mezo_dequantize", "mezo_nf4_quantize", "mezo_nf4_dequantize",
            "mezo_f8_quantize", "mezo_f8_matmul_workspace", "mezo_f8_matmul",
+           "mezo_f8_linear_workspace", "mezo_f8_linear",
            "mezo_attention_workspace", "mezo_attention",
            "mezo_token_loss_workspace", "mezo_token_loss", "mezo_debug_generate", "mezo_debug_box_muller",
            "mezo_strerror", "mezo_last_error", "mezo_version")
@@ -131,6 +133,10 @@ def _load() -> ctypes.CDLL:
     L.mezo_f8_matmul_workspace.restype = u64
     L.mezo_f8_matmul.argtypes = [vp, vp, vp, vp, u64, u64, u64, vp, u32, u64, vp, u64, vp]
     L.mezo_f8_matmul.restype = i32
+    L.mezo_f8_linear_workspace.argtypes = [u64, u64, u64, u32]
+    L.mezo_f8_linear_workspace.restype = u64
+    L.mezo_f8_linear.argtypes = [vp, u32, u64, vp, vp, u64, u64, u64, vp, u32, u64, vp, u64, vp]
+    L.mezo_f8_linear.restype = i32
     L.mezo_attention_workspace.argtypes = [ctypes.POINTER(Attention)]
     L.mezo_attention_workspace.restype = u64
     L.mezo_attention.argtypes = [ctypes.POINTER(Attention), vp, u64, vp]
@@ -275,14 +281,21 @@ def nf4_dequantize(t: NF4Tensor, dtype=None, out=None, stream=None):
 
 # ---- the forward pass ------------------------------------------------------
 
+_NO_SWITCH = contextlib.nullcontext()
+_DEVICES = 0
+
+
 def _on(device, stream):
     """Run a call on `device`, its outputs and scratch allocated on the stream
     it runs on (memory of another stream's pool could still be in use there)."""
-    import contextlib
     import torch
+    global _DEVICES
+    if not _DEVICES:
+        _DEVICES = torch.cuda.device_count()
+    if stream is None and _DEVICES == 1:
+        return _NO_SWITCH  # (a context of its own costs a small call 2 us)
     stack = contextlib.ExitStack()
-    if torch.cuda.device_count() > 1:
-        stack.enter_context(torch.cuda.device(device))
+    stack.enter_context(torch.cuda.device(device))
     if stream is not None:
         if not isinstance(stream, torch.cuda.Stream):
             stream = torch.cuda.ExternalStream(int(stream), device=device)
@@ -302,10 +315,10 @@ def _rows_of(t, what: str):
     return rows, cols, t.stride(0) if rows > 1 else cols
 
 
-def _same_device(*tensors):
-    devices = {t.device for t in tensors if t is not None}
-    if len(devices) != 1:
-        raise ValueError(f"tensors on several devices: {sorted(map(str, devices))}")
+def _same_device(first, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on several devices: {first.device} and {t.device}")
 
 
 def _scratch(nbytes: int, device):
@@ -393,11 +406,30 @@ def f8_matmul(x: F8Matrix, w: F8Matrix, dtype=None, out=None, stream=None):
 
 def f8_linear(x, w: F8Matrix, dtype=None, out=None, stream=None):
     """A layer's product: the activations x (fp32/bf16 [m, k]) quantized, times
-    the weights w ([n, k]) in 8-bit storage: [m, n] of dtype (x's by default)."""
-    if dtype is None and out is None:
-        dtype = x.dtype
+    the weights w ([n, k]) in 8-bit storage: [m, n] of dtype (x's by default).
+    The same as f8_matmul(f8_quantize(x), w, dtype), in one call."""
+    import torch
+    m, k, ldx = _rows_of(x, "x")
+    if k != w.cols:
+        raise ValueError(f"x has {k} columns, w {w.cols}")
+    n, x_code = w.rows, _dtype_code(x)
     with _on(x.device, stream):
-        return f8_matmul(f8_quantize(x), w, dtype, out)
+        if out is None:
+            out = torch.empty(m, n, dtype=dtype or x.dtype, device=x.device)
+            ldc = n
+        else:
+            if dtype is not None and out.dtype != dtype:
+                raise TypeError(f"out is {out.dtype}, dtype {dtype}")
+            if out.shape != (m, n):
+                raise ValueError(f"out is {tuple(out.shape)}, the product {(m, n)}")
+            ldc = _rows_of(out, "out")[2]
+        _same_device(x, w.codes, out)
+        code = _dtype_code(out)
+        nbytes = lib.mezo_f8_linear_workspace(m, n, k, code)
+        ws = _scratch(nbytes, x.device)
+        _check(lib.mezo_f8_linear(x.data_ptr(), x_code, ldx, w.codes.data_ptr(), w.scales.data_ptr(), m, n, k,
+                                  out.data_ptr(), code, ldc, _ptr(ws), nbytes, _stream_ptr(None)), "mezo_f8_linear")
+    return out
 
 
 class Documents:
@@ -583,7 +615,6 @@ class ParamSet:
         """Make the paramset's device current for a call (a stream or pointer
         of another device would not be valid for its kernels); with a single
         visible device there is nothing to switch."""
-        import contextlib
         import torch
         return torch.cuda.device(self.device) if self._switch else contextlib.nullcontext()
 
