@@ -15,8 +15,6 @@
 //  fp32: the codes are widened to bf16 in registers, exactly, their scales
 //        applied, and v_mfma_f32_16x16x32_bf16 sums the exact products in fp32
 //        (error 1e-8 to 2e-7, as a chain of fp32 additions), at half the rate.
-#include <type_traits>
-
 #include "f8_launch.hpp"
 #include "lds_dma.hpp"
 #include "records.hpp"
@@ -247,11 +245,21 @@ __device__ __forceinline__ bool whole_groups(const F8MatmulArgs& a)
     return ((a.c | (a.ldc * kBytes)) & (4 * kBytes - 1)) == 0;
 }
 
-// 16 bytes that other workgroups read too.
-__device__ __forceinline__ uint4 load_shared(uint64_t addr)
+// Where a split of k leaves its sums: rows of whole groups of four columns.
+__device__ __forceinline__ uint64_t partial_at(const F8MatmulArgs& a, uint32_t split, uint32_t row, uint32_t col)
 {
-    const u32x4_t v = *reinterpret_cast<const gu32x4_t*>(addr);
-    return make_uint4(v.x, v.y, v.z, v.w);
+    return a.partial + ((uint64_t(split) * a.m + row) * ((a.n + 3) / 4) + col / 4) * 16;
+}
+
+// A lane's four results of a tile: into c, or of a split product into its partials.
+template <bool kWide>
+__device__ __forceinline__ void store_result(const F8MatmulArgs& a, bool whole, uint32_t split, uint32_t row,
+                                             uint32_t col, v4f_t v)
+{
+    if (a.splits == 1)
+        store4<kWide>(a, whole, row, col, v);
+    else if (col < a.n)
+        *reinterpret_cast<MEZO_GLOBAL v4f_t*>(partial_at(a, split, row, col)) = v;
 }
 
 // Tiles of kBM activations x kBN weights, kWM x kWN waves. Weights are the matrix
@@ -372,96 +380,163 @@ __global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a
     }
 }
 
-// A product of few activations: bound by the weights' bytes. A workgroup takes 16
-// weights' rows and all m <= 16 kFM activations; its waves share out the blocks of
-// k and load both operands from global memory straight into registers, a few
-// blocks ahead; their sums join through LDS in the order of the waves.
-constexpr uint32_t kThinAhead = 4;
+// A product of few activations, m <= 16 kFM: bound by the weights' bytes. A
+// workgroup takes 64 weights' rows, a wave 16 of them, and a share of k. A stage is
+// four blocks of every row (512 bytes, and a word of scales), loaded straight into
+// LDS, as many stages in flight as fit. Fragments loaded from global memory straight
+// into registers would need neither LDS nor barriers, but there neighbouring lanes
+// read different rows, and the address units take such a load apart line by line:
+// 25 us for 24 activations and 16384 x 4096 weights, as slow with all weights in L2.
+constexpr uint32_t kThinRows = 64, kThinBytes = 512, kThinBlocks = 4;
 
-template <uint32_t kFM, uint32_t kWaves, bool kWide>
-__global__ void __launch_bounds__(kWaves * 64) f8_thin_kernel(F8MatmulArgs a)
+template <uint32_t kFM, bool kWide>
+__global__ void __launch_bounds__(256) f8_thin_kernel(F8MatmulArgs a)
 {
+    constexpr uint32_t kX = kFM * 16, kRows = kThinRows + kX, kStage = kRows * kThinBytes;
+    constexpr uint32_t kDepth = kFM == 4 ? 2 : 3;
+    constexpr uint32_t kWLoads = kThinRows / 8, kXLoads = kX / 8;  // a wave's, 2 rows each
+    constexpr uint32_t kPerStage = kWLoads + kXLoads + 1;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kDepth][kStage];
+    __shared__ __attribute__((aligned(256))) uint32_t scales[kDepth][kThinRows + 64];
+
     const uint32_t l = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t fr = l & 15u, fg = l >> 4, n0 = blockIdx.x * 16;
-    const uint32_t blocks = uint32_t(f8_blocks(a.k));
-    const uint64_t stride = f8_code_stride(a.k), sstride = f8_scale_stride(a.k);
-    const uint32_t b0 = blocks * wave / kWaves, b1 = blocks * (wave + 1) / kWaves;
-    const uint64_t wr = n0 + fr < a.n ? n0 + fr : a.n - 1;
-    const uint64_t w = a.w + wr * stride + fg * 16, ws = a.ws + wr * sstride;
-    uint64_t x[kFM], xs[kFM];
+    const uint32_t n0 = blockIdx.x * kThinRows;
+    const uint32_t blocks = uint32_t(f8_blocks(a.k)), stages = (blocks + kThinBlocks - 1) / kThinBlocks;
+    const uint32_t s0 = stages * blockIdx.y / a.splits, s1 = stages * (blockIdx.y + 1) / a.splits;
+    const uint32_t stride = uint32_t(f8_code_stride(a.k)), sstride = uint32_t(f8_scale_stride(a.k));
+    const uint64_t w0 = a.w + uint64_t(n0) * stride, ws0 = a.ws + uint64_t(n0) * sstride;
+    const uint32_t wend = a.n - n0 - 1, xend = a.m - 1;
+    // wave 0 loads x's scales, the others w's (three times the same)
+    const uint64_t words = wave == 0 ? a.xs : ws0;
+    const uint32_t word = (l < (wave == 0 ? xend : wend) ? l : (wave == 0 ? xend : wend)) * sstride;
+    const uint32_t lds0 = lds_offset(&lds[0][0]);
+    const uint32_t sc0 = lds_offset(&scales[0][0]) + (wave == 0 ? kThinRows * 4 : 0);
+    auto load = [&](uint32_t s, uint32_t buffer) {
+        // past the row's end (its blocks are no multiple of four): its last bytes again
+        const uint32_t col0 = s * kThinBytes + (l & 31u) * 16, last = stride - 16;
+#pragma unroll
+        for (uint32_t i = 0; i < kWLoads + kXLoads; ++i) {
+            const bool ofw = i < kWLoads;
+            const uint32_t r = (ofw ? (wave * kWLoads + i) : (wave * kXLoads + i - kWLoads)) * 2 + (l >> 5);
+            const uint32_t end = ofw ? wend : xend, col = col0 ^ ((r & 7u) * 16);
+            dma_to_lds(ofw ? w0 : a.x, (r < end ? r : end) * stride + (col < last ? col : last),
+                       lds0 + buffer * kStage + (ofw ? wave * kWLoads + i : kThinRows / 2 + wave * kXLoads + i - kWLoads) * 1024);
+        }
+        dma_word_to_lds(words + uint64_t(s) * 4, word, sc0 + buffer * (kThinRows + 64) * 4);
+    };
+    const uint32_t fr = l & 15u, fg = l >> 4;
+    v4f_t acc[kFM] = {};
+    uint32_t ahead = s0;
+    for (uint32_t d = 0; d + 1 < kDepth && ahead < s1; ++d, ++ahead) load(ahead, (ahead - s0) % kDepth);
+    for (uint32_t s = s0; s < s1; ++s) {
+        // stage s is there (all that is in flight after it: whole stages), and the one
+        // before it is read by all
+        if (ahead - s == kDepth - 1)
+            dma_wait<(kDepth - 2) * kPerStage>();
+        else
+            dma_wait();
+        lds_barrier();
+        if (ahead < s1) {
+            load(ahead, (ahead - s0) % kDepth);
+            ++ahead;
+        }
+        const uint32_t buffer = (s - s0) % kDepth;
+        const uint8_t* t = lds[buffer];
+        const uint32_t sw = scales[buffer][wave * 16 + fr];
+        uint32_t sx[kFM];
+#pragma unroll
+        for (uint32_t i = 0; i < kFM; ++i) sx[i] = scales[buffer][kThinRows + i * 16 + fr];
+        const uint32_t n = blocks - s * kThinBlocks;
+#pragma unroll
+        for (uint32_t d = 0; d < kThinBlocks; ++d) {
+            if (d >= n) break;
+            auto fragment = [&](uint32_t row, uint32_t scale) {
+                const uint8_t* p = t + (row + fr) * kThinBytes + d * 128;
+                Operand<kWide> o;
+                o.set(*reinterpret_cast<const uint4*>(p + ((fg ^ (fr & 7u)) * 16)),
+                      *reinterpret_cast<const uint4*>(p + (((fg + 4) ^ (fr & 7u)) * 16)), scale >> (8 * d));
+                return o;
+            };
+            const Operand<kWide> w = fragment(wave * 16, sw);
+#pragma unroll
+            for (uint32_t i = 0; i < kFM; ++i)
+                acc[i] = mma(w, fragment(kThinRows + i * 16, sx[i]), acc[i]);
+        }
+    }
+    const bool whole = whole_groups<kWide>(a);
 #pragma unroll
     for (uint32_t i = 0; i < kFM; ++i) {
-        const uint64_t r = i * 16 + fr < a.m ? i * 16 + fr : a.m - 1;
-        x[i] = a.x + r * stride + fg * 16;
-        xs[i] = a.xs + r * sstride;
-    }
-    v4f_t acc[kFM] = {};
-    auto run = [&](auto ahead, uint32_t kb) {
-        constexpr uint32_t kN = decltype(ahead)::value;
-        uint4 lo[kN], hi[kN], xlo[kN][kFM], xhi[kN][kFM];
-        uint32_t s[kN], sx[kN][kFM];
-#pragma unroll
-        for (uint32_t d = 0; d < kN; ++d) {
-            const uint64_t b = kb + d;
-            lo[d] = load_stream(w + b * 128);
-            hi[d] = load_stream(w + b * 128 + 64);
-            s[d] = reinterpret_cast<const gu8_t*>(ws)[b];
-#pragma unroll
-            for (uint32_t i = 0; i < kFM; ++i) {
-                xlo[d][i] = load_shared(x[i] + b * 128);
-                xhi[d][i] = load_shared(x[i] + b * 128 + 64);
-                sx[d][i] = reinterpret_cast<const gu8_t*>(xs[i])[b];
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);  // all loads before the first use
-#pragma unroll
-        for (uint32_t d = 0; d < kN; ++d) {
-            Operand<kWide> wo;
-            wo.set(lo[d], hi[d], s[d]);
-#pragma unroll
-            for (uint32_t i = 0; i < kFM; ++i) {
-                Operand<kWide> xo;
-                xo.set(xlo[d][i], xhi[d][i], sx[d][i]);
-                acc[i] = mma(wo, xo, acc[i]);
-            }
-        }
-    };
-    uint32_t kb = b0;
-    for (; kb + kThinAhead <= b1; kb += kThinAhead) run(std::integral_constant<uint32_t, kThinAhead>{}, kb);
-    for (; kb < b1; ++kb) run(std::integral_constant<uint32_t, 1>{}, kb);
-    __shared__ v4f_t part[kWaves][kFM][64];
-#pragma unroll
-    for (uint32_t i = 0; i < kFM; ++i) part[wave][i][l] = acc[i];
-    __syncthreads();
-    for (uint32_t i = wave; i < kFM; i += kWaves) {
-        v4f_t sum = part[0][i][l];
-#pragma unroll
-        for (uint32_t v = 1; v < kWaves; ++v) sum += part[v][i][l];
-        if (i * 16 + fr < a.m) store4<kWide>(a, whole_groups<kWide>(a), i * 16 + fr, n0 + fg * 4, sum);
+        const uint32_t row = i * 16 + fr, col = n0 + wave * 16 + fg * 4;
+        if (row < a.m) store_result<kWide>(a, whole, blockIdx.y, row, col, acc[i]);
     }
 }
 
-uint64_t f8_matmul_workspace(uint64_t, uint64_t, uint64_t, uint32_t) { return 0; }
+// The sums of a product whose k was split, joined in the order of the splits.
+template <bool kWide>
+__global__ void __launch_bounds__(256) f8_join_kernel(F8MatmulArgs a)
+{
+    const uint32_t groups = (a.n + 3) / 4;
+    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= uint64_t(a.m) * groups) return;
+    const uint32_t row = uint32_t(i / groups), col = uint32_t(i % groups) * 4;
+    v4f_t sum = {};
+    for (uint32_t s = 0; s < a.splits; ++s)
+        sum += *reinterpret_cast<const MEZO_GLOBAL v4f_t*>(partial_at(a, s, row, col));
+    store4<kWide>(a, whole_groups<kWide>(a), row, col, sum);
+}
+
+// How a product is cut: the kernel (rows of its tile of activations) and the
+// workgroups that share out k.
+struct Cut {
+    uint32_t tile, splits;
+};
+
+Cut cut_product(uint64_t m, uint64_t n, uint64_t k, bool wide)
+{
+    auto tiles = [&](uint64_t bm, uint64_t bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
+    if (m <= 64) {
+        // a workgroup a CU, each with two stages at least
+        const uint64_t want = 256 / tiles(64, kThinRows), most = f8_blocks(k) / (2 * kThinBlocks);
+        const uint64_t splits = want < most ? want : most;
+        return {64, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits))};
+    }
+    if (!wide && tiles(256, 256) >= 256) return {256, 1};
+    return {128, 1};
+}
+
+uint64_t f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t out_dtype)
+{
+    const Cut c = cut_product(m, n, k, out_dtype == kF32);
+    return c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 16) : 0;
+}
 
 template <bool kWide>
 hipError_t launch_product(F8MatmulArgs a, hipStream_t stream)
 {
+    const Cut cut = cut_product(a.m, a.n, a.k, kWide);
+    a.splits = cut.splits;
     void* params[] = {&a};
-    auto go = [&](const void* f, uint32_t groups, uint32_t lanes) {
-        return hipLaunchKernel(f, dim3(groups), dim3(lanes), params, 0, stream);
+    auto go = [&](const void* f, dim3 groups, uint32_t lanes) {
+        return hipLaunchKernel(f, groups, dim3(lanes), params, 0, stream);
     };
-    if (a.m <= 64) {
-        const uint32_t groups = (a.n + 15) / 16;
-        if (a.m <= 16) return go(reinterpret_cast<const void*>(f8_thin_kernel<1, 4, kWide>), groups, 256);
-        if (a.m <= 32) return go(reinterpret_cast<const void*>(f8_thin_kernel<2, 4, kWide>), groups, 256);
-        return go(reinterpret_cast<const void*>(f8_thin_kernel<4, 4, kWide>), groups, 256);
+    auto tiles = [&](uint32_t bm, uint32_t bn) { return dim3(((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn), a.splits); };
+    hipError_t e;
+    if (cut.tile == 64) {
+        const void* f = a.m <= 16   ? reinterpret_cast<const void*>(f8_thin_kernel<1, kWide>)
+                        : a.m <= 32 ? reinterpret_cast<const void*>(f8_thin_kernel<2, kWide>)
+                                    : reinterpret_cast<const void*>(f8_thin_kernel<4, kWide>);
+        e = go(f, tiles(64, kThinRows), 256);
+    } else if (cut.tile == 128) {
+        e = go(reinterpret_cast<const void*>(f8_matmul_kernel<128, 128, 2, 2, kWide>), tiles(128, 128), 256);
+    } else {
+        if constexpr (kWide)
+            return hipErrorInvalidValue;  // (cut_product never says so)
+        else
+            e = go(reinterpret_cast<const void*>(f8_matmul_kernel<256, 256, 2, 4, false>), tiles(256, 256), 512);
     }
-    auto tiles = [&](uint32_t bm, uint32_t bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
-    if constexpr (!kWide) {
-        if (tiles(256, 256) >= 256)
-            return go(reinterpret_cast<const void*>(f8_matmul_kernel<256, 256, 2, 4, false>), tiles(256, 256), 512);
-    }
-    return go(reinterpret_cast<const void*>(f8_matmul_kernel<128, 128, 2, 2, kWide>), tiles(128, 128), 256);
+    if (e != hipSuccess || a.splits == 1) return e;
+    const uint64_t groups = uint64_t(a.m) * ((a.n + 3) / 4);
+    return go(reinterpret_cast<const void*>(f8_join_kernel<kWide>), dim3(uint32_t((groups + 255) / 256)), 256);
 }
 
 hipError_t launch_f8_matmul(const F8MatmulArgs& args, hipStream_t stream)

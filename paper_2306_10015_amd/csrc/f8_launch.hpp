@@ -28,9 +28,10 @@ struct F8MatmulArgs {
     uint64_t w, ws;  // and of the n weights' rows
     uint64_t c;      // [m, n] of out_dtype
     uint64_t ldc;    // elements from one row of c to the next
-    uint64_t partial;  // fp32 [splits, m, n] of a split product
+    uint64_t partial;  // fp32 [splits, m, n rounded up to 4] of a split product
     uint32_t m, n, k;
     uint32_t out_dtype;
+    uint32_t splits;  // workgroups that share out k (set by the launch)
 };
 
 hipError_t launch_f8_quantize(const F8QuantArgs& args, hipStream_t stream);
