@@ -448,10 +448,12 @@ MEZO_API int mezo_f8_linear(const void* x, uint32_t x_dtype, uint64_t ldx, const
  *
  * heads a multiple of kv_heads, heads <= MEZO_ATTENTION_MAX_HEADS, dim a
  * multiple of 8 up to 128, pointers 16-byte aligned, strides multiples of 16
- * bytes (MEZO_EINVAL); scale and softcap finite, softcap >= 0 (MEZO_ERANGE);
+ * bytes, a token of k and v less than MEZO_ATTENTION_MAX_STRIDE bytes from the
+ * next (MEZO_EINVAL); scale and softcap finite, softcap >= 0 (MEZO_ERANGE);
  * out, lse and the workspace share no memory with each other or with anything
  * read (MEZO_EOVERLAP). n_docs = 0, max_q = 0 and q_tokens = 0 enqueue nothing. */
 #define MEZO_ATTENTION_MAX_HEADS 65536u
+#define MEZO_ATTENTION_MAX_STRIDE (1ull << 26)
 typedef struct {
     const void* q;
     const void* k;

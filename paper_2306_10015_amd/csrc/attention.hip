@@ -29,7 +29,9 @@
 //   rows: each wave has 32 rows of its own and all share stages of 64 keys;
 //   keys: at most 32 rows (single tokens): all waves have the same rows, each takes
 //         every kWaves-th stage of 32 keys through LDS of its own, without barriers,
-//         and they join at the end.
+//         and they join at the end. One buffer for K and one for V: K of the next
+//         stage loads under the softmax and the product with V, V under the scores,
+//         and eight waves a CU keep the memory busy.
 // Where that gives too few workgroups for the GPU, a document's keys are split over
 // several, which leave (m, l, accumulator) and a second kernel joins them.
 //
@@ -37,6 +39,8 @@
 // an infinite or NaN value is not. So a row whose result is not finite is computed
 // once more, from its visible keys alone (careful_row), slowly; finite inputs never
 // get there.
+#include <type_traits>
+
 #include "attention_launch.hpp"
 #include "lds_dma.hpp"
 #include "records.hpp"
@@ -56,20 +60,28 @@ constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLowest = -3.0e38f;  // a reference below every score that counts
 constexpr float kSlack = 8.0f;
 
-// What a padded column of a narrower head is loaded from.
-__device__ const u32x4_t kZeros[1] = {};
-
 struct Document {
     uint64_t q_first, k_first;
     int64_t nq, nk, prefix;
 };
+
+// A value that is the same for all lanes, in scalar registers.
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(uint64_t(x)));
+    const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(uint64_t(x) >> 32));
+    return int64_t(uint64_t(hi) << 32 | lo);
+}
 
 // A document's row of the table, cut to the arrays it points into: no table makes
 // a kernel leave them.
 __device__ __forceinline__ Document read_document(const AttentionArgs& a, uint32_t d)
 {
     const MEZO_GLOBAL int64_t* t = reinterpret_cast<const MEZO_GLOBAL int64_t*>(a.table) + uint64_t(d) * 5;
-    auto within = [](int64_t x, uint64_t top) { return x < 0 ? 0 : (uint64_t(x) > top ? int64_t(top) : x); };
+    auto within = [&](int64_t y, uint64_t top) {
+        const int64_t x = uniform(y);
+        return x < 0 ? 0 : (uint64_t(x) > top ? int64_t(top) : x);
+    };
     Document r;
     r.q_first = uint64_t(within(t[0], a.q_tokens));
     r.nq = within(t[1], a.q_tokens - r.q_first);
@@ -297,7 +309,8 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
     constexpr uint32_t kStage = kKeys ? 32 : 64;  // keys of a stage
     constexpr uint32_t kBytes = kStage * T::kRow;
     constexpr uint32_t kSets = kKeys ? kWaves : 1;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[kSets][2][2][kBytes];
+    constexpr uint32_t kBuffers = kKeys ? 1 : 2;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kSets][kBuffers][2][kBytes];  // [..][0] K, [1] V
 
     const uint32_t l = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t kvh = blockIdx.x % a.kv_heads, doc = blockIdx.x / a.kv_heads;
@@ -314,16 +327,17 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
     auto query = [&](uint64_t r) { return int64_t((r < tile1 ? r : tile1 - 1) / a.group); };
     const int64_t i = query(row);
     const uint32_t h = kvh * a.group + uint32_t((row < tile1 ? row : tile1 - 1) % a.group);
-    const bool mine = row < tile1;
+    const bool valid = row < tile1;
     const int64_t limit = visible(a, d, i) > 0 ? visible(a, d, i) : 0;
     // the wave's rows see all keys below low and none from high
-    const int64_t low0 = visible(a, d, query(first)), low = low0 > 0 ? low0 : 0;
-    const int64_t high0 = visible(a, d, query(first + 31)), high = high0 > 0 ? high0 : 0;
-    const int64_t last0 = visible(a, d, int64_t((tile1 - 1) / a.group)), last = last0 > 0 ? last0 : 0;
+    const int64_t low0 = uniform(visible(a, d, query(first))), low = low0 > 0 ? low0 : 0;
+    const int64_t high0 = uniform(visible(a, d, query(first + 31))), high = high0 > 0 ? high0 : 0;
+    const int64_t last0 = uniform(visible(a, d, query(tile1 - 1))), last = last0 > 0 ? last0 : 0;
 
     // the stages of this split of the workgroup's keys
-    const uint64_t stages = (uint64_t(last) + kStage - 1) / kStage;
-    const uint64_t s0 = stages * blockIdx.z / a.splits, s1 = stages * (blockIdx.z + 1) / a.splits;
+    const uint64_t stages = (uint64_t(last) + kStage - 1) / kStage, per = a.chunk / kStage;
+    const uint64_t s0 = blockIdx.z * per, s1 = a.splits == 1 || s0 + per > stages ? stages : s0 + per;
+    if (a.splits > 1 && s0 >= stages) return;  // the join does not look for these
 
     u32x4_t q[T::kQ];
     {
@@ -337,23 +351,45 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
     const uint64_t kbase = a.k + d.k_first * a.k_token + kvh * a.k_head;
     const uint64_t vbase = a.v + d.k_first * a.v_token + kvh * a.v_head;
     const uint32_t lds0 = lds_offset(&lds[kKeys ? wave : 0][0][0][0]);
-    // stage s into buffer b; keys past the document's end: the last one again
-    auto load = [&](uint64_t s, uint32_t b) {
-        constexpr uint32_t kLoads = kBytes / 1024 / (kKeys ? 1 : kWaves);  // of K, and of V
-        const int64_t left = d.nk - int64_t(s * kStage) - 1;
+    // K or V of stage s into buffer b. A lane's chunk of a row follows the swizzle, whose
+    // pattern returns every 8 rows; columns past a narrower head's end are loaded from its
+    // first chunk: for K the query is 0 there, of V they are not stored. Keys past the
+    // document's end: the last one again.
+    constexpr uint32_t kLoads = kBytes / 1024 / (kKeys ? 1 : kWaves);  // a wave's
+    constexpr uint32_t kPatterns = 8 / T::kLoadRows;
+    static_assert(kLoads % kPatterns == 0, "a wave's first load has the first pattern");
+    auto column = [&](bool isv, uint32_t r) {
+        const uint32_t chunk = (l % T::kChunks) ^ (isv ? T::v_swizzle(r) : T::k_swizzle(r));
+        return chunk * 16 < a.dim * T::kElement ? chunk * 16 : 0;
+    };
+    uint32_t koff[kPatterns], voff[kPatterns];
 #pragma unroll
-        for (uint32_t n = 0; n < 2 * kLoads; ++n) {
-            const bool isv = n >= kLoads;
-            const uint32_t at = (kKeys ? 0 : wave * kLoads) + n % kLoads;
-            const uint32_t r = at * T::kLoadRows + l / T::kChunks;
-            const uint32_t chunk = (l % T::kChunks) ^ (isv ? T::v_swizzle(r) : T::k_swizzle(r));
-            const uint64_t key = s * kStage + (int64_t(r) < left ? r : uint32_t(left));
-            uint64_t addr = isv ? vbase + key * a.v_token : kbase + key * a.k_token;
-            addr += chunk * 16;
-            if (chunk * 16 >= a.dim * T::kElement) addr = reinterpret_cast<uint64_t>(&kZeros[0]);
-            dma_to_lds(addr, lds0 + (2 * b + (isv ? 1 : 0)) * kBytes + at * 1024);
+    for (uint32_t n = 0; n < kPatterns; ++n) {
+        const uint32_t r = l / T::kChunks;
+        koff[n] = r * uint32_t(a.k_token) + column(false, n * T::kLoadRows + r);
+        voff[n] = r * uint32_t(a.v_token) + column(true, n * T::kLoadRows + r);
+    }
+    auto load = [&](auto isv, uint64_t s, uint32_t b) {
+        constexpr bool kV = decltype(isv)::value;
+        const uint64_t token = kV ? a.v_token : a.k_token;
+        const uint64_t base = (kV ? vbase : kbase) + s * kStage * token;
+        const uint32_t to = lds0 + (2 * b + (kV ? 1 : 0)) * kBytes, at0 = kKeys ? 0 : wave * kLoads;
+        if (int64_t((s + 1) * kStage) <= d.nk) {
+            uint64_t at = base + at0 * T::kLoadRows * token;
+#pragma unroll
+            for (uint32_t n = 0; n < kLoads; ++n, at += T::kLoadRows * token)
+                dma_to_lds(at, (kV ? voff : koff)[n % kPatterns], to + (at0 + n) * 1024);
+        } else {
+            const uint32_t left = uint32_t(d.nk - int64_t(s * kStage)) - 1;
+#pragma unroll
+            for (uint32_t n = 0; n < kLoads; ++n) {
+                const uint32_t r = (at0 + n) * T::kLoadRows + l / T::kChunks;
+                dma_to_lds(base, (r < left ? r : left) * uint32_t(token) + column(kV, r), to + (at0 + n) * 1024);
+            }
         }
     };
+    constexpr std::integral_constant<bool, false> kOfK{};
+    constexpr std::integral_constant<bool, true> kOfV{};
 
     const Score sc = score_of(a);
     const float slope = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
@@ -362,17 +398,26 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
     float m = kLowest, sum = 0.0f;
 
     const uint64_t step = kKeys ? kWaves : 1, begin = s0 + (kKeys ? wave : 0);
-    if (begin < s1) load(begin, 0);
+    if (begin < s1) {
+        load(kOfK, begin, 0);
+        load(kOfV, begin, 0);
+    }
     uint32_t b = 0;
-    for (uint64_t s = begin; s < s1; s += step, b ^= 1) {
-        dma_wait();
-        if constexpr (kKeys)
-            lds_wait();  // the other buffer is read
-        else
+    for (uint64_t s = begin; s < s1; s += step, b ^= kBuffers - 1) {
+        const bool more = s + step < s1;
+        if constexpr (kKeys) {
+            dma_wait<kLoads>();  // K of this stage; its V may still come
+        } else {
+            dma_wait();
             lds_barrier();  // everyone's part of this stage is there, and the other buffer is read
-        if (s + step < s1) load(s + step, b ^ 1);
+            if (more) {
+                load(kOfK, s + step, b ^ 1);
+                load(kOfV, s + step, b ^ 1);
+            }
+        }
         const int64_t k0 = int64_t(s * kStage);
-        if (k0 >= high) continue;  // (of the wave)
+        if constexpr (!kKeys)
+            if (k0 >= high) continue;  // (of the wave)
         const uint8_t* kt = lds[kKeys ? wave : 0][b][0];
         const uint8_t* vt = lds[kKeys ? wave : 0][b][1];
         v16f_t x[kStage / 32];
@@ -380,6 +425,10 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
 #pragma unroll
         for (uint32_t t = 0; t < kStage / 32; ++t) {
             x[t] = T::scores(kt, t * 32, q, l);
+            if constexpr (kKeys) {
+                lds_wait();  // K's buffer is read: the next stage's loads under the rest of this one
+                if (more) load(kOfK, s + step, 0);
+            }
 if (sc.capped) {
 #pragma unroll
                 for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped<kF>(sc, x[t][e]);
@@ -422,61 +471,88 @@ if (sc.capped) {
                 x[t][e] = exp2_fast(x[t][e] - m);
                 sum += x[t][e];
             }
+            if constexpr (kKeys) {
+                if (more)
+                    dma_wait<kLoads>();
+                else
+                    dma_wait();
+            }
             T::values(vt, t * 32, x[t], acc, l);
+            if constexpr (kKeys) {
+                lds_wait();
+                if (more) load(kOfV, s + step, 0);
+            }
         }
     }
     sum = sum_halves(sum);
 
-    if constexpr (kKeys) {  // the waves' parts, joined in their order by the first
+    // the tiles of 32 columns that this wave stores: all, or its part of those that the
+    // waves' sums over their keys join in, in the order of the waves
+    constexpr uint32_t kTiles = kD / 32, kMine = !kKeys ? kTiles : (kTiles > kWaves ? kTiles / kWaves : 1);
+    const uint32_t t0 = kKeys ? wave * kMine : 0;
+    v16f_t mine[kMine];
+    __shared__ uint32_t bad_rows;
+    if constexpr (kKeys) {
         __shared__ float stats[kWaves][2][32];
-        float* room = reinterpret_cast<float*>(&lds[0][0][0][0]);  // [kWaves - 1][kD / 32][16][64]
+        float* room = reinterpret_cast<float*>(&lds[0][0][0][0]);  // [kWaves][kTiles][16][64]
+        static_assert(kWaves * kTiles * 16 * 64 * 4 <= sizeof(lds), "the joined tiles fit");
         if (l < 32) {
             stats[wave][0][l] = m;
             stats[wave][1][l] = sum;
         }
+        if (threadIdx.x == 0) bad_rows = 0;
         __syncthreads();
         float now = stats[0][0][l & 31u];
 #pragma unroll
         for (uint32_t w = 1; w < kWaves; ++w) now = fmaxf(now, stats[w][0][l & 31u]);
         const float old = exp2_fast(m - now);
-        if (wave > 0) {
 #pragma unroll
-            for (uint32_t t = 0; t < kD / 32; ++t)
+        for (uint32_t t = 0; t < kTiles; ++t)
 #pragma unroll
-                for (uint32_t e = 0; e < 16; ++e)
-                    room[(((wave - 1) * (kD / 32) + t) * 16 + e) * 64 + l] = acc[t][e] * old;
-        }
-        __syncthreads();
-        if (wave > 0) return;
+            for (uint32_t e = 0; e < 16; ++e) room[((wave * kTiles + t) * 16 + e) * 64 + l] = acc[t][e] * old;
+        m = now;
         sum = 0.0f;
 #pragma unroll
         for (uint32_t w = 0; w < kWaves; ++w) sum += stats[w][1][l & 31u] * exp2_fast(stats[w][0][l & 31u] - now);
+        __syncthreads();
 #pragma unroll
-        for (uint32_t t = 0; t < kD / 32; ++t)
+        for (uint32_t t = 0; t < kMine; ++t)
 #pragma unroll
             for (uint32_t e = 0; e < 16; ++e) {
-                float x = acc[t][e] * old;
+                float x = 0.0f;
+                if (t0 + t < kTiles)
 #pragma unroll
-                for (uint32_t w = 1; w < kWaves; ++w) x += room[(((w - 1) * (kD / 32) + t) * 16 + e) * 64 + l];
-                acc[t][e] = x;
+                    for (uint32_t w = 0; w < kWaves; ++w) x += room[((w * kTiles + t0 + t) * 16 + e) * 64 + l];
+                mine[t][e] = x;
             }
-        m = now;
+    } else {
+#pragma unroll
+        for (uint32_t t = 0; t < kTiles; ++t) mine[t] = acc[t];
     }
 
     const bool split = a.splits > 1;
     const float inv = split ? 1.0f : (sum == 0.0f ? 0.0f : 1.0f / sum);
     bool finite = true;
 #pragma unroll
-    for (uint32_t t = 0; t < kD / 32; ++t)
+    for (uint32_t t = 0; t < kMine; ++t)
 #pragma unroll
         for (uint32_t e = 0; e < 16; ++e) {
-            acc[t][e] *= inv;
-            finite = finite && fabsf(acc[t][e]) < __builtin_inff();
+            mine[t][e] *= inv;
+            finite = finite && fabsf(mine[t][e]) < __builtin_inff();
         }
-    const uint64_t token = d.q_first + uint64_t(i);
-    if (mine) {
+    // rows that are not finite in some column
+    uint64_t bad = __ballot(valid && !finite);
+    uint32_t again = uint32_t(bad | (bad >> 32));
+    if constexpr (kKeys) {
+        if (again && l == 0) atomicOr(&bad_rows, again);
+        __syncthreads();
+        again = bad_rows;
+    }
+    again = __builtin_amdgcn_readfirstlane(again);
+    if (valid && !(again >> (l & 31u) & 1u)) {
+        const uint64_t token = d.q_first + uint64_t(i);
         const PartialRow p = partial_row(a, blockIdx.z, doc, i, h);
-        if (l < 32) {
+        if (l < 32 && t0 == 0) {
             if (split)
                 *reinterpret_cast<MEZO_GLOBAL v2f_t*>(p.stats) = v2f_t{m, sum};
             else
@@ -484,12 +560,12 @@ if (sc.capped) {
         }
         const uint64_t o = a.out + token * a.o_token + h * a.o_head;
 #pragma unroll
-        for (uint32_t t = 0; t < kD / 32; ++t)
+        for (uint32_t t = 0; t < kMine; ++t)
 #pragma unroll
             for (uint32_t e = 0; e < 16; e += 4) {
-                const uint32_t c = t * 32 + 8 * (e >> 2) + 4 * (l >> 5);
+                const uint32_t c = (t0 + t) * 32 + 8 * (e >> 2) + 4 * (l >> 5);
                 if (c >= a.dim) continue;
-                const v4f_t w = {acc[t][e], acc[t][e + 1], acc[t][e + 2], acc[t][e + 3]};
+                const v4f_t w = {mine[t][e], mine[t][e + 1], mine[t][e + 2], mine[t][e + 3]};
                 if (split)
                     *reinterpret_cast<MEZO_GLOBAL v4f_t*>(p.acc + c * 4) = w;
                 else if constexpr (kF)
@@ -498,11 +574,9 @@ if (sc.capped) {
                     *reinterpret_cast<MEZO_GLOBAL v4bf_t*>(o + c * 2) = __builtin_convertvector(w, v4bf_t);
             }
     }
-    // rows that are not finite, once more
-    uint64_t again = __ballot(mine && !finite);
-    again = (again | (again >> 32)) & 0xFFFFFFFFull;
+    if (kKeys && wave > 0) return;
     while (again) {
-        const uint32_t lane = uint32_t(__builtin_ctzll(again));
+        const uint32_t lane = uint32_t(__builtin_ctz(again));
         again &= again - 1;
         const int64_t ri = query(first + lane);
         const uint32_t rh = kvh * a.group + uint32_t((first + lane) % a.group);
@@ -511,7 +585,8 @@ if (sc.capped) {
     }
 }
 
-// The splits of a row, joined in their order: a wave a row.
+// The splits of a row, joined in their order: a wave a row, a lane a split for the
+// statistics and two columns of the accumulator a lane. splits <= 64.
 template <bool kF>
 __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a)
 {
@@ -523,24 +598,46 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a)
     const uint32_t doc = uint32_t(row / a.heads / a.max_q);
     const Document d = read_document(a, doc);
     if (i >= d.nq) return;
-    float m = kLowest;
-    for (uint32_t s = 0; s < a.splits; ++s)
-        m = fmaxf(m, reinterpret_cast<const gfloat_t*>(partial_row(a, s, doc, i, h).stats)[0]);
-    float sum = 0.0f, acc[2] = {0.0f, 0.0f};
-    for (uint32_t s = 0; s < a.splits; ++s) {
-        const PartialRow p = partial_row(a, s, doc, i, h);
-        const float pl = reinterpret_cast<const gfloat_t*>(p.stats)[1];
-        if (pl == 0.0f) continue;  // no key of this row in this split
-        const float w = exp2_fast(reinterpret_cast<const gfloat_t*>(p.stats)[0] - m);
-        sum += pl * w;
-        for (uint32_t c = 0; c < 2; ++c)
-            if (l + 64 * c < a.dim) acc[c] += reinterpret_cast<const gfloat_t*>(p.acc)[l + 64 * c] * w;
+    const int64_t limit0 = visible(a, d, i), limit = limit0 > 0 ? limit0 : 0;
+    const uint32_t most = uint32_t((limit + a.chunk - 1) / a.chunk), splits = most < a.splits ? most : a.splits;
+    float m = kLowest, sum = 0.0f;
+    if (l < splits) {
+        const v2f_t s = *reinterpret_cast<const MEZO_GLOBAL v2f_t*>(partial_row(a, l, doc, i, h).stats);
+        m = s.x;
+        sum = s.y;
+    }
+    float top = m;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+    // (a split without a key of this row has the sum 0 and the accumulator 0)
+    const float weight = exp2_fast(m - top);
+    sum *= weight;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+    float acc[2] = {0.0f, 0.0f};
+    constexpr uint32_t kAhead = 8;  // loads in flight
+    for (uint32_t s0 = 0; s0 < splits; s0 += kAhead) {
+        float part[kAhead][2];
+#pragma unroll
+        for (uint32_t s = 0; s < kAhead; ++s) {
+            const uint64_t at = partial_row(a, s0 + s < splits ? s0 + s : splits - 1, doc, i, h).acc;
+#pragma unroll
+            for (uint32_t c = 0; c < 2; ++c)
+                part[s][c] = l + 64 * c < a.dim ? reinterpret_cast<const gfloat_t*>(at)[l + 64 * c] : 0.0f;
+        }
+#pragma unroll
+        for (uint32_t s = 0; s < kAhead; ++s) {
+            if (s0 + s >= splits) break;
+            const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s0 + s));
+#pragma unroll
+            for (uint32_t c = 0; c < 2; ++c) acc[c] += part[s][c] * w;
+        }
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     const uint64_t token = d.q_first + uint64_t(i);
     for (uint32_t c = 0; c < 2; ++c)
         if (l + 64 * c < a.dim) store_element<kF>(a.out + token * a.o_token + h * a.o_head, l + 64 * c, acc[c] * inv);
-    if (l == 0) store_lse(a, token, h, m, sum);
+    if (l == 0) store_lse(a, token, h, top, sum);
 }
 
 // Few rows: the waves of a workgroup share out the keys.
@@ -552,13 +649,18 @@ AttentionPlan plan_attention(uint32_t docs, uint32_t heads, uint32_t kv_heads, u
     const uint64_t rows = uint64_t(max_q) * (heads / kv_heads);
     const uint64_t tiles = by_keys(rows) ? 1 : (rows + 127) / 128;
     const uint64_t groups = uint64_t(docs) * kv_heads * tiles;
-    const uint64_t want = (1024 + groups - 1) / groups, most = max_k / 256;
-    uint64_t splits = want < most ? want : most;
-    splits = splits < 1 || groups >= 512 ? 1 : (splits > 64 ? 64 : splits);
-    AttentionPlan p;
+    // Split where the groups alone leave CUs idle, into chunks of keys rather than parts
+    // of a document: documents of any length then give equal work.
+    AttentionPlan p = {1, 64, 0};
+    if (groups >= 1024 || max_k <= 256) return p;
+    uint64_t chunk = (max_k * groups / 2048 + 63) / 64 * 64;
+    chunk = chunk < 256 ? 256 : chunk;
+    while ((max_k + chunk - 1) / chunk > 64) chunk += 64;
+    const uint64_t splits = (max_k + chunk - 1) / chunk, kept = splits * docs * max_q * heads;
+    if (splits == 1) return p;
     p.splits = uint32_t(splits);
-    const uint64_t kept = splits * docs * max_q * heads;
-    p.workspace = splits > 1 ? (kept + 1) / 2 * 16 + kept * dim * 4 : 0;
+    p.chunk = uint32_t(chunk);
+    p.workspace = (kept + 1) / 2 * 16 + kept * dim * 4;
     return p;
 }
 

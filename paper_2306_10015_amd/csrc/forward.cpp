@@ -208,6 +208,7 @@ int attention(const mezo_attention_t* p, void* workspace, uint64_t workspace_byt
     const uint64_t strides[8] = {a.q_token, a.q_head, a.k_token, a.k_head, a.v_token, a.v_head, a.o_token, a.o_head};
     for (uint64_t s : strides)
         if (s % align) return MEZO_EINVAL;
+    if (a.k_token * e >= MEZO_ATTENTION_MAX_STRIDE || a.v_token * e >= MEZO_ATTENTION_MAX_STRIDE) return MEZO_EINVAL;
     // the bytes of each array; out's elements must not share memory with each other
     Range r[4];
     for (int i = 0; i < 4; ++i) {
@@ -260,6 +261,7 @@ int attention(const mezo_attention_t* p, void* workspace, uint64_t workspace_byt
     g.max_q = static_cast<uint32_t>(most_q(a));
     g.max_k = static_cast<uint32_t>(most_k(a));
     g.splits = plan.splits;
+    g.chunk = plan.chunk;
     g.causal = a.causal ? 1u : 0u;
     g.dtype = a.dtype;
     g.scale = a.scale;

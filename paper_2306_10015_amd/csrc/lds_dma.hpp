@@ -27,7 +27,7 @@ __device__ __forceinline__ void dma_to_lds(uint64_t addr, uint32_t lds)
                  "s_nop 0\n\t"
                  "global_load_lds_dwordx4 %0, off"
                  :
-                 : "v"(addr), "s"(lds)
+                 : "v"(addr), "s"(__builtin_amdgcn_readfirstlane(lds))
                  : "memory");
 }
 
@@ -38,7 +38,7 @@ __device__ __forceinline__ void dma_to_lds(uint64_t base, uint32_t offset, uint3
                  "s_nop 0\n\t"
                  "global_load_lds_dwordx4 %0, %1"
                  :
-                 : "v"(offset), "s"(base), "s"(lds)
+                 : "v"(offset), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds))
                  : "memory");
 }
 
@@ -49,7 +49,7 @@ __device__ __forceinline__ void dma_word_to_lds(uint64_t base, uint32_t offset, 
                  "s_nop 0\n\t"
                  "global_load_lds_dword %0, %1"
                  :
-                 : "v"(offset), "s"(base), "s"(lds)
+                 : "v"(offset), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds))
                  : "memory");
 }
 
