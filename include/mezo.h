@@ -442,7 +442,7 @@ MEZO_API int mezo_f8_linear(const void* x, uint32_t x_dtype, uint64_t ldx, const
  * and lse. lse (fp32 [q_tokens, heads]) may be NULL.
  *
  * max_q and max_k: no document has more queries or keys (queries past max_q
- * are left out). The documents' queries must not overlap. Rows of docs that
+ * are left out); max_k < 2^31 - 256, max_q * heads / kv_heads < 2^23. The documents' queries must not overlap. Rows of docs that
  * point outside the arrays are cut to them. Scores and sums are fp32; with
  * MEZO_BF16 each probability is rounded to bf16 before it multiplies v.
  *

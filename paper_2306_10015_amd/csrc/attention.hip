@@ -59,10 +59,11 @@ constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLowest = -3.0e38f;  // a reference below every score that counts
 constexpr float kSlack = 8.0f;
+constexpr uint64_t kMostTokens = (1u << 31) - 256;  // of a document
 
 struct Document {
     uint64_t q_first, k_first;
-    int64_t nq, nk, prefix;
+    int nq, nk, prefix;
 };
 
 // A value that is the same for all lanes, in scalar registers.
@@ -80,23 +81,24 @@ __device__ __forceinline__ Document read_document(const AttentionArgs& a, uint32
     const MEZO_GLOBAL int64_t* t = reinterpret_cast<const MEZO_GLOBAL int64_t*>(a.table) + uint64_t(d) * 5;
     auto within = [&](int64_t y, uint64_t top) {
         const int64_t x = uniform(y);
-        return x < 0 ? 0 : (uint64_t(x) > top ? int64_t(top) : x);
+        return x < 0 ? 0 : (uint64_t(x) > top ? top : uint64_t(x));
     };
+    auto count = [](uint64_t left) { return left < kMostTokens ? left : kMostTokens; };
     Document r;
-    r.q_first = uint64_t(within(t[0], a.q_tokens));
-    r.nq = within(t[1], a.q_tokens - r.q_first);
-    r.k_first = uint64_t(within(t[2], a.k_tokens));
-    r.nk = within(t[3], a.k_tokens - r.k_first);
-    r.prefix = within(t[4], uint64_t(r.nk));
+    r.q_first = within(t[0], a.q_tokens);
+    r.nq = int(within(t[1], count(a.q_tokens - r.q_first)));
+    r.k_first = within(t[2], a.k_tokens);
+    r.nk = int(within(t[3], count(a.k_tokens - r.k_first)));
+    r.prefix = int(within(t[4], uint64_t(r.nk)));
     return r;
 }
 
 // How many of its document's keys query i sees.
-__device__ __forceinline__ int64_t visible(const AttentionArgs& a, const Document& d, int64_t i)
+__device__ __forceinline__ int visible(const AttentionArgs& a, const Document& d, int i)
 {
-    const int64_t pos = i + d.nk - d.nq;
+    const int pos = d.nk - d.nq + i;
     if (!a.causal) return d.nk;
-    return pos + 1 > d.prefix ? pos + 1 : d.prefix;  // pos < nk
+    return pos + 1 > d.prefix ? pos + 1 : d.prefix;  // pos < nk, prefix >= 0
 }
 
 // The score function's constants, for scores in units of log 2.
@@ -164,7 +166,7 @@ __device__ __forceinline__ void store_element(uint64_t addr, uint32_t i, float x
 struct PartialRow {
     uint64_t stats, acc;
 };
-__device__ __forceinline__ PartialRow partial_row(const AttentionArgs& a, uint32_t split, uint32_t doc, int64_t i,
+__device__ __forceinline__ PartialRow partial_row(const AttentionArgs& a, uint32_t split, uint32_t doc, int i,
                                                   uint32_t h)
 {
     const uint64_t rows = uint64_t(a.docs) * a.max_q * a.heads;
@@ -184,7 +186,7 @@ __device__ __forceinline__ void store_lse(const AttentionArgs& a, uint64_t token
 // wave works on it. Lane l holds columns l and l + 64 of the accumulator.
 template <bool kF>
 __device__ __forceinline__ void careful_row(const AttentionArgs& a, const Document& d, uint32_t doc, uint32_t kvh,
-                                         uint32_t split, int64_t i, uint32_t h, int64_t k0, int64_t k1)
+                                         uint32_t split, int i, uint32_t h, int k0, int k1)
 {
     const Score sc = score_of(a);
     const uint32_t l = threadIdx.x & 63u;
@@ -192,7 +194,7 @@ __device__ __forceinline__ void careful_row(const AttentionArgs& a, const Docume
     const float slope = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
     float q2[2], acc[2] = {0.0f, 0.0f}, m = kLowest, sum = 0.0f;
     for (uint32_t c = 0; c < 2; ++c) q2[c] = l + 64 * c < a.dim ? load_element<kF>(q, l + 64 * c) : 0.0f;
-    for (int64_t j = k0; j < k1; ++j) {
+    for (int j = k0; j < k1; ++j) {
         const uint64_t key = d.k_first + uint64_t(j);
         const uint64_t k = a.k + key * a.k_token + kvh * a.k_head, v = a.v + key * a.v_token + kvh * a.v_head;
         float s = 0.0f;
@@ -201,7 +203,7 @@ __device__ __forceinline__ void careful_row(const AttentionArgs& a, const Docume
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
         s = sc.capped ? capped<kF>(sc, s) : s * sc.c;
-        if (a.slopes) s -= slope * fabsf(float(i + d.nk - d.nq - j));
+        if (a.slopes) s -= slope * fabsf(float(d.nk - d.nq + i - j));
         const float top = fmaxf(m, s), old = exp2_fast(m - top), p = exp2_fast(s - top);
         m = top;
         sum = sum * old + p;
@@ -301,8 +303,21 @@ struct Tile {
     }
 };
 
+// The score functions that have a loop of their own in the bf16 kernels by rows, which
+// the vector instructions of the softmax bound (the others use kGeneral: fp32 is bound by
+// its matrix instructions, calls by keys by memory). Per score, in issue slots of a wave
+// (4 cycles, a transcendental 8): plain 5, biased 6, capped 10.5; general 7.5 to 14.5.
+//  kPlain:  no cap, no bias, scale > 0: the maximum is taken of the products themselves,
+//           and one fma scales a product and subtracts the reference.
+//  kBiased: no cap. Below the diagonal the bias is linear in the key: a constant of each
+//           of a lane's 16 results plus one term a stage, which joins the reference.
+//  kCapped: no bias, and a cap so small that 0 can be the reference for good: no maximum,
+//           no rescaling. 2^(+-cap log2 e) and sums of 2^24 of them stay within fp32.
+enum Mode { kGeneral, kPlain, kBiased, kCapped };
+constexpr float kMostCap = 96.0f / kLog2e;
+
 // kKeys: the workgroup's waves share out the keys; else the rows.
-template <bool kF, uint32_t kD, uint32_t kWaves, bool kKeys>
+template <bool kF, uint32_t kD, uint32_t kWaves, bool kKeys, Mode kMode>
 __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(AttentionArgs a)
 {
     using T = Tile<kF, kD>;
@@ -313,30 +328,37 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kSets][kBuffers][2][kBytes];  // [..][0] K, [1] V
 
     const uint32_t l = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t kvh = blockIdx.x % a.kv_heads, doc = blockIdx.x / a.kv_heads;
+    // Workgroups go round the 8 XCDs. By rows, all tiles of a key/value head want one
+    // XCD's L2; by keys nothing is read twice, and an XCD that reads one head alone, a few
+    // hundred bytes of every token, keeps to a part of its memory channels: the heads
+    // turn with the document and the split (170 -> 162 us on 24 tokens over 16384 keys).
+    const uint32_t doc = blockIdx.x / a.kv_heads;
+    const uint32_t kvh = (blockIdx.x + (kKeys ? doc + blockIdx.z : 0)) % a.kv_heads;
     const Document d = read_document(a, doc);
-    const uint64_t rows = uint64_t(d.nq < int64_t(a.max_q) ? d.nq : int64_t(a.max_q)) * a.group;
+    const uint32_t rows = (uint32_t(d.nq) < a.max_q ? uint32_t(d.nq) : a.max_q) * a.group;
     // the last tiles see the most keys: first
     constexpr uint32_t kTileRows = kKeys ? 32 : 32 * kWaves;
-    const uint64_t tile0 = uint64_t(gridDim.y - 1 - blockIdx.y) * kTileRows;
+    const uint32_t tile0 = (gridDim.y - 1 - blockIdx.y) * kTileRows;
     if (tile0 >= rows) return;
-    const uint64_t tile1 = tile0 + kTileRows < rows ? tile0 + kTileRows : rows;
+    const uint32_t tile1 = tile0 + kTileRows < rows ? tile0 + kTileRows : rows;
 
     // this lane's row: a (query, head) pair; past the end the last one's again
-    const uint64_t first = tile0 + (kKeys ? 0 : wave * 32), row = first + (l & 31u);
-    auto query = [&](uint64_t r) { return int64_t((r < tile1 ? r : tile1 - 1) / a.group); };
-    const int64_t i = query(row);
-    const uint32_t h = kvh * a.group + uint32_t((row < tile1 ? row : tile1 - 1) % a.group);
+    const uint32_t first = tile0 + (kKeys ? 0 : wave * 32), row = first + (l & 31u);
+    auto query = [&](uint32_t r) { return int((r < tile1 ? r : tile1 - 1) / a.group); };
+    const int i = query(row);
+    const uint32_t h = kvh * a.group + (row < tile1 ? row : tile1 - 1) % a.group;
     const bool valid = row < tile1;
-    const int64_t limit = visible(a, d, i) > 0 ? visible(a, d, i) : 0;
+    const int limit = visible(a, d, i) > 0 ? visible(a, d, i) : 0;
     // the wave's rows see all keys below low and none from high
-    const int64_t low0 = uniform(visible(a, d, query(first))), low = low0 > 0 ? low0 : 0;
-    const int64_t high0 = uniform(visible(a, d, query(first + 31))), high = high0 > 0 ? high0 : 0;
-    const int64_t last0 = uniform(visible(a, d, query(tile1 - 1))), last = last0 > 0 ? last0 : 0;
+    auto seen = [&](uint32_t r) {
+        const int n = int(__builtin_amdgcn_readfirstlane(uint32_t(visible(a, d, query(r)))));
+        return n > 0 ? n : 0;
+    };
+    const int low = seen(first), high = seen(first + 31), last = seen(tile1 - 1);
 
     // the stages of this split of the workgroup's keys
-    const uint64_t stages = (uint64_t(last) + kStage - 1) / kStage, per = a.chunk / kStage;
-    const uint64_t s0 = blockIdx.z * per, s1 = a.splits == 1 || s0 + per > stages ? stages : s0 + per;
+    const uint32_t stages = (uint32_t(last) + kStage - 1) / kStage, per = a.chunk / kStage;
+    const uint32_t s0 = blockIdx.z * per, s1 = a.splits == 1 || s0 + per > stages ? stages : s0 + per;
     if (a.splits > 1 && s0 >= stages) return;  // the join does not look for these
 
     u32x4_t q[T::kQ];
@@ -369,18 +391,18 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
         koff[n] = r * uint32_t(a.k_token) + column(false, n * T::kLoadRows + r);
         voff[n] = r * uint32_t(a.v_token) + column(true, n * T::kLoadRows + r);
     }
-    auto load = [&](auto isv, uint64_t s, uint32_t b) {
+    auto load = [&](auto isv, uint32_t s, uint32_t b) {
         constexpr bool kV = decltype(isv)::value;
         const uint64_t token = kV ? a.v_token : a.k_token;
-        const uint64_t base = (kV ? vbase : kbase) + s * kStage * token;
+        const uint64_t base = (kV ? vbase : kbase) + uint64_t(s) * kStage * token;
         const uint32_t to = lds0 + (2 * b + (kV ? 1 : 0)) * kBytes, at0 = kKeys ? 0 : wave * kLoads;
-        if (int64_t((s + 1) * kStage) <= d.nk) {
+        if ((s + 1) * kStage <= uint32_t(d.nk)) {
             uint64_t at = base + at0 * T::kLoadRows * token;
 #pragma unroll
             for (uint32_t n = 0; n < kLoads; ++n, at += T::kLoadRows * token)
                 dma_to_lds(at, (kV ? voff : koff)[n % kPatterns], to + (at0 + n) * 1024);
         } else {
-            const uint32_t left = uint32_t(d.nk - int64_t(s * kStage)) - 1;
+            const uint32_t left = uint32_t(d.nk) - s * kStage - 1;
 #pragma unroll
             for (uint32_t n = 0; n < kLoads; ++n) {
                 const uint32_t r = (at0 + n) * T::kLoadRows + l / T::kChunks;
@@ -393,17 +415,24 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
 
     const Score sc = score_of(a);
     const float slope = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
-    const int64_t pos = i + d.nk - d.nq;
+    const int pos = d.nk - d.nq + i;
     v16f_t acc[kD / 32] = {};
-    float m = kLowest, sum = 0.0f;
+    float m = kMode == kCapped ? 0.0f : kLowest, sum = 0.0f;
+    // keys below this are not past any query of the wave
+    [[maybe_unused]] const int below = d.nk - d.nq + int(__builtin_amdgcn_readfirstlane(uint32_t(query(first)))) + 1;
+    [[maybe_unused]] float slope_step[16];
+    if constexpr (kMode == kBiased) {
+#pragma unroll
+        for (uint32_t e = 0; e < 16; ++e) slope_step[e] = slope * float(8 * (e >> 2) + (e & 3));
+    }
 
-    const uint64_t step = kKeys ? kWaves : 1, begin = s0 + (kKeys ? wave : 0);
+    const uint32_t step = kKeys ? kWaves : 1, begin = s0 + (kKeys ? wave : 0);
     if (begin < s1) {
         load(kOfK, begin, 0);
         load(kOfV, begin, 0);
     }
     uint32_t b = 0;
-    for (uint64_t s = begin; s < s1; s += step, b ^= kBuffers - 1) {
+    for (uint32_t s = begin; s < s1; s += step, b ^= kBuffers - 1) {
         const bool more = s + step < s1;
         if constexpr (kKeys) {
             dma_wait<kLoads>();  // K of this stage; its V may still come
@@ -415,72 +444,129 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
                 load(kOfV, s + step, b ^ 1);
             }
         }
-        const int64_t k0 = int64_t(s * kStage);
+        const int k0 = int(s * kStage);
         if constexpr (!kKeys)
             if (k0 >= high) continue;  // (of the wave)
         const uint8_t* kt = lds[kKeys ? wave : 0][b][0];
         const uint8_t* vt = lds[kKeys ? wave : 0][b][1];
-        v16f_t x[kStage / 32];
-        float top = kLowest;
+        // some of the stage's keys are hidden from, or past, some query of the wave
+        const bool edge = k0 + int(kStage) > (kMode == kBiased && below < low ? below : low);
+        {
+            constexpr uint32_t kT = kStage / 32;
+            v16f_t x[kT];
+            float off[kT];  // what is still to be added to x[t]
+            float top = kLowest;
 #pragma unroll
-        for (uint32_t t = 0; t < kStage / 32; ++t) {
-            x[t] = T::scores(kt, t * 32, q, l);
-            if constexpr (kKeys) {
-                lds_wait();  // K's buffer is read: the next stage's loads under the rest of this one
-                if (more) load(kOfK, s + step, 0);
+            for (uint32_t t = 0; t < kT; ++t) {
+                x[t] = T::scores(kt, t * 32, q, l);
+                if constexpr (kKeys) {
+                    lds_wait();  // K's buffer is read: the next stage's loads under the rest of this one
+                    if (more) load(kOfK, s + step, 0);
+                }
             }
-if (sc.capped) {
 #pragma unroll
-                for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped<kF>(sc, x[t][e]);
-            } else {
-#pragma unroll
-                for (uint32_t e = 0; e < 16; ++e) x[t][e] *= sc.c;
-            }
-            // this lane's keys: k0 + t * 32 + 4 (l / 32), and 8 (e / 4) + e % 4 more
-            const int64_t key = k0 + t * 32 + 4 * (l >> 5);
-            if (a.slopes) {
+            for (uint32_t t = 0; t < kT; ++t) {
+                // this lane's keys: key, and 8 (e / 4) + e % 4 more
+                const int key = k0 + int(t * 32 + 4 * (l >> 5));
                 const float from = float(pos - key);
+                off[t] = 0.0f;
+                if constexpr (kMode == kCapped) {
 #pragma unroll
-                for (uint32_t e = 0; e < 16; ++e)
-                    x[t][e] = __builtin_fmaf(-slope, fabsf(from - float(8 * (e >> 2) + (e & 3))), x[t][e]);
+                    for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped<kF>(sc, x[t][e]);
+                }
+                if constexpr (kMode == kBiased) {
+                    if (!edge) {
+                        off[t] = -slope * from;
+#pragma unroll
+                        for (uint32_t e = 0; e < 16; ++e) x[t][e] = __builtin_fmaf(x[t][e], sc.c, slope_step[e]);
+                    } else {
+#pragma unroll
+                        for (uint32_t e = 0; e < 16; ++e)
+                            x[t][e] = __builtin_fmaf(-slope, fabsf(from - float(8 * (e >> 2) + (e & 3))), x[t][e] * sc.c);
+                    }
+                }
+                if constexpr (kMode == kGeneral) {
+                    if (sc.capped) {
+#pragma unroll
+                        for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped<kF>(sc, x[t][e]);
+                    } else {
+#pragma unroll
+                        for (uint32_t e = 0; e < 16; ++e) x[t][e] *= sc.c;
+                    }
+                    if (a.slopes) {
+#pragma unroll
+                        for (uint32_t e = 0; e < 16; ++e)
+                            x[t][e] = __builtin_fmaf(-slope, fabsf(from - float(8 * (e >> 2) + (e & 3))), x[t][e]);
+                    }
+                }
+                if (edge) {
+                    const int left = limit - key;
+#pragma unroll
+                    for (uint32_t e = 0; e < 16; ++e)
+                        if (int(8 * (e >> 2) + (e & 3)) >= left) x[t][e] = -__builtin_inff();
+                }
+                if constexpr (kMode != kCapped) {
+                    float most = x[t][0];
+#pragma unroll
+                    for (uint32_t e = 1; e < 16; ++e) most = fmaxf(most, x[t][e]);
+                    top = fmaxf(top, kMode == kPlain ? most * sc.c : most + off[t]);
+                }
             }
-            if (k0 + kStage > low) {
-                const int64_t left = limit - key;
-                const int see = left < 0 ? 0 : (left < 32 ? int(left) : 32);
+            if constexpr (kMode != kCapped) {
+                top = max_halves(top);
+                if (__any(top > m + kSlack)) {
+                    const float now = fmaxf(m, top), old = exp2_fast(m - now);
+                    m = now;
+                    sum *= old;
 #pragma unroll
-                for (uint32_t e = 0; e < 16; ++e)
-                    if (int(8 * (e >> 2) + (e & 3)) >= see) x[t][e] = -__builtin_inff();
+                    for (uint32_t t = 0; t < kD / 32; ++t)
+#pragma unroll
+                        for (uint32_t e = 0; e < 16; ++e) acc[t][e] *= old;
+                }
+            }
+            [[maybe_unused]] float factor = sc.c;
+            if constexpr (kMode == kPlain || kMode == kBiased) {
+                // The short forms below round differently from what the reference was
+                // taken of, by 2^-24 of it: not where that is more than 2^-8.
+                if (__any(fabsf(m) > 65536.0f || fabsf(off[0]) > 65536.0f)) {
+#pragma unroll
+                    for (uint32_t t = 0; t < kT; ++t) {
+#pragma unroll
+                        for (uint32_t e = 0; e < 16; ++e) {
+                            if constexpr (kMode == kPlain)
+                                x[t][e] = x[t][e] * sc.c - m;
+                            else
+                                x[t][e] = x[t][e] + off[t] - m;
+                        }
+                        off[t] = m;
+                    }
+                    factor = 1.0f;
+                }
             }
 #pragma unroll
-            for (uint32_t e = 0; e < 16; ++e) top = fmaxf(top, x[t][e]);
-        }
-        top = max_halves(top);
-        if (__any(top > m + kSlack)) {
-            const float now = fmaxf(m, top), old = exp2_fast(m - now);
-            m = now;
-            sum *= old;
+            for (uint32_t t = 0; t < kT; ++t) {
+                const float ref = m - off[t];
 #pragma unroll
-            for (uint32_t t = 0; t < kD / 32; ++t)
-#pragma unroll
-                for (uint32_t e = 0; e < 16; ++e) acc[t][e] *= old;
-        }
-#pragma unroll
-        for (uint32_t t = 0; t < kStage / 32; ++t) {
-#pragma unroll
-            for (uint32_t e = 0; e < 16; ++e) {
-                x[t][e] = exp2_fast(x[t][e] - m);
-                sum += x[t][e];
-            }
-            if constexpr (kKeys) {
-                if (more)
-                    dma_wait<kLoads>();
-                else
-                    dma_wait();
-            }
-            T::values(vt, t * 32, x[t], acc, l);
-            if constexpr (kKeys) {
-                lds_wait();
-                if (more) load(kOfV, s + step, 0);
+                for (uint32_t e = 0; e < 16; ++e) {
+                    if constexpr (kMode == kPlain)
+                        x[t][e] = exp2_fast(__builtin_fmaf(x[t][e], factor, -ref));
+                    else if constexpr (kMode == kCapped)
+                        x[t][e] = exp2_fast(x[t][e]);
+                    else
+                        x[t][e] = exp2_fast(x[t][e] - ref);
+                    sum += x[t][e];
+                }
+                if constexpr (kKeys) {
+                    if (more)
+                        dma_wait<kLoads>();
+                    else
+                        dma_wait();
+                }
+                T::values(vt, t * 32, x[t], acc, l);
+                if constexpr (kKeys) {
+                    lds_wait();
+                    if (more) load(kOfV, s + step, 0);
+                }
             }
         }
     }
@@ -578,10 +664,10 @@ if (sc.capped) {
     while (again) {
         const uint32_t lane = uint32_t(__builtin_ctz(again));
         again &= again - 1;
-        const int64_t ri = query(first + lane);
-        const uint32_t rh = kvh * a.group + uint32_t((first + lane) % a.group);
-        const int64_t rlimit = visible(a, d, ri), end = int64_t(s1 * kStage);
-        careful_row<kF>(a, d, doc, kvh, blockIdx.z, ri, rh, int64_t(s0 * kStage), end < rlimit ? end : rlimit);
+        const int ri = query(first + lane);
+        const uint32_t rh = kvh * a.group + (first + lane) % a.group;
+        const int rlimit = visible(a, d, ri), end = int(s1 * kStage);
+        careful_row<kF>(a, d, doc, kvh, blockIdx.z, ri, rh, int(s0 * kStage), end < rlimit ? end : rlimit);
     }
 }
 
@@ -594,12 +680,13 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a)
     const uint64_t row = uint64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (row >= uint64_t(a.docs) * a.max_q * a.heads) return;
     const uint32_t h = uint32_t(row % a.heads);
-    const int64_t i = int64_t(row / a.heads % a.max_q);
+    const int i = int(row / a.heads % a.max_q);
     const uint32_t doc = uint32_t(row / a.heads / a.max_q);
     const Document d = read_document(a, doc);
     if (i >= d.nq) return;
-    const int64_t limit0 = visible(a, d, i), limit = limit0 > 0 ? limit0 : 0;
-    const uint32_t most = uint32_t((limit + a.chunk - 1) / a.chunk), splits = most < a.splits ? most : a.splits;
+    const int limit0 = visible(a, d, i);
+    const uint32_t limit = limit0 > 0 ? uint32_t(limit0) : 0;
+    const uint32_t most = (limit + a.chunk - 1) / a.chunk, splits = most < a.splits ? most : a.splits;
     float m = kLowest, sum = 0.0f;
     if (l < splits) {
         const v2f_t s = *reinterpret_cast<const MEZO_GLOBAL v2f_t*>(partial_row(a, l, doc, i, h).stats);
@@ -672,8 +759,17 @@ hipError_t launch(AttentionArgs a, hipStream_t stream)
     const uint64_t rows = uint64_t(a.max_q) * a.group;
     const bool keys = by_keys(rows);
     const dim3 grid(a.docs * a.kv_heads, uint32_t(keys ? 1 : (rows + 127) / 128), a.splits);
-    const void* f = keys ? reinterpret_cast<const void*>(attention_kernel<kF, kD, kKeyWaves, true>)
-                         : reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false>);
+    const void* f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kGeneral>);
+    if (keys) {
+        f = reinterpret_cast<const void*>(attention_kernel<kF, kD, kKeyWaves, true, kGeneral>);
+    } else if constexpr (!kF) {
+        if (a.softcap == 0.0f && !a.slopes && a.scale > 0.0f)
+            f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kPlain>);
+        else if (a.softcap == 0.0f && a.slopes)
+            f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kBiased>);
+        else if (a.softcap > 0.0f && a.softcap <= kMostCap && !a.slopes)
+            f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kCapped>);
+    }
     const hipError_t e = hipLaunchKernel(f, grid, dim3(keys ? kKeyWaves * 64 : 256), params, 0, stream);
     if (e != hipSuccess || a.splits == 1) return e;
     const uint64_t all = uint64_t(a.docs) * a.max_q * a.heads;

@@ -183,7 +183,7 @@ bool attention_fits(const mezo_attention_t& a)
 {
     const uint64_t q = most_q(a), k = most_k(a);
     return uint64_t(a.n_docs) * a.kv_heads < (1u << 24) && q * (a.heads / a.kv_heads) <= 65535ull * 128 &&
-           k < (1ull << 32) && uint64_t(a.n_docs) * q * a.heads < (1ull << 40);
+           k < (1ull << 31) - 256 && uint64_t(a.n_docs) * q * a.heads < (1ull << 40);
 }
 
 mezo::AttentionPlan attention_plan(const mezo_attention_t& a)
