@@ -234,19 +234,24 @@ struct Tile {
     static constexpr uint32_t kLoadRows = 1024 / kRow;  // rows of one load of a wave
     static constexpr uint32_t kQ = kD * kElement / 2 / 16;  // 16-byte operands of a lane's half row
 
-    // The order of a row's chunks in LDS, such that the lanes that read together
-    // read different banks: K 8 rows at one chunk, V (bf16) 4 rows at a pair of chunks.
-    static __device__ __forceinline__ uint32_t k_swizzle(uint32_t row) { return row & 7u; }
+    // The order of a row's chunks in LDS, such that the lanes that read together read
+    // different banks (64 of 4 bytes): of K 16 rows at one chunk, of V (bf16) 4 rows at 64
+    // bytes. Both patterns return every kPeriod rows.
+    static constexpr uint32_t kPeriod = 16;
+    static __device__ __forceinline__ uint32_t k_swizzle(uint32_t row)
+    {
+        return kChunks >= 16 ? row & 15u : (row >> 1) & 7u;
+    }
     static __device__ __forceinline__ uint32_t v_swizzle(uint32_t row)
     {
         if constexpr (kF) return 0;
-        return (row & (kChunks >= 16 ? 7u : 3u)) << 1;
+        return kChunks >= 16 ? (row & 3u) << 2 : (row & 2u) << 1;
     }
 
-    // scores += 32 keys (from row of K's stage) x 32 queries
-    static __device__ __forceinline__ v16f_t scores(const uint8_t* k, uint32_t row, const u32x4_t (&q)[kQ], uint32_t l)
+    // s + 32 keys (from row of K's stage) x 32 queries
+    static __device__ __forceinline__ v16f_t scores(const uint8_t* k, uint32_t row, const u32x4_t (&q)[kQ], uint32_t l,
+                                                    v16f_t s)
     {
-        v16f_t s = {};
         const uint32_t r = row + (l & 31u);
 #pragma unroll
         for (uint32_t c = 0; c < kQ; ++c) {
@@ -306,11 +311,12 @@ struct Tile {
 // The score functions that have a loop of their own in the bf16 kernels by rows, which
 // the vector instructions of the softmax bound (the others use kGeneral: fp32 is bound by
 // its matrix instructions, calls by keys by memory). Per score, in issue slots of a wave
-// (4 cycles, a transcendental 8): plain 5, biased 6, capped 10.5; general 7.5 to 14.5.
+// (4 cycles, a transcendental 8): plain and biased 5.5, capped 11; general 8 to 15.
 //  kPlain:  no cap, no bias, scale > 0: the maximum is taken of the products themselves,
 //           and one fma scales a product and subtracts the reference.
-//  kBiased: no cap. Below the diagonal the bias is linear in the key: a constant of each
-//           of a lane's 16 results plus one term a stage, which joins the reference.
+//  kBiased: no cap, scale > 0. Away from the diagonal the bias is linear in the key: a
+//           constant of each of a lane's 16 results, which the products are added to
+//           instead of to zero, and one term a stage, which joins the reference.
 //  kCapped: no bias, and a cap so small that 0 can be the reference for good: no maximum,
 //           no rescaling. 2^(+-cap log2 e) and sums of 2^24 of them stay within fp32.
 enum Mode { kGeneral, kPlain, kBiased, kCapped };
@@ -373,12 +379,11 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
     const uint64_t kbase = a.k + d.k_first * a.k_token + kvh * a.k_head;
     const uint64_t vbase = a.v + d.k_first * a.v_token + kvh * a.v_head;
     const uint32_t lds0 = lds_offset(&lds[kKeys ? wave : 0][0][0][0]);
-    // K or V of stage s into buffer b. A lane's chunk of a row follows the swizzle, whose
-    // pattern returns every 8 rows; columns past a narrower head's end are loaded from its
+    // K or V of stage s into buffer b. A lane's chunk of a row follows the swizzle; columns past a narrower head's end are loaded from its
     // first chunk: for K the query is 0 there, of V they are not stored. Keys past the
     // document's end: the last one again.
     constexpr uint32_t kLoads = kBytes / 1024 / (kKeys ? 1 : kWaves);  // a wave's
-    constexpr uint32_t kPatterns = 8 / T::kLoadRows;
+    constexpr uint32_t kPatterns = T::kPeriod / T::kLoadRows;
     static_assert(kLoads % kPatterns == 0, "a wave's first load has the first pattern");
     auto column = [&](bool isv, uint32_t r) {
         const uint32_t chunk = (l % T::kChunks) ^ (isv ? T::v_swizzle(r) : T::k_swizzle(r));
@@ -418,12 +423,15 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
     const int pos = d.nk - d.nq + i;
     v16f_t acc[kD / 32] = {};
     float m = kMode == kCapped ? 0.0f : kLowest, sum = 0.0f;
-    // keys below this are not past any query of the wave
-    [[maybe_unused]] const int below = d.nk - d.nq + int(__builtin_amdgcn_readfirstlane(uint32_t(query(first)))) + 1;
-    [[maybe_unused]] float slope_step[16];
+    // the positions of the wave's first and last query
+    [[maybe_unused]] const int pos0 = d.nk - d.nq + int(__builtin_amdgcn_readfirstlane(uint32_t(query(first))));
+    [[maybe_unused]] const int pos1 = d.nk - d.nq + int(__builtin_amdgcn_readfirstlane(uint32_t(query(first + 31))));
+    // the bias of a lane's results before the diagonal, but for a term a stage, as a product
+    v16f_t bias = {};
+    const float per_key = kMode == kBiased ? slope / sc.c : 0.0f;
     if constexpr (kMode == kBiased) {
 #pragma unroll
-        for (uint32_t e = 0; e < 16; ++e) slope_step[e] = slope * float(8 * (e >> 2) + (e & 3));
+        for (uint32_t e = 0; e < 16; ++e) bias[e] = per_key * float(8 * (e >> 2) + (e & 3));
     }
 
     const uint32_t step = kKeys ? kWaves : 1, begin = s0 + (kKeys ? wave : 0);
@@ -449,8 +457,7 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
             if (k0 >= high) continue;  // (of the wave)
         const uint8_t* kt = lds[kKeys ? wave : 0][b][0];
         const uint8_t* vt = lds[kKeys ? wave : 0][b][1];
-        // some of the stage's keys are hidden from, or past, some query of the wave
-        const bool edge = k0 + int(kStage) > (kMode == kBiased && below < low ? below : low);
+        const bool edge = k0 + int(kStage) > low;  // some query of the wave does not see them all
         {
             constexpr uint32_t kT = kStage / 32;
             v16f_t x[kT];
@@ -458,7 +465,7 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
             float top = kLowest;
 #pragma unroll
             for (uint32_t t = 0; t < kT; ++t) {
-                x[t] = T::scores(kt, t * 32, q, l);
+                x[t] = T::scores(kt, t * 32, q, l, bias);
                 if constexpr (kKeys) {
                     lds_wait();  // K's buffer is read: the next stage's loads under the rest of this one
                     if (more) load(kOfK, s + step, 0);
@@ -475,14 +482,17 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
                     for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped<kF>(sc, x[t][e]);
                 }
                 if constexpr (kMode == kBiased) {
-                    if (!edge) {
-                        off[t] = -slope * from;
+                    off[t] = -slope * from;
+                    if (k0 > pos1) {  // all keys past all queries
+                        off[t] = slope * from;
 #pragma unroll
-                        for (uint32_t e = 0; e < 16; ++e) x[t][e] = __builtin_fmaf(x[t][e], sc.c, slope_step[e]);
-                    } else {
+                        for (uint32_t e = 0; e < 16; ++e) x[t][e] = __builtin_fmaf(-2.0f, bias[e], x[t][e]);
+                    } else if (k0 + int(kStage) > pos0 + 1) {  // some past some
+                        off[t] = 0.0f;
 #pragma unroll
                         for (uint32_t e = 0; e < 16; ++e)
-                            x[t][e] = __builtin_fmaf(-slope, fabsf(from - float(8 * (e >> 2) + (e & 3))), x[t][e] * sc.c);
+                            x[t][e] = __builtin_fmaf(-per_key, fabsf(from - float(8 * (e >> 2) + (e & 3))),
+                                                     x[t][e] - bias[e]);
                     }
                 }
                 if constexpr (kMode == kGeneral) {
@@ -509,7 +519,7 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
                     float most = x[t][0];
 #pragma unroll
                     for (uint32_t e = 1; e < 16; ++e) most = fmaxf(most, x[t][e]);
-                    top = fmaxf(top, kMode == kPlain ? most * sc.c : most + off[t]);
+                    top = fmaxf(top, kMode == kGeneral ? most : most * sc.c + off[t]);
                 }
             }
             if constexpr (kMode != kCapped) {
@@ -526,17 +536,14 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
             }
             [[maybe_unused]] float factor = sc.c;
             if constexpr (kMode == kPlain || kMode == kBiased) {
-                // The short forms below round differently from what the reference was
+                // The short form below rounds differently from what the reference was
                 // taken of, by 2^-24 of it: not where that is more than 2^-8.
                 if (__any(fabsf(m) > 65536.0f || fabsf(off[0]) > 65536.0f)) {
 #pragma unroll
                     for (uint32_t t = 0; t < kT; ++t) {
 #pragma unroll
                         for (uint32_t e = 0; e < 16; ++e) {
-                            if constexpr (kMode == kPlain)
-                                x[t][e] = x[t][e] * sc.c - m;
-                            else
-                                x[t][e] = x[t][e] + off[t] - m;
+                            x[t][e] = x[t][e] * sc.c + off[t] - m;
                         }
                         off[t] = m;
                     }
@@ -548,7 +555,7 @@ __global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(Atte
                 const float ref = m - off[t];
 #pragma unroll
                 for (uint32_t e = 0; e < 16; ++e) {
-                    if constexpr (kMode == kPlain)
+                    if constexpr (kMode == kPlain || kMode == kBiased)
                         x[t][e] = exp2_fast(__builtin_fmaf(x[t][e], factor, -ref));
                     else if constexpr (kMode == kCapped)
                         x[t][e] = exp2_fast(x[t][e]);
@@ -765,7 +772,7 @@ hipError_t launch(AttentionArgs a, hipStream_t stream)
     } else if constexpr (!kF) {
         if (a.softcap == 0.0f && !a.slopes && a.scale > 0.0f)
             f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kPlain>);
-        else if (a.softcap == 0.0f && a.slopes)
+        else if (a.softcap == 0.0f && a.scale > 0.0f)
             f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kBiased>);
         else if (a.softcap > 0.0f && a.softcap <= kMostCap && !a.slopes)
             f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kCapped>);

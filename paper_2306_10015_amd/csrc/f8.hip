@@ -268,8 +268,8 @@ __device__ __forceinline__ void store_result(const F8MatmulArgs& a, bool whole, 
 //
 // A stage is one block of 128 of every row of the tile, loaded straight into LDS;
 // two stages, one computed on while the other loads. A row's eight 16-byte chunks
-// are stored at chunk ^ (row & 7): the 16 rows of a fragment then spread over all
-// banks. The scales of four blocks are a word of a row; they come the same way,
+// are stored at chunk ^ ((row / 2) & 7): the 16 rows of a fragment then spread over
+// all 64 banks. The scales of four blocks are a word of a row; they come the same way,
 // every fourth stage.
 template <uint32_t kBM, uint32_t kBN, uint32_t kWM, uint32_t kWN, bool kWide>
 __global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a)
@@ -304,7 +304,9 @@ __global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a
     for (uint32_t i = 0; i < kLoads; ++i) {
         const uint32_t r = (wave * kLoads + i) * 8 + (l >> 3) - (ofx ? 0 : kBM);
         const uint32_t end = (ofx ? a.m - m0 : a.n - n0) - 1;
-        src[i] = (r < end ? r : end) * stride + ((l & 7u) ^ (l >> 3)) * 16;
+        // (row / 2) & 7 of row 8 (wave kLoads + i) + l / 8 of the tile
+        const uint32_t swizzle = (4 * (wave * kLoads + i) + (l >> 4)) & 7u;
+        src[i] = (r < end ? r : end) * stride + ((l & 7u) ^ swizzle) * 16;
     }
     uint32_t word;
     {
@@ -348,8 +350,8 @@ __global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a
         auto fragment = [&](uint32_t row) {
             const uint32_t r = row + fr;
             Fragment f;
-            f.lo = *reinterpret_cast<const uint4*>(t + r * 128 + ((fg ^ (fr & 7u)) * 16));
-            f.hi = *reinterpret_cast<const uint4*>(t + r * 128 + (((fg + 4) ^ (fr & 7u)) * 16));
+            f.lo = *reinterpret_cast<const uint4*>(t + r * 128 + ((fg ^ (fr >> 1)) * 16));
+            f.hi = *reinterpret_cast<const uint4*>(t + r * 128 + (((fg + 4) ^ (fr >> 1)) * 16));
             return f;
         };
         Operand<kWide> w[kFN];
@@ -418,7 +420,7 @@ __global__ void __launch_bounds__(256) f8_thin_kernel(F8MatmulArgs a)
         for (uint32_t i = 0; i < kWLoads + kXLoads; ++i) {
             const bool ofw = i < kWLoads;
             const uint32_t r = (ofw ? (wave * kWLoads + i) : (wave * kXLoads + i - kWLoads)) * 2 + (l >> 5);
-            const uint32_t end = ofw ? wend : xend, col = col0 ^ ((r & 7u) * 16);
+            const uint32_t end = ofw ? wend : xend, col = col0 ^ ((r & 15u) * 16);
             dma_to_lds(ofw ? w0 : a.x, (r < end ? r : end) * stride + (col < last ? col : last),
                        lds0 + buffer * kStage + (ofw ? wave * kWLoads + i : kThinRows / 2 + wave * kXLoads + i - kWLoads) * 1024);
         }
@@ -451,10 +453,10 @@ __global__ void __launch_bounds__(256) f8_thin_kernel(F8MatmulArgs a)
         for (uint32_t d = 0; d < kThinBlocks; ++d) {
             if (d >= n) break;
             auto fragment = [&](uint32_t row, uint32_t scale) {
-                const uint8_t* p = t + (row + fr) * kThinBytes + d * 128;
+                const uint8_t* p = t + (row + fr) * kThinBytes;  // chunks at chunk ^ (row & 15)
                 Operand<kWide> o;
-                o.set(*reinterpret_cast<const uint4*>(p + ((fg ^ (fr & 7u)) * 16)),
-                      *reinterpret_cast<const uint4*>(p + (((fg + 4) ^ (fr & 7u)) * 16)), scale >> (8 * d));
+                o.set(*reinterpret_cast<const uint4*>(p + (((8 * d + fg) ^ fr) * 16)),
+                      *reinterpret_cast<const uint4*>(p + (((8 * d + fg + 4) ^ fr) * 16)), scale >> (8 * d));
                 return o;
             };
             const Operand<kWide> w = fragment(wave * 16, sw);
