@@ -236,11 +236,12 @@ struct Tile {
 
     // The order of a row's chunks in LDS, such that the lanes that read together read
     // different banks (64 of 4 bytes): of K 16 rows at one chunk, of V (bf16) 4 rows at 64
-    // bytes. Both patterns return every kPeriod rows.
-    static constexpr uint32_t kPeriod = 16;
+    // bytes. Both patterns return every kPeriod rows (for 512-byte rows, where the matrix
+    // instructions take far longer than the reads, as often as a wave's loads do).
+    static constexpr uint32_t kPeriod = kRow == 512 ? 8 : 16;
     static __device__ __forceinline__ uint32_t k_swizzle(uint32_t row)
     {
-        return kChunks >= 16 ? row & 15u : (row >> 1) & 7u;
+        return kChunks >= 16 ? row & (kPeriod - 1) : (row >> 1) & 7u;
     }
     static __device__ __forceinline__ uint32_t v_swizzle(uint32_t row)
     {
@@ -324,10 +325,10 @@ constexpr float kMostCap = 96.0f / kLog2e;
 
 // kKeys: the workgroup's waves share out the keys; else the rows.
 template <bool kF, uint32_t kD, uint32_t kWaves, bool kKeys, Mode kMode>
-__global__ void __launch_bounds__(kWaves * 64, kF ? 1 : 2) attention_kernel(AttentionArgs a)
+__global__ void __launch_bounds__(kWaves * 64, kKeys && kF && kD > 64 ? 1 : 2) attention_kernel(AttentionArgs a)
 {
     using T = Tile<kF, kD>;
-    constexpr uint32_t kStage = kKeys ? 32 : 64;  // keys of a stage
+    constexpr uint32_t kStage = kKeys || (kF && kD > 64) ? 32 : 64;  // keys of a stage
     constexpr uint32_t kBytes = kStage * T::kRow;
     constexpr uint32_t kSets = kKeys ? kWaves : 1;
     constexpr uint32_t kBuffers = kKeys ? 1 : 2;
