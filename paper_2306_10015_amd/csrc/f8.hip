@@ -15,6 +15,8 @@
 //  fp32: the codes are widened to bf16 in registers, exactly, their scales
 //        applied, and v_mfma_f32_16x16x32_bf16 sums the exact products in fp32
 //        (error 1e-8 to 2e-7, as a chain of fp32 additions), at half the rate.
+#include <type_traits>
+
 #include "f8_launch.hpp"
 #include "lds_dma.hpp"
 #include "records.hpp"
@@ -277,7 +279,7 @@ __global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a
     constexpr uint32_t kWaves = kWM * kWN, kRows = kBM + kBN;
     constexpr uint32_t kFM = kBM / kWM / 16, kFN = kBN / kWN / 16;  // fragments of a wave
     constexpr uint32_t kLoads = kRows / 8 / kWaves;                 // 8 rows a load
-    static_assert(kRows == kWaves * 64, "a word of scales a lane");
+    static_assert(kRows % (8 * kWaves) == 0 && kRows <= kWaves * 64 && kBM % 64 == 0 && kBN % 64 == 0);
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2][kRows * 128];
     __shared__ __attribute__((aligned(256))) uint32_t scales[2][kRows];
 
@@ -291,34 +293,38 @@ __global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a
     const uint32_t in = id - band * 8 * tn;
     const uint32_t m0 = (band * 8 + in % height) * kBM, n0 = in / height * kBN;
 
-    const uint32_t blocks = uint32_t(f8_blocks(a.k));
+    // this workgroup's blocks of k: whole words of scales
+    const uint32_t all = uint32_t(f8_blocks(a.k)), words4 = (all + 3) / 4;
+    const uint32_t begin = words4 * blockIdx.y / a.splits * 4, end4 = words4 * (blockIdx.y + 1) / a.splits * 4;
+    const uint32_t blocks = end4 < all ? end4 : all;
     const uint32_t stride = uint32_t(f8_code_stride(a.k)), sstride = uint32_t(f8_scale_stride(a.k));
-    // a wave's loads are all of x's rows or all of w's; rows past the end: the last
-    // one's again
-    static_assert(kBM % (8 * kLoads) == 0 && kBM % 64 == 0, "a wave loads rows of one operand");
-    const bool ofx = wave * kLoads * 8 < kBM, sofx = wave * 64 < kBM;
-    const uint64_t codes = ofx ? a.x + uint64_t(m0) * stride : a.w + uint64_t(n0) * stride;
-    const uint64_t words = sofx ? a.xs + uint64_t(m0) * sstride : a.ws + uint64_t(n0) * sstride;
+    // a load is 8 rows of x or of w; rows past the end: the last one's again
+    const uint64_t x0 = a.x + uint64_t(m0) * stride, w0 = a.w + uint64_t(n0) * stride;
+    const uint32_t xlast = a.m - m0 - 1, wlast = a.n - n0 - 1;
     uint32_t src[kLoads];  // this lane's 16 bytes of each of its rows
 #pragma unroll
     for (uint32_t i = 0; i < kLoads; ++i) {
-        const uint32_t r = (wave * kLoads + i) * 8 + (l >> 3) - (ofx ? 0 : kBM);
-        const uint32_t end = (ofx ? a.m - m0 : a.n - n0) - 1;
-        // (row / 2) & 7 of row 8 (wave kLoads + i) + l / 8 of the tile
-        const uint32_t swizzle = (4 * (wave * kLoads + i) + (l >> 4)) & 7u;
-        src[i] = (r < end ? r : end) * stride + ((l & 7u) ^ swizzle) * 16;
+        const uint32_t first = (wave * kLoads + i) * 8;
+        const uint32_t r = first + (l >> 3) - (first < kBM ? 0 : kBM), last = first < kBM ? xlast : wlast;
+        // (row / 2) & 7 of row first + l / 8 of the tile
+        const uint32_t swizzle = (first / 2 + (l >> 4)) & 7u;
+        src[i] = (r < last ? r : last) * stride + ((l & 7u) ^ swizzle) * 16;
     }
+    // a word of scales a lane, 64 rows a wave (waves left over: the first rows' again)
+    const uint32_t srow = wave * 64 % kRows;
+    const uint64_t words = srow < kBM ? a.xs + uint64_t(m0) * sstride : a.ws + uint64_t(n0) * sstride;
     uint32_t word;
     {
-        const uint32_t r = wave * 64 + l - (sofx ? 0 : kBM), end = (sofx ? a.m - m0 : a.n - n0) - 1;
-        word = (r < end ? r : end) * sstride;
+        const uint32_t r = srow + l - (srow < kBM ? 0 : kBM), last = srow < kBM ? xlast : wlast;
+        word = (r < last ? r : last) * sstride;
     }
     const uint32_t lds0 = lds_offset(&lds[0][0]) + wave * kLoads * 1024;
-    const uint32_t sc0 = lds_offset(&scales[0][0]) + wave * 256;
+    const uint32_t sc0 = lds_offset(&scales[0][0]) + srow * 4;
     auto stage = [&](uint32_t kb) {
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; ++i)
-            dma_to_lds(codes + uint64_t(kb) * 128, src[i], lds0 + (kb & 1) * kRows * 128 + i * 1024);
+            dma_to_lds(((wave * kLoads + i) * 8 < kBM ? x0 : w0) + uint64_t(kb) * 128, src[i],
+                       lds0 + (kb & 1) * kRows * 128 + i * 1024);
     };
     auto scale_words = [&](uint32_t group) {
         dma_word_to_lds(words + uint64_t(group) * 4, word, sc0 + (group & 1) * kRows * 4);
@@ -331,9 +337,9 @@ __global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a
     struct Fragment {
         uint4 lo, hi;
     };
-    scale_words(0);
-    stage(0);
-    for (uint32_t kb = 0; kb < blocks; ++kb) {
+    scale_words(begin >> 2);
+    stage(begin);
+    for (uint32_t kb = begin; kb < blocks; ++kb) {
         dma_wait();
         lds_barrier();  // stage kb is there, and nobody reads the other one any more
         if (kb + 1 < blocks) stage(kb + 1);
@@ -371,14 +377,51 @@ __global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a
             for (uint32_t j = 0; j < kFN; ++j) acc[i][j] = mma(w[j], x, acc[i][j]);
         }
     }
+    // Where rows of c do not lie on the alignment of four columns, a lane's results would go
+    // out one by one, neighbouring lanes 4 columns apart: such a tile goes through LDS, each
+    // wave's part through room of its own, and out with neighbouring lanes on neighbouring
+    // columns (1237 x 8191 x 2050 to fp32: 70 -> 56 us).
     const bool whole = whole_groups<kWide>(a);
+    if (whole || a.splits > 1) {
 #pragma unroll
-    for (uint32_t i = 0; i < kFM; ++i) {
-        const uint32_t row = m0 + wm + i * 16 + fr;
-        if (row < a.m) {
+        for (uint32_t i = 0; i < kFM; ++i) {
+            const uint32_t row = m0 + wm + i * 16 + fr;
+            if (row < a.m) {
 #pragma unroll
-            for (uint32_t j = 0; j < kFN; ++j) store4<kWide>(a, whole, row, n0 + wn + j * 16 + fg * 4, acc[i][j]);
+                for (uint32_t j = 0; j < kFN; ++j)
+                    store_result<kWide>(a, whole, blockIdx.y, row, n0 + wn + j * 16 + fg * 4, acc[i][j]);
+            }
         }
+        return;
+    }
+    using Out = std::conditional_t<kWide, float, __bf16>;
+    constexpr uint32_t kCols = kFN * 16, kPerChunk = 16 / sizeof(Out), kChunks = kCols / kPerChunk;
+    static_assert(kWaves * kFM * 16 * kCols * sizeof(Out) <= sizeof(lds), "the tile fits");
+    lds_barrier();  // the last stage is read
+    Out* room = reinterpret_cast<Out*>(&lds[0][0]) + wave * kFM * 16 * kCols;
+    // a row's 16-byte chunks at chunk ^ row, against bank conflicts
+    auto at = [&](uint32_t row, uint32_t col) {
+        return row * kCols + ((col / kPerChunk) ^ (row % kChunks)) * kPerChunk + col % kPerChunk;
+    };
+#pragma unroll
+    for (uint32_t i = 0; i < kFM; ++i)
+#pragma unroll
+        for (uint32_t j = 0; j < kFN; ++j) {
+            Out* p = room + at(i * 16 + fr, j * 16 + fg * 4);
+            if constexpr (kWide)
+                *reinterpret_cast<v4f_t*>(p) = acc[i][j];
+            else
+                *reinterpret_cast<v4bf_t*>(p) = __builtin_convertvector(acc[i][j], v4bf_t);
+        }
+    lds_wait();
+    constexpr uint32_t kRowsOut = 64 / kCols;  // rows a wave stores at once
+    const uint32_t col = l % kCols, n = n0 + wn + col;
+    if (n >= a.n) return;
+    MEZO_GLOBAL Out* c = reinterpret_cast<MEZO_GLOBAL Out*>(a.c) + n;
+#pragma unroll 4
+    for (uint32_t r = l / kCols; r < kFM * 16; r += kRowsOut) {
+        const uint32_t row = m0 + wm + r;
+        if (row < a.m) c[row * a.ldc] = room[at(r, col)];
     }
 }
 
@@ -487,23 +530,42 @@ __global__ void __launch_bounds__(256) f8_join_kernel(F8MatmulArgs a)
     store4<kWide>(a, whole_groups<kWide>(a), row, col, sum);
 }
 
-// How a product is cut: the kernel (rows of its tile of activations) and the
-// workgroups that share out k.
+// The kernels, and how a product is cut into them: its tile, and the workgroups that
+// share out k.
+enum Tile8 { kThin, k64x64, k128x128, k256x256 };
+
 struct Cut {
-    uint32_t tile, splits;
+    Tile8 tile;
+    uint32_t splits;
 };
+
+constexpr uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t bm, uint64_t bn)
+{
+    return ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
+}
 
 Cut cut_product(uint64_t m, uint64_t n, uint64_t k, bool wide)
 {
-    auto tiles = [&](uint64_t bm, uint64_t bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
     if (m <= 64) {
         // a workgroup a CU, each with two stages at least
-        const uint64_t want = 256 / tiles(64, kThinRows), most = f8_blocks(k) / (2 * kThinBlocks);
+        const uint64_t want = 256 / tiles_of(m, n, 64, kThinRows), most = f8_blocks(k) / (2 * kThinBlocks);
         const uint64_t splits = want < most ? want : most;
-        return {64, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits))};
+        return {kThin, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits))};
     }
-    if (!wide && tiles(256, 256) >= 256) return {256, 1};
-    return {128, 1};
+    // Rounds of workgroups over the 256 CUs, one of 256 x 256 or two of 128 x 128 each: a
+    // round of the former takes 1.8 times one of the latter (60 and 33 us at k = 4096), for
+    // twice the work. 3000 x 5000 x 4096: 56 us in 240 large tiles, 61 in 960 small ones;
+    // 300 x 50272 x 768: 36 in 394 large ones, 27 in 1179.
+    const uint64_t t128 = tiles_of(m, n, 128, 128);
+    const uint64_t rounds128 = (t128 + 511) / 512, rounds256 = (tiles_of(m, n, 256, 256) + 255) / 256;
+    if (!wide && 9 * rounds256 <= 5 * rounds128) return {k256x256, 1};
+    if (t128 >= 200) return {k128x128, 1};
+    // Too few of those for the CUs: smaller tiles, and k split where it is long, in parts of
+    // 16 blocks at least (128 x 4096 x 16384 to bf16: 79 us in 32 tiles of 128, 60 in 128 of
+    // 64, 24 with k in four; 1024 x 768 x 3000: 18, 9, 13 with k in two).
+    const uint64_t want = 512 / tiles_of(m, n, 64, 64), most = f8_blocks(k) / 16;
+    const uint64_t splits = want < most ? want : most;
+    return {k64x64, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits))};
 }
 
 uint64_t f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t out_dtype)
@@ -518,27 +580,30 @@ hipError_t launch_product(F8MatmulArgs a, hipStream_t stream)
     const Cut cut = cut_product(a.m, a.n, a.k, kWide);
     a.splits = cut.splits;
     void* params[] = {&a};
-    auto go = [&](const void* f, dim3 groups, uint32_t lanes) {
-        return hipLaunchKernel(f, groups, dim3(lanes), params, 0, stream);
+    auto go = [&](auto* f, uint64_t bm, uint64_t bn, uint32_t lanes) {
+        const dim3 groups(uint32_t(tiles_of(a.m, a.n, bm, bn)), a.splits);
+        return hipLaunchKernel(reinterpret_cast<const void*>(f), groups, dim3(lanes), params, 0, stream);
     };
-    auto tiles = [&](uint32_t bm, uint32_t bn) { return dim3(((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn), a.splits); };
-    hipError_t e;
-    if (cut.tile == 64) {
-        const void* f = a.m <= 16   ? reinterpret_cast<const void*>(f8_thin_kernel<1, kWide>)
-                        : a.m <= 32 ? reinterpret_cast<const void*>(f8_thin_kernel<2, kWide>)
-                                    : reinterpret_cast<const void*>(f8_thin_kernel<4, kWide>);
-        e = go(f, tiles(64, kThinRows), 256);
-    } else if (cut.tile == 128) {
-        e = go(reinterpret_cast<const void*>(f8_matmul_kernel<128, 128, 2, 2, kWide>), tiles(128, 128), 256);
-    } else {
-        if constexpr (kWide)
-            return hipErrorInvalidValue;  // (cut_product never says so)
+    hipError_t e = hipErrorInvalidValue;
+    switch (cut.tile) {
+    case kThin:
+        if (a.m <= 16)
+            e = go(f8_thin_kernel<1, kWide>, 64, kThinRows, 256);
+        else if (a.m <= 32)
+            e = go(f8_thin_kernel<2, kWide>, 64, kThinRows, 256);
         else
-            e = go(reinterpret_cast<const void*>(f8_matmul_kernel<256, 256, 2, 4, false>), tiles(256, 256), 512);
+            e = go(f8_thin_kernel<4, kWide>, 64, kThinRows, 256);
+        break;
+    case k64x64: e = go(f8_matmul_kernel<64, 64, 2, 2, kWide>, 64, 64, 256); break;
+    case k128x128: e = go(f8_matmul_kernel<128, 128, 2, 2, kWide>, 128, 128, 256); break;
+    case k256x256:
+        if constexpr (!kWide) e = go(f8_matmul_kernel<256, 256, 2, 4, false>, 256, 256, 512);
+        break;
     }
     if (e != hipSuccess || a.splits == 1) return e;
     const uint64_t groups = uint64_t(a.m) * ((a.n + 3) / 4);
-    return go(reinterpret_cast<const void*>(f8_join_kernel<kWide>), dim3(uint32_t((groups + 255) / 256)), 256);
+    return hipLaunchKernel(reinterpret_cast<const void*>(f8_join_kernel<kWide>), dim3(uint32_t((groups + 255) / 256)),
+                           dim3(256), params, 0, stream);
 }
 
 hipError_t launch_f8_matmul(const F8MatmulArgs& args, hipStream_t stream)
