@@ -323,9 +323,18 @@ struct Tile {
 enum Mode { kGeneral, kPlain, kBiased, kCapped };
 constexpr float kMostCap = 96.0f / kLog2e;
 
+// The waves a SIMD that the registers are kept down for: what LDS allows, and as far as
+// nothing spills.
+template <bool kF, uint32_t kD, bool kKeys>
+constexpr uint32_t waves_per_simd()
+{
+    if (kF) return kKeys && kD > 64 ? 1 : 2;
+    return kD > 64 || kKeys ? 2 : 3;
+}
+
 // kKeys: the workgroup's waves share out the keys; else the rows.
 template <bool kF, uint32_t kD, uint32_t kWaves, bool kKeys, Mode kMode>
-__global__ void __launch_bounds__(kWaves * 64, kKeys && kF && kD > 64 ? 1 : 2) attention_kernel(AttentionArgs a)
+__global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())) attention_kernel(AttentionArgs a)
 {
     using T = Tile<kF, kD>;
     constexpr uint32_t kStage = kKeys || (kF && kD > 64) ? 32 : 64;  // keys of a stage
@@ -361,7 +370,8 @@ __global__ void __launch_bounds__(kWaves * 64, kKeys && kF && kD > 64 ? 1 : 2) a
         const int n = int(__builtin_amdgcn_readfirstlane(uint32_t(visible(a, d, query(r)))));
         return n > 0 ? n : 0;
     };
-    const int low = seen(first), high = seen(first + 31), last = seen(tile1 - 1);
+    // (a wave without a row has nothing to do but to load its part of the stages)
+    const int low = seen(first), high = first < tile1 ? seen(first + 31) : 0, last = seen(tile1 - 1);
 
     // the stages of this split of the workgroup's keys
     const uint32_t stages = (uint32_t(last) + kStage - 1) / kStage, per = a.chunk / kStage;
@@ -459,6 +469,9 @@ __global__ void __launch_bounds__(kWaves * 64, kKeys && kF && kD > 64 ? 1 : 2) a
         const uint8_t* kt = lds[kKeys ? wave : 0][b][0];
         const uint8_t* vt = lds[kKeys ? wave : 0][b][1];
         const bool edge = k0 + int(kStage) > low;  // some query of the wave does not see them all
+        // fp32: the matrix instructions bound it, so the halves of a stage that no query of
+        // the wave sees are left out; for bf16 the branches would cost more than that saves
+        auto hidden = [&](uint32_t t) { return kF && k0 + int(t * 32) >= high; };
         {
             constexpr uint32_t kT = kStage / 32;
             v16f_t x[kT];
@@ -466,6 +479,7 @@ __global__ void __launch_bounds__(kWaves * 64, kKeys && kF && kD > 64 ? 1 : 2) a
             float top = kLowest;
 #pragma unroll
             for (uint32_t t = 0; t < kT; ++t) {
+                if (hidden(t)) continue;
                 x[t] = T::scores(kt, t * 32, q, l, bias);
                 if constexpr (kKeys) {
                     lds_wait();  // K's buffer is read: the next stage's loads under the rest of this one
@@ -478,6 +492,7 @@ __global__ void __launch_bounds__(kWaves * 64, kKeys && kF && kD > 64 ? 1 : 2) a
                 const int key = k0 + int(t * 32 + 4 * (l >> 5));
                 const float from = float(pos - key);
                 off[t] = 0.0f;
+                if (hidden(t)) continue;
                 if constexpr (kMode == kCapped) {
 #pragma unroll
                     for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped<kF>(sc, x[t][e]);
@@ -554,6 +569,7 @@ __global__ void __launch_bounds__(kWaves * 64, kKeys && kF && kD > 64 ? 1 : 2) a
 #pragma unroll
             for (uint32_t t = 0; t < kT; ++t) {
                 const float ref = m - off[t];
+                if (hidden(t)) continue;
 #pragma unroll
                 for (uint32_t e = 0; e < 16; ++e) {
                     if constexpr (kMode == kPlain || kMode == kBiased)

@@ -164,25 +164,36 @@ __global__ void __launch_bounds__(kLossThreads) loss_rows_kernel(LossArgs a)
 template <uint32_t kDtype>
 __global__ void __launch_bounds__(kFinishThreads) loss_finish_kernel(LossArgs a)
 {
+    // a lane's rows in batches, whose loads are all under way before the first is used (16384
+    // rows: 9.4 -> 6.6 us)
+    constexpr uint32_t kBatch = 8;
     double sum = 0.0;
     uint32_t count = 0;
-    for (uint64_t t = threadIdx.x; t < a.rows; t += kFinishThreads) {
-        const int64_t target = a.targets[t];
-        float loss = 0.0f;
-        if (a.parts == 1) {
-            loss = a.losses[t];
-        } else {
-            if (target >= 0) {
-                const float2* p = a.partial + t * a.parts;
-                MaxSum s = {p[0].x, p[0].y};
-                for (uint32_t i = 1; i < a.parts; ++i) s = join(s, {p[i].x, p[i].y});
-                loss = loss_of(s, Row<kDtype>{a.logits + t * a.ld * Row<kDtype>::kBytes}, a.vocab, target);
-            }
-            a.losses[t] = loss;
+    for (uint64_t t0 = threadIdx.x; t0 < a.rows; t0 += kBatch * kFinishThreads) {
+        int64_t target[kBatch];
+        float loss[kBatch];
+#pragma unroll
+        for (uint32_t j = 0; j < kBatch; ++j) {
+            const uint64_t t = t0 + j * kFinishThreads;
+            target[j] = t < a.rows ? a.targets[t] : -1;
+            loss[j] = t < a.rows && a.parts == 1 ? a.losses[t] : 0.0f;
         }
-        if (target >= 0) {
-            sum += double(loss);
-            ++count;
+#pragma unroll
+        for (uint32_t j = 0; j < kBatch; ++j) {
+            const uint64_t t = t0 + j * kFinishThreads;
+            if (a.parts > 1 && t < a.rows) {
+                if (target[j] >= 0) {
+                    const float2* p = a.partial + t * a.parts;
+                    MaxSum s = {p[0].x, p[0].y};
+                    for (uint32_t i = 1; i < a.parts; ++i) s = join(s, {p[i].x, p[i].y});
+                    loss[j] = loss_of(s, Row<kDtype>{a.logits + t * a.ld * Row<kDtype>::kBytes}, a.vocab, target[j]);
+                }
+                a.losses[t] = loss[j];
+            }
+            if (target[j] >= 0) {
+                sum += double(loss[j]);
+                ++count;
+            }
         }
     }
     if (!a.mean) return;
@@ -212,8 +223,9 @@ constexpr uint64_t kWaveRow = 2048;
 
 uint32_t loss_parts(uint64_t rows, uint64_t vocab)
 {
-    // enough workgroups to fill the GPU, each with a few KB at least
-    const uint64_t want = (512 + rows - 1) / rows, most = vocab / 4096;
+    // enough workgroups that the last round over the CUs is a small part of all, each with a
+    // few KB at least
+    const uint64_t want = (2048 + rows - 1) / rows, most = vocab / 4096;
     const uint64_t parts = want < most ? want : most;
     return vocab < kWaveRow || parts < 1 ? 1u : uint32_t(parts < 16 ? parts : 16);
 }

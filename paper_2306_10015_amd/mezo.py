@@ -5,7 +5,6 @@ device memory and the current stream. Importing this module loads
 ``libmezo.so`` from this directory and raises if it is not built (build it
 with ``python -m paper_2306_10015_amd.build``); there is no fallback.
 
-    import torch
     from paper_2306_10015_amd import mezo
     params = [torch.randn(1024, 1024, device="cuda") * 0.02 for _ in range(4)]
     ps = mezo.ParamSet(params)                       # tensor_id = position
@@ -19,10 +18,12 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import math
+import struct
 from pathlib import Path
 from typing import Iterable, Sequence
 
 import numpy as np
+import torch
 
 LIB_PATH = Path(__file__).resolve().parent / "libmezo.so"
 
@@ -57,12 +58,8 @@ class Codec(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_uint32), ("scale", ctypes.c_float), ("alpha", ctypes.c_float)]
 
 
-class Attention(ctypes.Structure):
-    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "k", "v", "out", "lse", "docs", "slopes")]
-                + [(n, ctypes.c_uint64) for n in ("q_tokens", "k_tokens", "q_token", "q_head", "k_token", "k_head",
-                                                  "v_token", "v_head", "o_token", "o_head", "max_q", "max_k")]
-                + [(n, ctypes.c_uint32) for n in ("n_docs", "heads", "kv_heads", "dim", "dtype", "causal")]
-                + [("scale", ctypes.c_float), ("softcap", ctypes.c_float)])
+#: Layout of mezo_attention_t: 7 pointers, 12 u64, 6 u32, 2 floats.
+_ATTENTION = struct.Struct("=7Q12Q6I2f")
 
 
 class Step(ctypes.Structure):
@@ -87,9 +84,8 @@ EXPORTS = ("mezo_paramset_create", "mezo_paramset_destroy", "mezo_paramset_numel
 def _load() -> ctypes.CDLL:
     # libmezo must run on the same HIP runtime as torch: the streams and device
     # pointers it receives belong to that runtime. torch carries its own copy
-    # (same SONAME); importing torch first makes the dynamic loader bind
+    # (same SONAME); importing torch first (above) makes the dynamic loader bind
     # libmezo to it instead of loading a second runtime.
-    import torch  # noqa: F401
     if not LIB_PATH.exists():
         raise ImportError(f"{LIB_PATH} is not built: run python -m paper_2306_10015_amd.build")
     L = ctypes.CDLL(str(LIB_PATH))
@@ -137,9 +133,9 @@ def _load() -> ctypes.CDLL:
     L.mezo_f8_linear_workspace.restype = u64
     L.mezo_f8_linear.argtypes = [vp, u32, u64, vp, vp, u64, u64, u64, vp, u32, u64, vp, u64, vp]
     L.mezo_f8_linear.restype = i32
-    L.mezo_attention_workspace.argtypes = [ctypes.POINTER(Attention)]
+    L.mezo_attention_workspace.argtypes = [vp]
     L.mezo_attention_workspace.restype = u64
-    L.mezo_attention.argtypes = [ctypes.POINTER(Attention), vp, u64, vp]
+    L.mezo_attention.argtypes = [vp, vp, u64, vp]
     L.mezo_attention.restype = i32
     L.mezo_token_loss_workspace.argtypes = [u64, u64]
     L.mezo_token_loss_workspace.restype = u64
@@ -202,7 +198,6 @@ def seeds_array(seeds) -> np.ndarray:
 
 
 def _stream_ptr(stream) -> int | None:
-    import torch
     if stream is None:
         # (torch.cuda.current_stream() makes a Stream object: 3 us)
         return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
@@ -210,7 +205,6 @@ def _stream_ptr(stream) -> int | None:
 
 
 def _dtype_code(t) -> int:
-    import torch
     if t.dtype == torch.float32:
         return F32
     if t.dtype == torch.bfloat16:
@@ -225,7 +219,6 @@ class NF4Tensor:
     64 elements), both contiguous device tensors owned by torch."""
 
     def __init__(self, codes, absmax, numel: int):
-        import torch
         if codes.dtype != torch.uint8 or absmax.dtype != torch.float32:
             raise TypeError("codes must be uint8 and absmax float32")
         if not (codes.is_cuda and absmax.is_cuda and codes.is_contiguous() and absmax.is_contiguous()):
@@ -236,7 +229,6 @@ class NF4Tensor:
 
     @classmethod
     def empty(cls, numel: int, device="cuda") -> "NF4Tensor":
-        import torch
         return cls(torch.empty((numel + 1) // 2, dtype=torch.uint8, device=device),
                    torch.empty((numel + NF4_BLOCK - 1) // NF4_BLOCK, dtype=torch.float32, device=device),
                    numel)
@@ -259,7 +251,6 @@ def nf4_quantize(values, out: NF4Tensor | None = None, stream=None) -> NF4Tensor
     out = NF4Tensor.empty(n, values.device) if out is None else out
     if out.numel() != n or not values.is_contiguous():
         raise ValueError("size mismatch or non-contiguous values")
-    import torch
     with torch.cuda.device(values.device):
         _check(lib.mezo_nf4_quantize(values.data_ptr(), _dtype_code(values), n, out.codes.data_ptr(),
                                      out.absmax.data_ptr(), _stream_ptr(stream)), "mezo_nf4_quantize")
@@ -268,7 +259,6 @@ def nf4_quantize(values, out: NF4Tensor | None = None, stream=None) -> NF4Tensor
 
 def nf4_dequantize(t: NF4Tensor, dtype=None, out=None, stream=None):
     """NF4 storage -> a fp32 (default) or bf16 device tensor of numel elements."""
-    import torch
     if out is None:
         out = torch.empty(t.numel(), dtype=dtype or torch.float32, device=t.device)
     if out.numel() != t.numel() or not out.is_contiguous():
@@ -288,7 +278,6 @@ _DEVICES = 0
 def _on(device, stream):
     """Run a call on `device`, its outputs and scratch allocated on the stream
     it runs on (memory of another stream's pool could still be in use there)."""
-    import torch
     global _DEVICES
     if not _DEVICES:
         _DEVICES = torch.cuda.device_count()
@@ -322,7 +311,6 @@ def _same_device(first, *others):
 
 
 def _scratch(nbytes: int, device):
-    import torch
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
@@ -337,7 +325,6 @@ class F8Matrix:
     scale 2^(byte - 127)), both contiguous device tensors owned by torch."""
 
     def __init__(self, codes, scales, rows: int, cols: int):
-        import torch
         if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
             raise TypeError("codes and scales must be uint8")
         rows, cols = int(rows), int(cols)
@@ -352,7 +339,6 @@ class F8Matrix:
 
     @classmethod
     def empty(cls, rows: int, cols: int, device="cuda") -> "F8Matrix":
-        import torch
         blocks = (int(cols) + F8_BLOCK - 1) // F8_BLOCK
         return cls(torch.empty(rows, blocks * F8_BLOCK, dtype=torch.uint8, device=device),
                    torch.empty(rows, (blocks + 3) // 4 * 4, dtype=torch.uint8, device=device), rows, cols)
@@ -383,7 +369,6 @@ def f8_quantize(values, out: F8Matrix | None = None, stream=None) -> F8Matrix:
 def f8_matmul(x: F8Matrix, w: F8Matrix, dtype=None, out=None, stream=None):
     """x w^T of two 8-bit matrices, [m, k] and [n, k], as a [m, n] tensor of
     dtype (torch.bfloat16, the default, or torch.float32: see mezo_f8_matmul)."""
-    import torch
     if x.cols != w.cols:
         raise ValueError(f"x has {x.cols} columns, w {w.cols}")
     m, n, k = x.rows, w.rows, x.cols
@@ -408,7 +393,6 @@ def f8_linear(x, w: F8Matrix, dtype=None, out=None, stream=None):
     """A layer's product: the activations x (fp32/bf16 [m, k]) quantized, times
     the weights w ([n, k]) in 8-bit storage: [m, n] of dtype (x's by default).
     The same as f8_matmul(f8_quantize(x), w, dtype), in one call."""
-    import torch
     m, k, ldx = _rows_of(x, "x")
     if k != w.cols:
         raise ValueError(f"x has {k} columns, w {w.cols}")
@@ -439,7 +423,6 @@ class Documents:
     from lengths, checked."""
 
     def __init__(self, table, max_q: int, max_k: int):
-        import torch
         if table.dtype != torch.int64:
             raise TypeError(f"table must be int64, got {table.dtype}")
         if not table.is_cuda or table.dim() != 2 or table.shape[1] != 5 or not table.is_contiguous():
@@ -453,7 +436,6 @@ class Documents:
         """From sequences of lengths: q_lens queries and k_lens keys a document
         (q_lens by default), the visible prefix (0), and where each begins
         (packed one after another by default)."""
-        import torch
 
         def ints(x, default):
             out = [int(v) for v in (default if x is None else x)]
@@ -502,7 +484,6 @@ def attention(q, k, v, docs: Documents, causal: bool = True, scale: float | None
     default; slopes, fp32 [heads], biases scores by -slope * distance. Returns
     out, like q, and with return_lse the pair (out, lse), lse fp32 [tokens, heads].
     Tokens of no document are not written."""
-    import torch
     tq, heads, dim, q_token, q_head = _heads_of(q, "q")
     tk, kv_heads, k_dim, k_token, k_head = _heads_of(k, "k")
     tv, v_heads, v_dim, v_token, v_head = _heads_of(v, "v")
@@ -523,13 +504,14 @@ def attention(q, k, v, docs: Documents, causal: bool = True, scale: float | None
         _same_device(q, k, v, out, slopes, docs.table)
         lse = torch.empty(tq, heads, dtype=torch.float32, device=q.device) if return_lse else None
         _, _, _, o_token, o_head = _heads_of(out, "out")
-        a = Attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), docs.table.data_ptr(),
-                      _ptr(slopes), tq, tk, q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head,
-                      docs.max_q, docs.max_k, docs.table.shape[0], heads, kv_heads, dim, dtype, int(causal),
-                      1.0 / math.sqrt(dim) if scale is None else float(scale), float(softcap))
-        nbytes = lib.mezo_attention_workspace(ctypes.byref(a))
+        a = _ATTENTION.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse) or 0,
+                            docs.table.data_ptr(), _ptr(slopes) or 0, tq, tk, q_token, q_head, k_token, k_head,
+                            v_token, v_head, o_token, o_head, docs.max_q, docs.max_k, docs.table.shape[0], heads,
+                            kv_heads, dim, dtype, 1 if causal else 0,
+                            1.0 / math.sqrt(dim) if scale is None else scale, softcap)
+        nbytes = lib.mezo_attention_workspace(a)
         ws = _scratch(nbytes, q.device)
-        _check(lib.mezo_attention(ctypes.byref(a), _ptr(ws), nbytes, _stream_ptr(None)), "mezo_attention")
+        _check(lib.mezo_attention(a, _ptr(ws), nbytes, _stream_ptr(None)), "mezo_attention")
     return (out, lse) if return_lse else out
 
 
@@ -538,7 +520,6 @@ def token_loss(logits, targets, stream=None):
     logits fp32/bf16 [tokens, vocabulary] with contiguous rows, targets int64
     [tokens], negative where a token does not count. Returns (losses, mean),
     fp32 device tensors of [tokens] and of no dimension."""
-    import torch
     rows, vocab, ld = _rows_of(logits, "logits")
     dtype = _dtype_code(logits)
     if targets.dtype != torch.int64:
@@ -587,7 +568,6 @@ class ParamSet:
             raise ValueError(f"all tensors of a paramset must live on one device, got {sorted(map(str, devices))}")
         #: the device every call of this paramset runs on (made current for the call)
         self.device = devices.pop() if devices else None
-        import torch
         self._switch = torch.cuda.device_count() > 1
         ids = list(range(len(self.tensors))) if tensor_ids is None else [int(i) for i in tensor_ids]
         if len(ids) != len(self.tensors):
@@ -615,7 +595,6 @@ class ParamSet:
         """Make the paramset's device current for a call (a stream or pointer
         of another device would not be valid for its kernels); with a single
         visible device there is nothing to switch."""
-        import torch
         return torch.cuda.device(self.device) if self._switch else contextlib.nullcontext()
 
     @property
@@ -694,7 +673,6 @@ class ParamSet:
 
     def checksum(self, stream=None) -> int:
         """The checksum as a Python int (waits for the stream it ran on)."""
-        import torch
         out = torch.empty(1, dtype=torch.int64, device=self.device)
         self.checksum_into(out, stream)
         if stream is not None:
@@ -759,7 +737,6 @@ def debug_generate(seed, tensor_id: int, first: int, count: int, words=True, z=T
                    stream=None, gaussian: int = GAUSS_FAST):
     """Device tensors (words uint32 as int32 bits, z float32) of elements
     first .. first+count-1 of tensor tensor_id under seed."""
-    import torch
     w = torch.empty(count, dtype=torch.int32, device="cuda") if words else None
     zz = torch.empty(count, dtype=torch.float32, device="cuda") if z else None
     _check(lib.mezo_debug_generate(_seed(seed), int(tensor_id), int(first), int(count),
@@ -772,7 +749,6 @@ def debug_generate(seed, tensor_id: int, first: int, count: int, words=True, z=T
 def debug_box_muller(words, gaussian: int = GAUSS_FAST, stream=None):
     """z (float32 device tensor) of the given words (int32/uint32-bit device
     tensor, a multiple of 4 long), through the library's Gaussian transform."""
-    import torch
     if words.numel() % 4 or not words.is_contiguous() or words.element_size() != 4:
         raise ValueError("words: contiguous 32-bit device tensor, a multiple of 4 long")
     z = torch.empty(words.numel(), dtype=torch.float32, device=words.device)
