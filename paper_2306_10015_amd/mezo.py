@@ -200,7 +200,7 @@ def seeds_array(seeds) -> np.ndarray:
 def _stream_ptr(stream) -> int | None:
     if stream is None:
         # (torch.cuda.current_stream() makes a Stream object: 3 us)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -294,17 +294,25 @@ def _on(device, stream):
 
 def _rows_of(t, what: str):
     """A 2-D CUDA tensor whose rows are contiguous, and the elements between them."""
-    if t.dim() != 2 or not t.is_cuda:
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{what}: a 2-D CUDA tensor")
-    rows, cols = t.shape
+    rows, cols = shape
     if rows == 0 or cols == 0:
         raise ValueError(f"{what}: empty")
-    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+    ld, step = t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
         raise ValueError(f"{what}: the elements of a row must be contiguous")
-    return rows, cols, t.stride(0) if rows > 1 else cols
+    return rows, cols, ld if rows > 1 else cols
 
 
 def _same_device(first, *others):
+    """All on the device of `first`, a CUDA tensor (with one device: all on it)."""
+    if _DEVICES == 1:
+        for t in others:
+            if t is not None and not t.is_cuda:
+                raise ValueError(f"tensors on several devices: {first.device} and {t.device}")
+        return
     for t in others:
         if t is not None and t.device != first.device:
             raise ValueError(f"tensors on several devices: {first.device} and {t.device}")
@@ -425,11 +433,12 @@ class Documents:
     def __init__(self, table, max_q: int, max_k: int):
         if table.dtype != torch.int64:
             raise TypeError(f"table must be int64, got {table.dtype}")
-        if not table.is_cuda or table.dim() != 2 or table.shape[1] != 5 or not table.is_contiguous():
+        shape = table.shape
+        if len(shape) != 2 or shape[1] != 5 or not table.is_cuda or not table.is_contiguous():
             raise ValueError("table: a contiguous CUDA tensor [documents, 5]")
         if max_q < 0 or max_k < 0:
             raise ValueError("max_q and max_k must not be negative")
-        self.table, self.max_q, self.max_k = table, int(max_q), int(max_k)
+        self.table, self.count, self.max_q, self.max_k = table, shape[0], int(max_q), int(max_k)
 
     @classmethod
     def of(cls, q_lens, k_lens=None, prefix=None, q_first=None, k_first=None, device="cuda") -> "Documents":
@@ -465,9 +474,10 @@ class Documents:
 def _heads_of(t, what: str):
     """(tokens, heads, dim) of a 3-D CUDA tensor with contiguous heads, and the
     elements from one token and from one head to the next."""
-    if t.dim() != 3 or not t.is_cuda:
+    shape = t.shape
+    if len(shape) != 3 or not t.is_cuda:
         raise ValueError(f"{what}: a CUDA tensor [tokens, heads, dim]")
-    tokens, heads, dim = t.shape
+    tokens, heads, dim = shape
     st, sh, sd = t.stride()
     if dim > 1 and sd != 1:
         raise ValueError(f"{what}: the elements of a head must be contiguous")
@@ -498,15 +508,17 @@ def attention(q, k, v, docs: Documents, causal: bool = True, scale: float | None
         raise ValueError(f"slopes: a contiguous float32 tensor of {heads}")
     with _on(q.device, stream):
         if out is None:
-            out = torch.empty(tq, heads, dim, dtype=q.dtype, device=q.device)
-        elif out.dtype != q.dtype or out.shape != q.shape:
-            raise ValueError("out must be like q")
+            out = torch.empty((tq, heads, dim), dtype=q.dtype, device=q.device)
+            o_token, o_head = heads * dim, dim
+        else:
+            if out.dtype != q.dtype or out.shape != q.shape:
+                raise ValueError("out must be like q")
+            _, _, _, o_token, o_head = _heads_of(out, "out")
         _same_device(q, k, v, out, slopes, docs.table)
-        lse = torch.empty(tq, heads, dtype=torch.float32, device=q.device) if return_lse else None
-        _, _, _, o_token, o_head = _heads_of(out, "out")
+        lse = torch.empty((tq, heads), dtype=torch.float32, device=q.device) if return_lse else None
         a = _ATTENTION.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse) or 0,
                             docs.table.data_ptr(), _ptr(slopes) or 0, tq, tk, q_token, q_head, k_token, k_head,
-                            v_token, v_head, o_token, o_head, docs.max_q, docs.max_k, docs.table.shape[0], heads,
+                            v_token, v_head, o_token, o_head, docs.max_q, docs.max_k, docs.count, heads,
                             kv_heads, dim, dtype, 1 if causal else 0,
                             1.0 / math.sqrt(dim) if scale is None else scale, softcap)
         nbytes = lib.mezo_attention_workspace(a)
