@@ -218,11 +218,47 @@ __global__ void __launch_bounds__(kFinishThreads) loss_finish_kernel(LossArgs a)
     }
 }
 
+// A few short rows: one workgroup reads them all, one after another, and takes the mean.
+template <uint32_t kDtype>
+__global__ void __launch_bounds__(kFinishThreads) loss_all_kernel(LossArgs a)
+{
+    __shared__ MaxSum part[kFinishThreads / 64];
+    double sum = 0.0;
+    uint32_t count = 0;
+    for (uint32_t t = 0; t < a.rows; ++t) {
+        const int64_t target = a.targets[t];
+        float loss = 0.0f;
+        if (target >= 0) {  // (uniform)
+            const Row<kDtype> row = {a.logits + t * a.ld * Row<kDtype>::kBytes};
+            const MaxSum s = join_wave(read_row<kDtype, kFinishThreads>(row, a.vocab, 0, 1, threadIdx.x));
+            if ((threadIdx.x & 63u) == 0) part[threadIdx.x >> 6] = s;
+            __syncthreads();
+            // every wave joins the 16 parts: the same values in the same order
+            const uint32_t l = threadIdx.x & 63u;
+            MaxSum all = l < kFinishThreads / 64 ? part[l] : MaxSum{-__builtin_inff(), 0.0f};
+            all = join_wave(all);
+            loss = loss_of(all, row, a.vocab, target);
+            sum += double(loss);
+            ++count;
+            __syncthreads();  // the parts are read
+        }
+        if (threadIdx.x == 0) a.losses[t] = loss;
+    }
+    if (threadIdx.x == 0 && a.mean) *a.mean = count ? float(sum / double(count)) : 0.0f;
+}
+
+// One or two rows of together so many logits at most: one workgroup. A row of 50272 fp32
+// logits takes 6.8 us in it, 7.5 in 12 workgroups and a second launch, which costs the
+// host 4 us more.
+constexpr uint64_t kOneGroup = 65536;
+constexpr bool one_group(uint64_t rows, uint64_t vocab) { return rows <= 2 && vocab <= kOneGroup / rows; }
+
 // Rows shorter than this take a wave each.
 constexpr uint64_t kWaveRow = 2048;
 
 uint32_t loss_parts(uint64_t rows, uint64_t vocab)
 {
+    if (one_group(rows, vocab)) return 1;
     // enough workgroups that the last round over the CUs is a small part of all, each with a
     // few KB at least
     const uint64_t want = (2048 + rows - 1) / rows, most = vocab / 4096;
@@ -234,6 +270,9 @@ template <uint32_t kDtype>
 hipError_t launch(LossArgs a, hipStream_t stream)
 {
     void* params[] = {&a};
+    if (one_group(a.rows, a.vocab))
+        return hipLaunchKernel(reinterpret_cast<const void*>(loss_all_kernel<kDtype>), dim3(1), dim3(kFinishThreads),
+                               params, 0, stream);
     const bool wave = a.vocab < kWaveRow;
     const void* f = wave ? reinterpret_cast<const void*>(loss_rows_kernel<kDtype, 64>)
                          : reinterpret_cast<const void*>(loss_rows_kernel<kDtype, kLossThreads>);
