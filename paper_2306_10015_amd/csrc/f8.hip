@@ -40,7 +40,7 @@ typedef MEZO_GLOBAL u32x2_t gu32x2_t;
 // lanes, which find its maximum by DPP. A lane starts kQuantLoads loads before it
 // uses any.
 constexpr uint32_t kQuantThreads = 256;
-constexpr uint32_t kQuantLoads = 4;
+constexpr uint32_t kQuantLoads = 2;
 
 template <int kCtrl>
 __device__ __forceinline__ float dpp_max(float x)
