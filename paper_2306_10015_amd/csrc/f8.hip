@@ -427,19 +427,20 @@ __global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a
 
 // A product of few activations, m <= 16 kFM: bound by the weights' bytes. A
 // workgroup takes 64 weights' rows, a wave 16 of them, and a share of k. A stage is
-// four blocks of every row (512 bytes, and a word of scales), loaded straight into
-// LDS, as many stages in flight as fit. Fragments loaded from global memory straight
+// two blocks of every row (256 bytes, and the word that holds their scales), loaded
+// straight into LDS, two stages ahead (one for m > 32), two workgroups a CU. Fragments loaded from global memory straight
 // into registers would need neither LDS nor barriers, but there neighbouring lanes
 // read different rows, and the address units take such a load apart line by line:
 // 25 us for 24 activations and 16384 x 4096 weights, as slow with all weights in L2.
-constexpr uint32_t kThinRows = 64, kThinBytes = 512, kThinBlocks = 4;
+constexpr uint32_t kThinRows = 64, kThinBlocks = 2, kThinBytes = kThinBlocks * 128;
 
 template <uint32_t kFM, bool kWide>
 __global__ void __launch_bounds__(256) f8_thin_kernel(F8MatmulArgs a)
 {
     constexpr uint32_t kX = kFM * 16, kRows = kThinRows + kX, kStage = kRows * kThinBytes;
     constexpr uint32_t kDepth = kFM == 4 ? 2 : 3;
-    constexpr uint32_t kWLoads = kThinRows / 8, kXLoads = kX / 8;  // a wave's, 2 rows each
+    constexpr uint32_t kLoadRows = 1024 / kThinBytes, kChunks = kThinBytes / 16;
+    constexpr uint32_t kWLoads = kThinRows / kLoadRows / 4, kXLoads = kX / kLoadRows / 4;  // a wave's
     constexpr uint32_t kPerStage = kWLoads + kXLoads + 1;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kDepth][kStage];
     __shared__ __attribute__((aligned(256))) uint32_t scales[kDepth][kThinRows + 64];
@@ -458,16 +459,17 @@ __global__ void __launch_bounds__(256) f8_thin_kernel(F8MatmulArgs a)
     const uint32_t sc0 = lds_offset(&scales[0][0]) + (wave == 0 ? kThinRows * 4 : 0);
     auto load = [&](uint32_t s, uint32_t buffer) {
         // past the row's end (its blocks are no multiple of four): its last bytes again
-        const uint32_t col0 = s * kThinBytes + (l & 31u) * 16, last = stride - 16;
+        const uint32_t col0 = s * kThinBytes + l % kChunks * 16, last = stride - 16;
 #pragma unroll
         for (uint32_t i = 0; i < kWLoads + kXLoads; ++i) {
             const bool ofw = i < kWLoads;
-            const uint32_t r = (ofw ? (wave * kWLoads + i) : (wave * kXLoads + i - kWLoads)) * 2 + (l >> 5);
+            const uint32_t at = ofw ? wave * kWLoads + i : wave * kXLoads + i - kWLoads;
+            const uint32_t r = at * kLoadRows + l / kChunks;
             const uint32_t end = ofw ? wend : xend, col = col0 ^ ((r & 15u) * 16);
             dma_to_lds(ofw ? w0 : a.x, (r < end ? r : end) * stride + (col < last ? col : last),
-                       lds0 + buffer * kStage + (ofw ? wave * kWLoads + i : kThinRows / 2 + wave * kXLoads + i - kWLoads) * 1024);
+                       lds0 + buffer * kStage + ((ofw ? 0 : kThinRows / kLoadRows) + at) * 1024);
         }
-        dma_word_to_lds(words + uint64_t(s) * 4, word, sc0 + buffer * (kThinRows + 64) * 4);
+        dma_word_to_lds(words + uint64_t(s * kThinBlocks / 4) * 4, word, sc0 + buffer * (kThinRows + 64) * 4);
     };
     const uint32_t fr = l & 15u, fg = l >> 4;
     v4f_t acc[kFM] = {};
@@ -499,7 +501,8 @@ __global__ void __launch_bounds__(256) f8_thin_kernel(F8MatmulArgs a)
                 const uint8_t* p = t + (row + fr) * kThinBytes;  // chunks at chunk ^ (row & 15)
                 Operand<kWide> o;
                 o.set(*reinterpret_cast<const uint4*>(p + (((8 * d + fg) ^ fr) * 16)),
-                      *reinterpret_cast<const uint4*>(p + (((8 * d + fg + 4) ^ fr) * 16)), scale >> (8 * d));
+                      *reinterpret_cast<const uint4*>(p + (((8 * d + fg + 4) ^ fr) * 16)),
+                      scale >> (8 * ((s * kThinBlocks + d) & 3u)));
                 return o;
             };
             const Operand<kWide> w = fragment(wave * 16, sw);
@@ -547,8 +550,11 @@ constexpr uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t bm, uint64_t bn)
 Cut cut_product(uint64_t m, uint64_t n, uint64_t k, bool wide)
 {
     if (m <= 64) {
-        // a workgroup a CU, each with two stages at least
-        const uint64_t want = 256 / tiles_of(m, n, 64, kThinRows), most = f8_blocks(k) / (2 * kThinBlocks);
+        // Split where that brings two workgroups to a CU that would have none or one, each with
+        // 8 blocks at least: the join costs a launch (one token: 4096 x 16384 weights 20.7 us
+        // in 256 workgroups, 18.5 in 512; 12345 x 5000 in 193 14.2, in 386 16.8).
+        const uint64_t tiles = tiles_of(m, n, 64, kThinRows);
+        const uint64_t want = tiles >= 160 ? 1 : 512 / tiles, most = f8_blocks(k) / 8;
         const uint64_t splits = want < most ? want : most;
         return {kThin, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits))};
     }
