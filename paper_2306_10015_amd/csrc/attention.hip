@@ -19,10 +19,13 @@
 // product wants its operand, with the keys in an order that its other operand, the
 // values, follows: no exchange between lanes. The values' operand needs the columns
 // of the tile: ds_read_b64_tr_b16 transposes 4 keys x 16 columns at a time (bf16);
-// for fp32 the instruction takes one key a lane and a column read does.
-// All sums are fp32. bf16: probabilities are rounded to bf16 for the product with
-// the values (as large an error as the output's own rounding), l sums them
-// unrounded. fp32: v_mfma_f32_32x32x2_f32, exact products of fp32.
+// fp32 reads them one by one.
+// All sums are fp32, on v_mfma_f32_32x32x16_bf16. bf16: probabilities are rounded to
+// bf16 for the product with the values (as large an error as the output's own
+// rounding), l sums them unrounded. fp32: every operand is split into three bf16
+// (exactly), and six of the nine products are summed, all above 2^-24 of the whole:
+// 192 cycles for 16 columns where v_mfma_f32_32x32x2_f32 takes 512. A value so large
+// that its first part is infinite gives NaN, see below.
 //
 // The rows of a tile are (query, head) pairs of the heads that share a key/value
 // head, so these read it once. Two shapes of workgroup:
@@ -224,6 +227,35 @@ __device__ __forceinline__ void careful_row(const AttentionArgs& a, const Docume
     if (l == 0) store_lse(a, token, h, m, sum);
 }
 
+// A float as the sum of three bf16: its 24 bits in 8 and 8 and 8.
+struct Split {
+    v8bf_t h, m, l;
+};
+
+__device__ __forceinline__ Split split(const float (&x)[8])
+{
+    Split s;
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+        s.h[i] = static_cast<__bf16>(x[i]);
+        const float r = x[i] - static_cast<float>(s.h[i]);
+        s.m[i] = static_cast<__bf16>(r);
+        s.l[i] = static_cast<__bf16>(r - static_cast<float>(s.m[i]));
+    }
+    return s;
+}
+
+// c + a b of split operands, but for the terms below 2^-24 of the largest.
+__device__ __forceinline__ v16f_t product(const Split& a, const Split& b, v16f_t c)
+{
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.m, b.m, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.l, b.h, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.h, b.l, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.m, b.h, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.h, b.m, c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.h, b.h, c, 0, 0, 0);
+}
+
 // The tile of one type and padded head size: how it lies in LDS and what the
 // matrix instructions take from it.
 template <bool kF, uint32_t kD>
@@ -232,13 +264,14 @@ struct Tile {
     static constexpr uint32_t kRow = kD * kElement;     // bytes of a key's row
     static constexpr uint32_t kChunks = kRow / 16;
     static constexpr uint32_t kLoadRows = 1024 / kRow;  // rows of one load of a wave
-    static constexpr uint32_t kQ = kD * kElement / 2 / 16;  // 16-byte operands of a lane's half row
+    static constexpr uint32_t kQ = kD / 16;             // operands of a row: 16 columns each
+    using Operand = std::conditional_t<kF, Split, v8bf_t>;
 
     // The order of a row's chunks in LDS, such that the lanes that read together read
     // different banks (64 of 4 bytes): of K 16 rows at one chunk, of V (bf16) 4 rows at 64
-    // bytes. Both patterns return every kPeriod rows (for 512-byte rows, where the matrix
-    // instructions take far longer than the reads, as often as a wave's loads do).
-    static constexpr uint32_t kPeriod = kRow == 512 ? 8 : 16;
+    // bytes. Both patterns return every kPeriod rows (for fp32, which reads less in the time
+    // of its matrix instructions, as often as a wave's loads do).
+    static constexpr uint32_t kPeriod = kF ? 8 : 16;
     static __device__ __forceinline__ uint32_t k_swizzle(uint32_t row)
     {
         return kChunks >= 16 ? row & (kPeriod - 1) : (row >> 1) & 7u;
@@ -249,22 +282,46 @@ struct Tile {
         return kChunks >= 16 ? (row & 3u) << 2 : (row & 2u) << 1;
     }
 
+    // Columns 16 c + 8 (l / 32) .. + 7 of the query at `at` that exist (dim of them).
+    static __device__ __forceinline__ Operand query(uint64_t at, uint32_t c, uint32_t dim, uint32_t l)
+    {
+        u32x4_t w[kElement / 2];
+#pragma unroll
+        for (uint32_t e = 0; e < kElement / 2; ++e) {
+            const uint32_t byte = (c * 16 + (l >> 5) * 8) * kElement + e * 16;
+            w[e] = u32x4_t{0, 0, 0, 0};
+            if (byte < dim * kElement) w[e] = *reinterpret_cast<const gu32x4_t*>(at + byte);
+        }
+        if constexpr (kF) {
+            float x[8];
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e) x[e] = __uint_as_float(w[e / 4][e % 4]);
+            return split(x);
+        } else {
+            return __builtin_bit_cast(v8bf_t, w[0]);
+        }
+    }
+
     // s + 32 keys (from row of K's stage) x 32 queries
-    static __device__ __forceinline__ v16f_t scores(const uint8_t* k, uint32_t row, const u32x4_t (&q)[kQ], uint32_t l,
+    static __device__ __forceinline__ v16f_t scores(const uint8_t* k, uint32_t row, const Operand (&q)[kQ], uint32_t l,
                                                     v16f_t s)
     {
         const uint32_t r = row + (l & 31u);
+        auto chunk = [&](uint32_t i) { return *reinterpret_cast<const u32x4_t*>(k + r * kRow + ((i ^ k_swizzle(r)) * 16)); };
 #pragma unroll
         for (uint32_t c = 0; c < kQ; ++c) {
-            const u32x4_t w =
-                *reinterpret_cast<const u32x4_t*>(k + r * kRow + (((2 * c + (l >> 5)) ^ k_swizzle(r)) * 16));
             if constexpr (kF) {
-                const v4f_t kv = __builtin_bit_cast(v4f_t, w), qv = __builtin_bit_cast(v4f_t, q[c]);
+                const u32x4_t lo = chunk(4 * c + 2 * (l >> 5)), hi = chunk(4 * c + 2 * (l >> 5) + 1);
+                float x[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[e], qv[e], s, 0, 0, 0);
+                for (uint32_t e = 0; e < 4; ++e) {
+                    x[e] = __uint_as_float(lo[e]);
+                    x[e + 4] = __uint_as_float(hi[e]);
+                }
+                s = product(split(x), q[c], s);
             } else {
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf_t, w),
-                                                            __builtin_bit_cast(v8bf_t, q[c]), s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf_t, chunk(2 * c + (l >> 5))), q[c], s,
+                                                            0, 0, 0);
             }
         }
         return s;
@@ -276,12 +333,20 @@ struct Tile {
     {
         if constexpr (kF) {
 #pragma unroll
-            for (uint32_t i = 0; i < 16; ++i) {
-                const uint32_t r = row + 8 * (i >> 2) + 4 * (l >> 5) + (i & 3);
+            for (uint32_t u = 0; u < 2; ++u) {  // 16 keys an instruction, in the order below
+                float pv[8];
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) pv[j] = p[8 * u + j];
+                const Split ps = split(pv);
+                const uint32_t r = row + 16 * u + 4 * (l >> 5);
 #pragma unroll
                 for (uint32_t t = 0; t < kD / 32; ++t) {
-                    const float x = *reinterpret_cast<const float*>(v + r * kRow + (t * 32 + (l & 31u)) * 4);
-                    acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[i], acc[t], 0, 0, 0);
+                    float x[8];
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j)
+                        x[j] = *reinterpret_cast<const float*>(v + (r + 8 * (j >> 2) + (j & 3)) * kRow +
+                                                               (t * 32 + (l & 31u)) * 4);
+                    acc[t] = product(split(x), ps, acc[t]);
                 }
             }
         } else {
@@ -328,7 +393,7 @@ constexpr float kMostCap = 96.0f / kLog2e;
 template <bool kF, uint32_t kD, bool kKeys>
 constexpr uint32_t waves_per_simd()
 {
-    if (kF) return kKeys && kD > 64 ? 1 : 2;
+    if (kF) return kD > 64 ? 1 : 2;
     return kD > 64 || kKeys ? 2 : 3;
 }
 
@@ -337,7 +402,7 @@ template <bool kF, uint32_t kD, uint32_t kWaves, bool kKeys, Mode kMode>
 __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())) attention_kernel(AttentionArgs a)
 {
     using T = Tile<kF, kD>;
-    constexpr uint32_t kStage = kKeys || (kF && kD > 64) ? 32 : 64;  // keys of a stage
+    constexpr uint32_t kStage = kKeys || kF ? 32 : 64;  // keys of a stage
     constexpr uint32_t kBytes = kStage * T::kRow;
     constexpr uint32_t kSets = kKeys ? kWaves : 1;
     constexpr uint32_t kBuffers = kKeys ? 1 : 2;
@@ -378,14 +443,11 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
     const uint32_t s0 = blockIdx.z * per, s1 = a.splits == 1 || s0 + per > stages ? stages : s0 + per;
     if (a.splits > 1 && s0 >= stages) return;  // the join does not look for these
 
-    u32x4_t q[T::kQ];
+    typename T::Operand q[T::kQ];
     {
-        const uint64_t at = a.q + (d.q_first + uint64_t(i)) * a.q_token + h * a.q_head + (l >> 5) * 16;
+        const uint64_t at = a.q + (d.q_first + uint64_t(i)) * a.q_token + h * a.q_head;
 #pragma unroll
-        for (uint32_t c = 0; c < T::kQ; ++c) {
-            q[c] = u32x4_t{0, 0, 0, 0};
-            if (c * 32 + (l >> 5) * 16 < a.dim * T::kElement) q[c] = *reinterpret_cast<const gu32x4_t*>(at + c * 32);
-        }
+        for (uint32_t c = 0; c < T::kQ; ++c) q[c] = T::query(at, c, a.dim, l);
     }
     const uint64_t kbase = a.k + d.k_first * a.k_token + kvh * a.k_head;
     const uint64_t vbase = a.v + d.k_first * a.v_token + kvh * a.v_head;

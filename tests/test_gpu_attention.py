@@ -355,3 +355,21 @@ def test_refusals(mz):
         mz.Documents(docs.table.int(), 10, 10)
     empty = mz.attention(q[:0], k, v, mz.Documents.of([]))
     assert empty.shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [1e-25, 1e35])
+@pytest.mark.parametrize("nq", [1, 80])
+def test_very_small_and_very_large_values(mz, nq, size, dtype):
+    """Sums keep their digits wherever the values lie in the type's range."""
+    q, k, v = tensors(nq, 300, 4, 2, 64, dtype)
+    check(mz, q, k, v * size, table([nq], [300]))
+    check(mz, q * 1e-15, k * 1e15, v, table([nq], [300]))
+
+
+def test_values_past_the_largest_bf16(mz):
+    """fp32 values that round to no bf16: their rows are computed one by one."""
+    q, k, v = tensors(70, 70, 2, 2, 64, "f32")
+    v[40, 0, 5] = 3.4e38
+    v[41, 1] = -3.4e38
+    check(mz, q, k, v, table([70]))
