@@ -29,7 +29,7 @@
 //
 // The rows of a tile are (query, head) pairs of the heads that share a key/value
 // head, so these read it once. Two shapes of workgroup:
-//   rows: each wave has 32 rows of its own and all share stages of 64 keys;
+//   rows: each wave has 32 rows of its own and all share stages of 64 keys (fp32: 32);
 //   keys: at most 32 rows (single tokens): all waves have the same rows, each takes
 //         every kWaves-th stage of 32 keys through LDS of its own, without barriers,
 //         and they join at the end. One buffer for K and one for V: K of the next
@@ -376,7 +376,7 @@ struct Tile {
 
 // The score functions that have a loop of their own in the bf16 kernels by rows, which
 // the vector instructions of the softmax bound (the others use kGeneral: fp32 is bound by
-// its matrix instructions, calls by keys by memory). Per score, in issue slots of a wave
+// splitting its operands, calls by keys by memory). Per score, in issue slots of a wave
 // (4 cycles, a transcendental 8): plain and biased 5.5, capped 11; general 8 to 15.
 //  kPlain:  no cap, no bias, scale > 0: the maximum is taken of the products themselves,
 //           and one fma scales a product and subtracts the reference.
@@ -531,9 +531,6 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
         const uint8_t* kt = lds[kKeys ? wave : 0][b][0];
         const uint8_t* vt = lds[kKeys ? wave : 0][b][1];
         const bool edge = k0 + int(kStage) > low;  // some query of the wave does not see them all
-        // fp32: the matrix instructions bound it, so the halves of a stage that no query of
-        // the wave sees are left out; for bf16 the branches would cost more than that saves
-        auto hidden = [&](uint32_t t) { return kF && k0 + int(t * 32) >= high; };
         {
             constexpr uint32_t kT = kStage / 32;
             v16f_t x[kT];
@@ -541,7 +538,6 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
             float top = kLowest;
 #pragma unroll
             for (uint32_t t = 0; t < kT; ++t) {
-                if (hidden(t)) continue;
                 x[t] = T::scores(kt, t * 32, q, l, bias);
                 if constexpr (kKeys) {
                     lds_wait();  // K's buffer is read: the next stage's loads under the rest of this one
@@ -554,7 +550,6 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
                 const int key = k0 + int(t * 32 + 4 * (l >> 5));
                 const float from = float(pos - key);
                 off[t] = 0.0f;
-                if (hidden(t)) continue;
                 if constexpr (kMode == kCapped) {
 #pragma unroll
                     for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped<kF>(sc, x[t][e]);
@@ -631,7 +626,6 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
 #pragma unroll
             for (uint32_t t = 0; t < kT; ++t) {
                 const float ref = m - off[t];
-                if (hidden(t)) continue;
 #pragma unroll
                 for (uint32_t e = 0; e < 16; ++e) {
                     if constexpr (kMode == kPlain || kMode == kBiased)
