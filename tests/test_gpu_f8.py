@@ -91,6 +91,22 @@ def test_quantize_extremes(mz):
     check_quantized(mz, torch.from_numpy(w).cuda(), w)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantize_every_exponent(mz, dtype):
+    """Rows whose largest exponent field runs from subnormal to the top, with
+    elements down to 2^-20 of it and, in bf16, every tie between two codes."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(11))
+    top = np.arange(255)[:, None]
+    exponent = np.maximum(top - rng.integers(0, 20, (255, 512)), 0)
+    bits = (rng.integers(0, 2, (255, 512)) << 31 | exponent << 23 | rng.integers(0, 1 << 23, (255, 512)))
+    if dtype == "bf16":
+        bits &= 0xFFFF0000
+    w = bits.astype(np.uint32).view(np.float32)
+    dev = torch.from_numpy(w).cuda()
+    check_quantized(mz, dev.bfloat16() if dtype == "bf16" else dev, w)
+
+
 def test_quantize_into_writes_the_padding(mz):
     import torch
     w = torch.from_numpy(values(6, 130, 4))
