@@ -817,10 +817,16 @@ AttentionPlan plan_attention(uint32_t docs, uint32_t heads, uint32_t kv_heads, u
     const uint64_t tiles = by_keys(rows) ? 1 : (rows + 127) / 128;
     const uint64_t groups = uint64_t(docs) * kv_heads * tiles;
     // Split where the groups alone leave CUs idle, into chunks of keys rather than parts
-    // of a document: documents of any length then give equal work.
+    // of a document: documents of any length then give equal work. A few rows leave little
+    // behind for the join, and eight workgroups a CU keep the memory busy. Of many rows the
+    // join costs as much as 256 keys do, so they are split where there are fewer groups
+    // than CUs, to two a CU (against the former rule for both: 8 documents of 512 tokens,
+    // 16 heads of 64, 52 -> 16 us; 2048 tokens, 32 heads of 128, 102 -> 62; 64 tokens over
+    // 16000 keys, 32 heads of 128, 91 -> 57; fp32, 2048 tokens, 12 heads of 64, 87 -> 97).
     AttentionPlan p = {1, 64, 0};
-    if (groups >= 1024 || max_k <= 256) return p;
-    uint64_t chunk = (max_k * groups / 2048 + 63) / 64 * 64;
+    const uint64_t wanted = by_keys(rows) ? 2048 : 512;
+    if (groups >= wanted / 2 || max_k <= 256) return p;
+    uint64_t chunk = (max_k * groups / wanted + 63) / 64 * 64;
     chunk = chunk < 256 ? 256 : chunk;
     while ((max_k + chunk - 1) / chunk > 64) chunk += 64;
     const uint64_t splits = (max_k + chunk - 1) / chunk, kept = splits * docs * max_q * heads;
