@@ -104,12 +104,14 @@ __device__ __forceinline__ int visible(const AttentionArgs& a, const Document& d
     return pos + 1 > d.prefix ? pos + 1 : d.prefix;  // pos < nk, prefix >= 0
 }
 
+constexpr float kMostCap = 96.0f / kLog2e;  // of the short form of a capped score
+
 // The score function's constants, for scores in units of log 2.
 struct Score {
     float c;      // scale log2 e
     float k, w;   // capped: x = w - 2 w / (1 + 2^(k s)), k = 2 scale log2 e / cap, w = cap log2 e
     float cap, scale;
-    bool capped;
+    bool capped, small;
 };
 
 __device__ __forceinline__ Score score_of(const AttentionArgs& a)
@@ -118,19 +120,31 @@ __device__ __forceinline__ Score score_of(const AttentionArgs& a)
     s.scale = a.scale;
     s.cap = a.softcap;
     s.capped = a.softcap > 0.0f;
+    s.small = a.softcap <= kMostCap;
     s.c = a.scale * kLog2e;
-    s.k = s.capped ? 2.0f * a.scale * kLog2e / a.softcap : 0.0f;
+    // (finite, so that a score of 0 stays 0 under the smallest caps)
+    constexpr float kLargest = 3.4e38f;
+    s.k = s.capped ? fminf(fmaxf(2.0f * a.scale * kLog2e / a.softcap, -kLargest), kLargest) : 0.0f;
     s.w = a.softcap * kLog2e;
     return s;
 }
 
-// A capped score, before the bias. fp32 takes the library's tanh: the short form's
-// error, 2^-23 cap in the exponent, is for results of bf16.
+// A capped score, before the bias, by two transcendentals. Its error is 2^-23 cap, since
+// 1 + 2^(k x) keeps no more of x: for results of bf16 and caps up to kMostCap.
+__device__ __forceinline__ float capped_short(const Score& s, float x)
+{
+    return __builtin_fmaf(__builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * s.k)), -2.0f * s.w, s.w);
+}
+
+// The same for all types and caps. Beyond the short form's: the library's tanh, and what is
+// far below the cap as it is (tanh y is y to 2^-25 of it below 2^-12; where the cap is near
+// the largest float, y loses its digits and w passes fp32's range).
 template <bool kF>
 __device__ __forceinline__ float capped(const Score& s, float x)
 {
-    if constexpr (kF) return s.w * tanhf(x * s.scale / s.cap);
-    return __builtin_fmaf(__builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * s.k)), -2.0f * s.w, s.w);
+    if (!kF && s.small) return capped_short(s, x);  // (uniform)
+    const float y = x * s.scale / s.cap;
+    return fabsf(y) < 0x1p-12f ? x * s.c : s.cap * tanhf(y) * kLog2e;
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -386,7 +400,6 @@ struct Tile {
 //  kCapped: no bias, and a cap so small that 0 can be the reference for good: no maximum,
 //           no rescaling. 2^(+-cap log2 e) and sums of 2^24 of them stay within fp32.
 enum Mode { kGeneral, kPlain, kBiased, kCapped };
-constexpr float kMostCap = 96.0f / kLog2e;
 
 // The waves a SIMD that the registers are kept down for: what LDS allows, and as far as
 // nothing spills.
@@ -552,7 +565,7 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
                 off[t] = 0.0f;
                 if constexpr (kMode == kCapped) {
 #pragma unroll
-                    for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped<kF>(sc, x[t][e]);
+                    for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped_short(sc, x[t][e]);
                 }
                 if constexpr (kMode == kBiased) {
                     off[t] = -slope * from;

@@ -1,0 +1,86 @@
+"""Attention on the GPU at the ends of its range: caps of any size, scores and
+values near the ends of their types, split documents with every score function,
+and what tokens that are not finite cost. Against the plain reference in 64 bits
+(attention_ref.py); the bars come from the arithmetic (bounds)."""
+import math
+
+import pytest
+
+import attention_ref
+from test_gpu_attention import DTYPES, table, tensors
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mz():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a visible GPU"
+    from paper_2306_10015_amd import mezo
+    return mezo
+
+
+def bounds(out, lse, weight, q, k, dtype, keys, scale, softcap, slopes):
+    """How far out and lse may be off. With u = 2^-24: a product of dim terms is off by
+    u (dim + 8) of the sum of their sizes; a cap is applied to 16 u of the score itself
+    and, up to 66 and for bf16, to 8 u of the cap; a bias by distance to 4 u of itself;
+    the difference from the reference and exp2 to 8 u of the score. No term grows with
+    a larger cap."""
+    u = 2.0 ** -24
+    heads, dim, group = q.shape[1], q.shape[2], q.shape[1] // k.shape[1]
+    scale = 1.0 / math.sqrt(dim) if scale is None else abs(scale)
+    qa, ka = q.cpu().double().abs(), k.cpu().double().abs()
+    raw = max(float((qa[:, h] @ ka[:, h // group].t()).max()) for h in range(heads)) * scale
+    top = min(raw, softcap) if softcap else raw
+    e = u * (dim + 8) * (raw if math.isfinite(raw) else 0.0)
+    if softcap:
+        e += 16 * u * top + 8 * u * min(softcap, 66.6)
+    if slopes is not None:
+        far = float(slopes.abs().max()) * keys
+        e += 4 * u * far
+        top += far
+    e += 8 * u * top + 4 * u
+    rounding = 2.0 ** -8 if str(dtype) == "torch.bfloat16" else 0.0
+    # (results below the smallest normal number of their type keep fewer digits)
+    return ((2 * e + 2 * keys * u + rounding) * weight + (rounding + 4 * u) * out.abs() + 2.0 ** -126,
+            e + (keys * u + 8 * u) + 8 * u * lse.abs())
+
+
+def check(mz, q, k, v, rows, causal=True, scale=None, softcap=0.0, slopes=None, max_k=None):
+    import torch
+    docs = mz.Documents(torch.tensor(rows, dtype=torch.int64, device="cuda"), max(r[1] for r in rows),
+                        max(r[3] for r in rows) if max_k is None else max_k)
+    out, lse = mz.attention(q, k, v, docs, causal=causal, scale=scale, softcap=softcap, slopes=slopes, return_lse=True)
+    want, want_lse, weight = attention_ref.attention(q, k, v, rows, causal, scale, softcap, slopes)
+    ob, lb = bounds(want, want_lse, weight, q, k, q.dtype, max(r[3] for r in rows), scale, softcap, slopes)
+    off = (out.cpu().double() - want).abs()
+    assert bool((off <= ob).all()), float((off / ob).max())
+    off = (lse.cpu().double() - want_lse).abs()
+    off[lse.cpu().double() == want_lse] = 0.0  # (infinities)
+    assert bool((off <= lb).all()), float((off / lb).max())
+    return out, lse
+
+
+# ---- caps of any size ----------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cap", [1e-40, 1e-12, 0.5, 66.0, 67.0, 100.0, 1e4, 1e6, 1e8, 1e30, 3.4e38])
+@pytest.mark.parametrize("bias", [False, True])
+def test_caps_of_any_size(mz, cap, bias, dtype):
+    """A cap far above the scores leaves them as they are, one far below takes them to 0."""
+    import torch
+    slopes = torch.tensor([0.5, 0.03, 0.0, -0.01], device="cuda") if bias else None
+    q, k, v = tensors(150, 150, 4, 2, 64, dtype)
+    q = q * 3
+    k[3] = 0  # a score of 0
+    check(mz, q, k, v, table([150], prefix=[10]), softcap=cap, slopes=slopes)
+    check(mz, q[:2], k, v, table([2], [150]), softcap=cap, slopes=slopes)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cap", [100.0, 1e4, 1e8])
+def test_large_caps_and_large_scores(mz, cap, dtype):
+    """Scores of the size of the cap, where neither end of the tanh holds."""
+    q, k, v = tensors(130, 130, 2, 1, 64, dtype)
+    check(mz, q, k, v, table([130]), softcap=cap, scale=cap / 30)
+    check(mz, q[:1], k, v, table([1], [130]), softcap=cap, scale=cap / 30)
