@@ -129,20 +129,20 @@ __device__ __forceinline__ Score score_of(const AttentionArgs& a)
     return s;
 }
 
-// A capped score, before the bias, by two transcendentals. Its error is 2^-23 cap, since
-// 1 + 2^(k x) keeps no more of x: for results of bf16 and caps up to kMostCap.
-__device__ __forceinline__ float capped_short(const Score& s, float x)
+// The cap by two transcendentals: a capped score before the bias is w - 2 w r. Its error is
+// 2^-23 cap, since 1 + 2^(k x) keeps no more of x: for results of bf16 and caps up to kMostCap.
+__device__ __forceinline__ float cap_share(const Score& s, float x)
 {
-    return __builtin_fmaf(__builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * s.k)), -2.0f * s.w, s.w);
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * s.k));
 }
 
-// The same for all types and caps. Beyond the short form's: the library's tanh, and what is
+// A capped score before the bias, of all types and caps. Beyond the short form's: the library's tanh, and what is
 // far below the cap as it is (tanh y is y to 2^-25 of it below 2^-12; where the cap is near
 // the largest float, y loses its digits and w passes fp32's range).
 template <bool kF>
 __device__ __forceinline__ float capped(const Score& s, float x)
 {
-    if (!kF && s.small) return capped_short(s, x);  // (uniform)
+    if (!kF && s.small) return __builtin_fmaf(cap_share(s, x), -2.0f * s.w, s.w);  // (uniform)
     const float y = x * s.scale / s.cap;
     return fabsf(y) < 0x1p-12f ? x * s.c : s.cap * tanhf(y) * kLog2e;
 }
@@ -397,9 +397,13 @@ struct Tile {
 //  kBiased: no cap, scale > 0. Away from the diagonal the bias is linear in the key: a
 //           constant of each of a lane's 16 results, which the products are added to
 //           instead of to zero, and one term a stage, which joins the reference.
-//  kCapped: no bias, and a cap so small that 0 can be the reference for good: no maximum,
-//           no rescaling. 2^(+-cap log2 e) and sums of 2^24 of them stay within fp32.
+//  kCapped: no bias, and a cap up to kMostCap. No score can pass the cap, so the maximum is
+//           taken only until a row's reference is within kHeadroom of it (for nearly all
+//           rows that is the first stage), and the cap's last fma subtracts the reference.
+//           Terms are then at most 2^kHeadroom; a row whose sums overflow all the same
+//           (values above 2^34 after a rise of that much) is one for careful_row.
 enum Mode { kGeneral, kPlain, kBiased, kCapped };
+constexpr float kHeadroom = 80.0f;
 
 // The waves a SIMD that the registers are kept down for: what LDS allows, and as far as
 // nothing spills.
@@ -508,7 +512,8 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
     const float slope = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
     const int pos = d.nk - d.nq + i;
     v16f_t acc[kD / 32] = {};
-    float m = kMode == kCapped ? 0.0f : kLowest, sum = 0.0f;
+    float m = kLowest, sum = 0.0f;
+    [[maybe_unused]] bool watch = true;  // (of the wave) the maximum is still taken
     // the positions of the wave's first and last query
     [[maybe_unused]] const int pos0 = d.nk - d.nq + int(__builtin_amdgcn_readfirstlane(uint32_t(query(first))));
     [[maybe_unused]] const int pos1 = d.nk - d.nq + int(__builtin_amdgcn_readfirstlane(uint32_t(query(first + 31))));
@@ -565,7 +570,7 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
                 off[t] = 0.0f;
                 if constexpr (kMode == kCapped) {
 #pragma unroll
-                    for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped_short(sc, x[t][e]);
+                    for (uint32_t e = 0; e < 16; ++e) x[t][e] = cap_share(sc, x[t][e]);
                 }
                 if constexpr (kMode == kBiased) {
                     off[t] = -slope * from;
@@ -599,16 +604,24 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
                     const int left = limit - key;
 #pragma unroll
                     for (uint32_t e = 0; e < 16; ++e)
-                        if (int(8 * (e >> 2) + (e & 3)) >= left) x[t][e] = -__builtin_inff();
+                        if (int(8 * (e >> 2) + (e & 3)) >= left)
+                            x[t][e] = kMode == kCapped ? __builtin_inff() : -__builtin_inff();
                 }
-                if constexpr (kMode != kCapped) {
+                if constexpr (kMode == kCapped) {
+                    if (watch) {
+                        float least = x[t][0];
+#pragma unroll
+                        for (uint32_t e = 1; e < 16; ++e) least = fminf(least, x[t][e]);
+                        top = fmaxf(top, __builtin_fmaf(least, -2.0f * sc.w, sc.w));
+                    }
+                } else {
                     float most = x[t][0];
 #pragma unroll
                     for (uint32_t e = 1; e < 16; ++e) most = fmaxf(most, x[t][e]);
                     top = fmaxf(top, kMode == kGeneral ? most : most * sc.c + off[t]);
                 }
             }
-            if constexpr (kMode != kCapped) {
+            if (kMode != kCapped || watch) {
                 top = max_halves(top);
                 if (__any(top > m + kSlack)) {
                     const float now = fmaxf(m, top), old = exp2_fast(m - now);
@@ -619,6 +632,7 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
 #pragma unroll
                         for (uint32_t e = 0; e < 16; ++e) acc[t][e] *= old;
                 }
+                if constexpr (kMode == kCapped) watch = __any(sc.w - m > kHeadroom);
             }
             [[maybe_unused]] float factor = sc.c;
             if constexpr (kMode == kPlain || kMode == kBiased) {
@@ -639,12 +653,13 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
 #pragma unroll
             for (uint32_t t = 0; t < kT; ++t) {
                 const float ref = m - off[t];
+                [[maybe_unused]] const float room = sc.w - m;
 #pragma unroll
                 for (uint32_t e = 0; e < 16; ++e) {
                     if constexpr (kMode == kPlain || kMode == kBiased)
                         x[t][e] = exp2_fast(__builtin_fmaf(x[t][e], factor, -ref));
                     else if constexpr (kMode == kCapped)
-                        x[t][e] = exp2_fast(x[t][e]);
+                        x[t][e] = exp2_fast(__builtin_fmaf(x[t][e], -2.0f * sc.w, room));
                     else
                         x[t][e] = exp2_fast(x[t][e] - ref);
                     sum += x[t][e];

@@ -84,3 +84,33 @@ def test_large_caps_and_large_scores(mz, cap, dtype):
     q, k, v = tensors(130, 130, 2, 1, 64, dtype)
     check(mz, q, k, v, table([130]), softcap=cap, scale=cap / 30)
     check(mz, q[:1], k, v, table([1], [130]), softcap=cap, scale=cap / 30)
+
+
+# ---- values near the ends of their types ------------------------------------------
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cap", [30.0, 50.0, 66.0])
+@pytest.mark.parametrize("size", [1e-30, 1.0, 1e30])
+@pytest.mark.parametrize("sign", [-1, 1])
+def test_saturated_caps_keep_the_values_digits(mz, sign, size, cap, dtype):
+    """All scores at one end of the cap: as good a softmax as any other, for values of
+    any size."""
+    q, k, v = tensors(150, 150, 2, 2, 64, dtype)
+    q, k = q * 0.01 + 4.0, k * 0.01 + sign * 4.0
+    check(mz, q, k, v * size, table([150]), softcap=cap)
+    check(mz, q[:40], k, v[:150] * size, table([40], [150]), softcap=cap)
+    check(mz, q[:1], k, v[:150] * size, table([1], [150]), softcap=cap)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cap", [20.0, 50.0, 66.0])
+@pytest.mark.parametrize("size", [1e-30, 1.0, 1e12])
+@pytest.mark.parametrize("at", [1, 63, 64, 100, 149])
+def test_caps_from_one_end_to_the_other(mz, at, size, cap, dtype):
+    """Keys of score -cap, then one of +cap, then -cap again: the rows before it are
+    theirs, the rows after it its."""
+    q, k, v = tensors(150, 150, 2, 2, 64, dtype)
+    q, k = q * 0.01 + 4.0, k * 0.01 - 4.0
+    k[at] += 8.0
+    check(mz, q, k, v * size, table([150]), softcap=cap)
+    check(mz, q, k, v * size, table([150]), softcap=cap, causal=False)
