@@ -40,8 +40,8 @@
 //
 // A masked key takes no part whatever its value: its probability is 0, but 0 times
 // an infinite or NaN value is not. So a row whose result is not finite is computed
-// once more, from its visible keys alone (careful_row), slowly; finite inputs never
-// get there.
+// once more, from its visible keys alone (careful_row). Finite inputs get there only
+// where a sum of theirs overflows.
 #include <type_traits>
 
 #include "attention_launch.hpp"
@@ -199,33 +199,78 @@ __device__ __forceinline__ void store_lse(const AttentionArgs& a, uint64_t token
             l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// A row by its visible keys alone, k0 <= j < k1, one key after another; the whole
-// wave works on it. Lane l holds columns l and l + 64 of the accumulator.
+// A row by its visible keys alone, k0 <= j < k1, 64 at a time; the whole wave works on it.
+// A lane has a key's score, then columns l and l + 64 of the accumulator. A key that is NaN
+// to the row ends it: nothing that follows changes its result.
 template <bool kF>
 __device__ __forceinline__ void careful_row(const AttentionArgs& a, const Document& d, uint32_t doc, uint32_t kvh,
                                          uint32_t split, int i, uint32_t h, int k0, int k1)
 {
+    constexpr uint32_t kPer = kF ? 4 : 8;  // elements of 16 bytes
     const Score sc = score_of(a);
     const uint32_t l = threadIdx.x & 63u;
     const uint64_t q = a.q + (d.q_first + uint64_t(i)) * a.q_token + h * a.q_head;
     const float slope = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
     float q2[2], acc[2] = {0.0f, 0.0f}, m = kLowest, sum = 0.0f;
     for (uint32_t c = 0; c < 2; ++c) q2[c] = l + 64 * c < a.dim ? load_element<kF>(q, l + 64 * c) : 0.0f;
-    for (int j = k0; j < k1; ++j) {
-        const uint64_t key = d.k_first + uint64_t(j);
-        const uint64_t k = a.k + key * a.k_token + kvh * a.k_head, v = a.v + key * a.v_token + kvh * a.v_head;
+    for (int j0 = k0; j0 < k1; j0 += 64) {
+        const int n = k1 - j0 < 64 ? k1 - j0 : 64, j = j0 + (int(l) < n ? int(l) : n - 1);
+        const uint64_t k = a.k + (d.k_first + uint64_t(j)) * a.k_token + kvh * a.k_head;
         float s = 0.0f;
-        for (uint32_t c = 0; c < 2; ++c)
-            if (l + 64 * c < a.dim) s += q2[c] * load_element<kF>(k, l + 64 * c);
+        for (uint32_t c0 = 0; c0 < a.dim; c0 += 4 * kPer) {
+            u32x4_t w[4];
 #pragma unroll
-        for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
+            for (uint32_t u = 0; u < 4; ++u) {
+                const uint32_t c = c0 + u * kPer;
+                w[u] = u32x4_t{0, 0, 0, 0};
+                if (c < a.dim) w[u] = *reinterpret_cast<const gu32x4_t*>(k + c * (16 / kPer));
+            }
+            const uint32_t part = __float_as_uint(c0 < 64 ? q2[0] : q2[1]);
+#pragma unroll
+            for (uint32_t e = 0; e < 4 * kPer; ++e) {
+                const u32x4_t x = w[e / kPer];
+                const uint32_t bits = kF ? x[e % 4] : (e & 1 ? x[e % 8 / 2] & 0xFFFF0000u : x[e % 8 / 2] << 16);
+                s = __builtin_fmaf(__uint_as_float(__builtin_amdgcn_readlane(part, (c0 + e) & 63u)),
+                                   __uint_as_float(bits), s);
+            }
+        }
         s = sc.capped ? capped<kF>(sc, s) : s * sc.c;
         if (a.slopes) s -= slope * fabsf(float(d.nk - d.nq + i - j));
-        const float top = fmaxf(m, s), old = exp2_fast(m - top), p = exp2_fast(s - top);
+        if (int(l) >= n) s = -__builtin_inff();
+        float top = s;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+        top = fmaxf(m, top);
+        const float old = exp2_fast(m - top), p = exp2_fast(s - top);
+        float all = p;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) all += __shfl_xor(all, off);
         m = top;
-        sum = sum * old + p;
-        for (uint32_t c = 0; c < 2; ++c)
-            if (l + 64 * c < a.dim) acc[c] = acc[c] * old + p * load_element<kF>(v, l + 64 * c);
+        sum = sum * old + all;
+        if (__any(sum != sum)) {  // (of all lanes)
+            acc[0] = acc[1] = __builtin_nanf("");
+            break;
+        }
+        for (uint32_t c = 0; c < 2; ++c) acc[c] *= old;
+        const uint64_t v = a.v + (d.k_first + uint64_t(j0)) * a.v_token + kvh * a.v_head;
+        constexpr int kAhead = 8;  // loads in flight
+        for (int g = 0; g < n; g += kAhead) {
+            float x[kAhead][2];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const uint64_t at = v + uint64_t(g + u < n ? g + u : n - 1) * a.v_token;
+#pragma unroll
+                for (uint32_t c = 0; c < 2; ++c)
+                    x[u][c] = l + 64 * c < a.dim ? load_element<kF>(at, l + 64 * c) : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (g + u >= n) break;
+                const float pj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p), g + u));
+#pragma unroll
+                for (uint32_t c = 0; c < 2; ++c) acc[c] = __builtin_fmaf(pj, x[u][c], acc[c]);
+            }
+        }
     }
     const uint64_t token = d.q_first + uint64_t(i);
     if (a.splits > 1) {
@@ -768,7 +813,8 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
                     *reinterpret_cast<MEZO_GLOBAL v4bf_t*>(o + c * 2) = __builtin_convertvector(w, v4bf_t);
             }
     }
-    if (kKeys && wave > 0) return;
+    // (by keys all waves have the same rows: each takes its share of these)
+    if constexpr (kKeys) again &= (0xFFFFFFFFu / ((1u << kWaves) - 1)) << wave;
     while (again) {
         const uint32_t lane = uint32_t(__builtin_ctz(again));
         again &= again - 1;

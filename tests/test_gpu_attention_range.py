@@ -114,3 +114,45 @@ def test_caps_from_one_end_to_the_other(mz, at, size, cap, dtype):
     k[at] += 8.0
     check(mz, q, k, v * size, table([150]), softcap=cap)
     check(mz, q, k, v * size, table([150]), softcap=cap, causal=False)
+
+
+# ---- tokens that are not finite: what they cost -----------------------------------
+
+def seconds(call, passes=5):
+    import torch
+    call()
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start.record()
+    for _ in range(passes):
+        call()
+    end.record()
+    end.synchronize()
+    return start.elapsed_time(end) / 1000 / passes
+
+
+@pytest.mark.parametrize("which,most", [("q", 40), ("k", 40), ("v", 400)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_tokens_that_are_not_finite_do_not_stall_a_pass(mz, bad, which, most):
+    """A token that every row sees (or every query) is not finite, as when a model
+    diverges, and every row is computed a second time. Queries and keys: a row ends at
+    its first 64 keys, a few us of latency for each of a wave's 32 rows, where the pass
+    takes 30 us or so. Values: about 15 instructions of a wave a row and key, where the
+    pass has one for 7 rows and keys, and little to hide their latency behind."""
+    import torch
+    q, k, v = tensors(2048, 2048, 8, 8, 64, "bf16")
+    docs = mz.Documents.of([2048])
+    clean = seconds(lambda: mz.attention(q, k, v, docs))
+    if which == "q":
+        q[:, :, 5] = bad
+    else:
+        (k if which == "k" else v)[0, :, 5] = bad
+    spent = seconds(lambda: mz.attention(q, k, v, docs))
+    print(f"clean {clean * 1e6:.0f} us, {which} {bad}: {spent * 1e6:.0f} us")
+    out = mz.attention(q, k, v, docs).float()
+    if which != "v" and bad > 0:  # (a score of -inf takes no part)
+        out = out[~torch.isfinite(out).all(2)]
+        assert len(out) > 0
+    assert not bool(torch.isfinite(out[..., 5]).any())
+    if which == "v":
+        assert bool(torch.isfinite(out[..., :5]).all())
+    assert spent <= most * clean
