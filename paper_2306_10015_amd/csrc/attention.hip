@@ -435,7 +435,9 @@ struct Tile {
 
 // The score functions that have a loop of their own in the bf16 kernels by rows, which
 // the vector instructions of the softmax bound (the others use kGeneral: fp32 is bound by
-// splitting its operands, calls by keys by memory). Per score, in issue slots of a wave
+// splitting its operands, calls by keys by memory; but the code of tanh, even where it is not
+// run, costs fp32 3%, so uncapped scores have kUncapped there: 16 documents of 50 to 2048
+// tokens, 16 heads of 128, 1242 -> 1202 us). Per score, in issue slots of a wave
 // (4 cycles, a transcendental 8): plain and biased 5.5, capped 11; general 8 to 15.
 //  kPlain:  no cap, no bias, scale > 0: the maximum is taken of the products themselves,
 //           and one fma scales a product and subtracts the reference.
@@ -447,7 +449,7 @@ struct Tile {
 //           rows that is the first stage), and the cap's last fma subtracts the reference.
 //           Terms are then at most 2^kHeadroom; a row whose sums overflow all the same
 //           (values above 2^34 after a rise of that much) is one for careful_row.
-enum Mode { kGeneral, kPlain, kBiased, kCapped };
+enum Mode { kGeneral, kPlain, kBiased, kCapped, kUncapped };
 constexpr float kHeadroom = 80.0f;
 
 // The waves a SIMD that the registers are kept down for: what LDS allows, and as far as
@@ -631,8 +633,8 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
                                                      x[t][e] - bias[e]);
                     }
                 }
-                if constexpr (kMode == kGeneral) {
-                    if (sc.capped) {
+                if constexpr (kMode == kGeneral || kMode == kUncapped) {
+                    if (kMode == kGeneral && sc.capped) {
 #pragma unroll
                         for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped<kF>(sc, x[t][e]);
                     } else {
@@ -663,7 +665,7 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
                     float most = x[t][0];
 #pragma unroll
                     for (uint32_t e = 1; e < 16; ++e) most = fmaxf(most, x[t][e]);
-                    top = fmaxf(top, kMode == kGeneral ? most : most * sc.c + off[t]);
+                    top = fmaxf(top, kMode == kGeneral || kMode == kUncapped ? most : most * sc.c + off[t]);
                 }
             }
             if (kMode != kCapped || watch) {
@@ -929,6 +931,8 @@ hipError_t launch(AttentionArgs a, hipStream_t stream)
             f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kBiased>);
         else if (a.softcap > 0.0f && a.softcap <= kMostCap && !a.slopes)
             f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kCapped>);
+    } else if (a.softcap == 0.0f) {
+        f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kUncapped>);
     }
     const hipError_t e = hipLaunchKernel(f, grid, dim3(keys ? kKeyWaves * 64 : 256), params, 0, stream);
     if (e != hipSuccess || a.splits == 1) return e;
