@@ -41,7 +41,7 @@
 // A masked key takes no part whatever its value: its probability is 0, but 0 times
 // an infinite or NaN value is not. So a row whose result is not finite is computed
 // once more, from its visible keys alone (careful_row). Finite inputs get there only
-// where a sum of theirs overflows.
+// where their scores or a sum of theirs leave fp32's range.
 #include <type_traits>
 
 #include "attention_launch.hpp"
@@ -136,15 +136,21 @@ __device__ __forceinline__ float cap_share(const Score& s, float x)
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * s.k));
 }
 
-// A capped score before the bias, of all types and caps. Beyond the short form's: the library's tanh, and what is
-// far below the cap as it is (tanh y is y to 2^-25 of it below 2^-12; where the cap is near
-// the largest float, y loses its digits and w passes fp32's range).
+// A capped score before the bias, of any cap, in its own units. By the library's tanh, and
+// what is far below the cap as it is (tanh y is y to 2^-25 of it below 2^-12; y itself loses
+// digits where the cap is near the largest float).
+__device__ __forceinline__ float capped_any(const Score& s, float x)
+{
+    const float y = x * s.scale / s.cap;
+    return fabsf(y) < 0x1p-12f ? x * s.scale : s.cap * tanhf(y);
+}
+
+// The same in units of log 2, by the short form where that will do.
 template <bool kF>
 __device__ __forceinline__ float capped(const Score& s, float x)
 {
     if (!kF && s.small) return __builtin_fmaf(cap_share(s, x), -2.0f * s.w, s.w);  // (uniform)
-    const float y = x * s.scale / s.cap;
-    return fabsf(y) < 0x1p-12f ? x * s.c : s.cap * tanhf(y) * kLog2e;
+    return capped_any(s, x) * kLog2e;
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -178,8 +184,9 @@ __device__ __forceinline__ void store_element(uint64_t addr, uint32_t i, float x
         reinterpret_cast<MEZO_GLOBAL __bf16*>(addr)[i] = static_cast<__bf16>(x);
 }
 
-// Where row (i, h) of a document keeps what a split of its keys found: (m, l), and
-// the accumulator, dim floats.
+// Where row (i, h) of a document keeps what a split of its keys found: (m, l), m in the
+// scores' own units and -inf where no key was seen, and the accumulator, dim floats; with
+// -l in the place of l, the accumulator is divided by l.
 struct PartialRow {
     uint64_t stats, acc;
 };
@@ -192,16 +199,18 @@ __device__ __forceinline__ PartialRow partial_row(const AttentionArgs& a, uint32
     return {a.partial + at * 8, a.partial + (a.splits * rows + 1) / 2 * 16 + at * a.dim * 4};
 }
 
-__device__ __forceinline__ void store_lse(const AttentionArgs& a, uint64_t token, uint32_t h, float m, float l)
+// lse = m + ln l (-inf where l is 0)
+__device__ __forceinline__ void store_lse(const AttentionArgs& a, uint64_t token, uint32_t h, float m, float ln_l)
 {
-    if (a.lse)
-        reinterpret_cast<gfloat_t*>(a.lse)[token * a.heads + h] =
-            l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    if (a.lse) reinterpret_cast<gfloat_t*>(a.lse)[token * a.heads + h] = ln_l == -__builtin_inff() ? ln_l : m + ln_l;
 }
 
 // A row by its visible keys alone, k0 <= j < k1, 64 at a time; the whole wave works on it.
-// A lane has a key's score, then columns l and l + 64 of the accumulator. A key that is NaN
-// to the row ends it: nothing that follows changes its result.
+// A lane has a key's score, then columns l and l + 64 of the accumulator. Where the other
+// kernels' arithmetic leaves fp32's range this one's does not: scores are in their own units
+// (in those of log 2 the largest floats are too large), and the accumulator is the mean of
+// the values so far, never more than the largest of them. A key that is NaN to the row ends
+// it: nothing that follows changes its result.
 template <bool kF>
 __device__ __forceinline__ void careful_row(const AttentionArgs& a, const Document& d, uint32_t doc, uint32_t kvh,
                                          uint32_t split, int i, uint32_t h, int k0, int k1)
@@ -210,8 +219,8 @@ __device__ __forceinline__ void careful_row(const AttentionArgs& a, const Docume
     const Score sc = score_of(a);
     const uint32_t l = threadIdx.x & 63u;
     const uint64_t q = a.q + (d.q_first + uint64_t(i)) * a.q_token + h * a.q_head;
-    const float slope = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
-    float q2[2], acc[2] = {0.0f, 0.0f}, m = kLowest, sum = 0.0f;
+    const float slope = a.slopes ? a.slopes[h] : 0.0f;
+    float q2[2], acc[2] = {0.0f, 0.0f}, m = -__builtin_inff(), sum = 0.0f;
     for (uint32_t c = 0; c < 2; ++c) q2[c] = l + 64 * c < a.dim ? load_element<kF>(q, l + 64 * c) : 0.0f;
     for (int j0 = k0; j0 < k1; j0 += 64) {
         const int n = k1 - j0 < 64 ? k1 - j0 : 64, j = j0 + (int(l) < n ? int(l) : n - 1);
@@ -234,24 +243,28 @@ __device__ __forceinline__ void careful_row(const AttentionArgs& a, const Docume
                                    __uint_as_float(bits), s);
             }
         }
-        s = sc.capped ? capped<kF>(sc, s) : s * sc.c;
+        s = sc.capped ? capped_any(sc, s) : s * sc.scale;
         if (a.slopes) s -= slope * fabsf(float(d.nk - d.nq + i - j));
         if (int(l) >= n) s = -__builtin_inff();
         float top = s;
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
         top = fmaxf(m, top);
-        const float old = exp2_fast(m - top), p = exp2_fast(s - top);
+        const float ref = top == -__builtin_inff() ? 0.0f : top;  // (all scores so far are -inf)
+        float old = exp2_fast((m - ref) * kLog2e), p = exp2_fast((s - ref) * kLog2e);
         float all = p;
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) all += __shfl_xor(all, off);
         m = top;
-        sum = sum * old + all;
+        old *= sum;
+        sum = old + all;
         if (__any(sum != sum)) {  // (of all lanes)
             acc[0] = acc[1] = __builtin_nanf("");
             break;
         }
-        for (uint32_t c = 0; c < 2; ++c) acc[c] *= old;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        p *= inv;
+        for (uint32_t c = 0; c < 2; ++c) acc[c] *= old * inv;
         const uint64_t v = a.v + (d.k_first + uint64_t(j0)) * a.v_token + kvh * a.v_head;
         constexpr int kAhead = 8;  // loads in flight
         for (int g = 0; g < n; g += kAhead) {
@@ -275,15 +288,14 @@ __device__ __forceinline__ void careful_row(const AttentionArgs& a, const Docume
     const uint64_t token = d.q_first + uint64_t(i);
     if (a.splits > 1) {
         const PartialRow p = partial_row(a, split, doc, i, h);
-        if (l == 0) *reinterpret_cast<MEZO_GLOBAL v2f_t*>(p.stats) = v2f_t{m, sum};
+        if (l == 0) *reinterpret_cast<MEZO_GLOBAL v2f_t*>(p.stats) = v2f_t{m, -sum};
         for (uint32_t c = 0; c < 2; ++c)
             if (l + 64 * c < a.dim) reinterpret_cast<gfloat_t*>(p.acc)[l + 64 * c] = acc[c];
         return;
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     for (uint32_t c = 0; c < 2; ++c)
-        if (l + 64 * c < a.dim) store_element<kF>(a.out + token * a.o_token + h * a.o_head, l + 64 * c, acc[c] * inv);
-    if (l == 0) store_lse(a, token, h, m, sum);
+        if (l + 64 * c < a.dim) store_element<kF>(a.out + token * a.o_token + h * a.o_head, l + 64 * c, acc[c]);
+    if (l == 0) store_lse(a, token, h, m, logf(sum));
 }
 
 // A float as the sum of three bf16: its 24 bits in 8 and 8 and 8.
@@ -773,7 +785,8 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
 
     const bool split = a.splits > 1;
     const float inv = split ? 1.0f : (sum == 0.0f ? 0.0f : 1.0f / sum);
-    bool finite = true;
+    // a sum of 0: no key seen, or only scores below the first reference
+    bool finite = sum < __builtin_inff() && (sum > 0.0f || limit <= int(s0 * kStage));
 #pragma unroll
     for (uint32_t t = 0; t < kMine; ++t)
 #pragma unroll
@@ -795,9 +808,9 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
         const PartialRow p = partial_row(a, blockIdx.z, doc, i, h);
         if (l < 32 && t0 == 0) {
             if (split)
-                *reinterpret_cast<MEZO_GLOBAL v2f_t*>(p.stats) = v2f_t{m, sum};
+                *reinterpret_cast<MEZO_GLOBAL v2f_t*>(p.stats) = v2f_t{sum == 0.0f ? -__builtin_inff() : m * kLn2, sum};
             else
-                store_lse(a, token, h, m, sum);
+                store_lse(a, token, h, m * kLn2, __builtin_amdgcn_logf(sum) * kLn2);
         }
         const uint64_t o = a.out + token * a.o_token + h * a.o_head;
 #pragma unroll
@@ -843,7 +856,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a)
     const int limit0 = visible(a, d, i);
     const uint32_t limit = limit0 > 0 ? uint32_t(limit0) : 0;
     const uint32_t most = (limit + a.chunk - 1) / a.chunk, splits = most < a.splits ? most : a.splits;
-    float m = kLowest, sum = 0.0f;
+    float m = -__builtin_inff(), sum = 0.0f;
     if (l < splits) {
         const v2f_t s = *reinterpret_cast<const MEZO_GLOBAL v2f_t*>(partial_row(a, l, doc, i, h).stats);
         m = s.x;
@@ -853,10 +866,13 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a)
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
     // (a split without a key of this row has the sum 0 and the accumulator 0)
-    const float weight = exp2_fast(m - top);
-    sum *= weight;
+    float weight = exp2_fast((m - (top == -__builtin_inff() ? 0.0f : top)) * kLog2e);
+    const float part_sum = sum;
+    sum = fabsf(sum) * weight;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+    // (at most 1 in all: the accumulator does not overflow)
+    weight *= (sum == 0.0f ? 0.0f : 1.0f / sum) * (part_sum < 0.0f ? -part_sum : 1.0f);
     float acc[2] = {0.0f, 0.0f};
     constexpr uint32_t kAhead = 8;  // loads in flight
     for (uint32_t s0 = 0; s0 < splits; s0 += kAhead) {
@@ -876,11 +892,10 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a)
             for (uint32_t c = 0; c < 2; ++c) acc[c] += part[s][c] * w;
         }
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     const uint64_t token = d.q_first + uint64_t(i);
     for (uint32_t c = 0; c < 2; ++c)
-        if (l + 64 * c < a.dim) store_element<kF>(a.out + token * a.o_token + h * a.o_head, l + 64 * c, acc[c] * inv);
-    if (l == 0) store_lse(a, token, h, top, sum);
+        if (l + 64 * c < a.dim) store_element<kF>(a.out + token * a.o_token + h * a.o_head, l + 64 * c, acc[c]);
+    if (l == 0) store_lse(a, token, h, top, logf(sum));
 }
 
 // Few rows: the waves of a workgroup share out the keys.

@@ -156,3 +156,44 @@ def test_tokens_that_are_not_finite_do_not_stall_a_pass(mz, bad, which, most):
     if which == "v":
         assert bool(torch.isfinite(out[..., :5]).all())
     assert spent <= most * clean
+
+
+# ---- scores and values near the largest float --------------------------------------
+
+SHAPES = [(70, 70), (1, 300), (5, 300), (1, 3000), (129, 2600)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nq,nk", SHAPES)
+@pytest.mark.parametrize("size", [-3e38, -2.5e38, 2.5e38, 3e38])
+def test_scores_near_the_largest_float(mz, size, nq, nk, dtype):
+    """Scores that are finite, but not in units of log 2: a row of equal ones is the mean
+    of its values, and one that is larger takes it all."""
+    import torch
+    q, k, v = tensors(nq, nk, 2, 2, 64, dtype)
+    q.zero_()
+    k.zero_()
+    q[..., 0] = 1
+    rows = table([nq], [nk])
+    docs = mz.Documents.of([nq], [nk])
+    # a mean of up to 2600 terms rounded to bf16 each, then itself
+    bar = 2.0 ** -6 if dtype == "bf16" else 2e-4
+    for one in (False, True):
+        k[..., 0] = size
+        if one:
+            k[nk // 2, :, 0] = size * (0.9 if size < 0 else 1.1)
+        out, lse = mz.attention(q, k, v, docs, scale=1.0, return_lse=True)
+        want, want_lse, _ = attention_ref.attention(q, k, v, rows, scale=1.0)
+        assert float((out.cpu().double() - want).abs().max()) <= bar
+        assert float(((lse.cpu().double() - want_lse) / size).abs().max()) <= 1e-6
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nq,nk", SHAPES)
+@pytest.mark.parametrize("softcap", [0.0, 30.0])
+def test_values_near_the_largest_float(mz, softcap, nq, nk, dtype):
+    """A mean of values is no larger than they are."""
+    q, k, v = tensors(nq, nk, 2, 2, 64, dtype)
+    v = (v.sign() * (1 - v.abs().clamp(max=0.9)) * 3.3e38).to(v.dtype)
+    v[:, :, :8] = 3.3e38
+    check(mz, q, k, v, table([nq], [nk]), softcap=softcap)
