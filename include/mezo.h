@@ -441,9 +441,12 @@ MEZO_API int mezo_f8_linear(const void* x, uint32_t x_dtype, uint64_t ldx, const
  * key/value head h / (heads / kv_heads). Tokens of no document keep their out
  * and lse. lse (fp32 [q_tokens, heads]) may be NULL.
  *
- * max_q and max_k: no document has more queries or keys (queries past max_q
- * are left out); max_k < 2^31 - 256, max_q * heads / kv_heads < 2^23. The documents' queries must not overlap. Rows of docs that
- * point outside the arrays are cut to them. Scores and sums are fp32; with
+ * max_q and max_k: the most queries and keys of a document, by which the work is
+ * cut. Queries past max_q are left out; keys past max_k are read like the others,
+ * but by one workgroup. With max_q and max_k taken as at most q_tokens and k_tokens:
+ * max_k < 2^31 - 256, max_q * heads / kv_heads <= 65535 * 128, n_docs * kv_heads < 2^24,
+ * n_docs * max_q * heads < 2^40 (MEZO_EINVAL). The documents' queries must not overlap.
+ * Rows of docs that point outside the arrays are cut to them. Scores and sums are fp32; with
  * MEZO_BF16 each probability is rounded to bf16 before it multiplies v.
  *
  * heads a multiple of kv_heads, heads <= MEZO_ATTENTION_MAX_HEADS, dim a

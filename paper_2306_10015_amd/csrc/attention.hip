@@ -514,9 +514,9 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
     // (a wave without a row has nothing to do but to load its part of the stages)
     const int low = seen(first), high = first < tile1 ? seen(first + 31) : 0, last = seen(tile1 - 1);
 
-    // the stages of this split of the workgroup's keys
+    // the stages of this split of the workgroup's keys (the last one takes those past max_k)
     const uint32_t stages = (uint32_t(last) + kStage - 1) / kStage, per = a.chunk / kStage;
-    const uint32_t s0 = blockIdx.z * per, s1 = a.splits == 1 || s0 + per > stages ? stages : s0 + per;
+    const uint32_t s0 = blockIdx.z * per, s1 = blockIdx.z + 1 == a.splits || s0 + per > stages ? stages : s0 + per;
     if (a.splits > 1 && s0 >= stages) return;  // the join does not look for these
 
     typename T::Operand q[T::kQ];

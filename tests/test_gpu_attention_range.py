@@ -197,3 +197,26 @@ def test_values_near_the_largest_float(mz, softcap, nq, nk, dtype):
     v = (v.sign() * (1 - v.abs().clamp(max=0.9)) * 3.3e38).to(v.dtype)
     v[:, :, :8] = 3.3e38
     check(mz, q, k, v, table([nq], [nk]), softcap=softcap)
+
+
+# ---- split documents -----------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nq", [1, 40, 129])
+@pytest.mark.parametrize("softcap,bias,prefix", [(30.0, False, 0), (0.0, True, 0), (5.0, True, 0), (100.0, False, 0),
+                                                 (0.0, False, 2590), (30.0, False, 2590)])
+def test_split_documents_with_every_score_function(mz, softcap, bias, prefix, nq, dtype):
+    import torch
+    n = 2600
+    slopes = torch.tensor([0.1, 0.003, 0.0, -0.002], device="cuda") if bias else None
+    q, k, v = tensors(2 * nq, n + 700, 4, 2, 64, dtype)
+    check(mz, q, k, v, table([nq] * 2, [n, 700], [prefix, 0]), softcap=softcap, slopes=slopes)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nq", [1, 40, 129])
+@pytest.mark.parametrize("max_k", [100, 300, 1000])
+def test_documents_with_more_keys_than_max_k(mz, max_k, nq, dtype):
+    """max_k says how the work is cut, not what is read: the same result for any."""
+    q, k, v = tensors(nq, 2000, 4, 2, 64, dtype)
+    check(mz, q, k, v, table([nq], [2000]), max_k=max_k)
