@@ -22,10 +22,12 @@
 // fp32 reads them one by one.
 // All sums are fp32, on v_mfma_f32_32x32x16_bf16. bf16: probabilities are rounded to
 // bf16 for the product with the values (as large an error as the output's own
-// rounding), l sums them unrounded. fp32: every operand is split into three bf16
-// (exactly), and six of the nine products are summed, all above 2^-24 of the whole:
-// 192 cycles for 16 columns where v_mfma_f32_32x32x2_f32 takes 512. A value so large
-// that its first part is infinite gives NaN, see below.
+// rounding), l sums them unrounded. fp32: every operand is split into three bf16, and
+// six of the nine products are summed, all above 2^-24 of the whole: 192 cycles for 16
+// columns where v_mfma_f32_32x32x2_f32 takes 512. The split is exact down to 2^-110; of what
+// is smaller it loses up to 2^-134 (bf16's numbers end at 2^-133). In a key that is 2^-24 of
+// a score where the query is of 2^110; in the values it shows in a result below kSmallest,
+// see below. A number so large that its first part is infinite gives NaN, see below.
 //
 // The rows of a tile are (query, head) pairs of the heads that share a key/value
 // head, so these read it once. Two shapes of workgroup:
@@ -41,7 +43,9 @@
 // A masked key takes no part whatever its value: its probability is 0, but 0 times
 // an infinite or NaN value is not. So a row whose result is not finite is computed
 // once more, from its visible keys alone (careful_row). Finite inputs get there only
-// where their scores or a sum of theirs leave fp32's range.
+// where their scores or a sum of theirs leave fp32's range, or where a result in fp32
+// is so small (but not 0) that the values' split may show in it: multiplying each value
+// by 2^16 before the split would do as well, for 2 to 4% of the time of all calls.
 #include <type_traits>
 
 #include "attention_launch.hpp"
@@ -62,6 +66,7 @@ constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLowest = -3.0e38f;  // a reference below every score that counts
 constexpr float kSlack = 8.0f;
+constexpr float kSmallest = 0x1p-110f;  // of fp32 results
 constexpr uint64_t kMostTokens = (1u << 31) - 256;  // of a document
 
 struct Document {
@@ -785,17 +790,22 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
 
     const bool split = a.splits > 1;
     const float inv = split ? 1.0f : (sum == 0.0f ? 0.0f : 1.0f / sum);
-    // a sum of 0: no key seen, or only scores below the first reference
-    bool finite = sum < __builtin_inff() && (sum > 0.0f || limit <= int(s0 * kStage));
+    float zero = 0.0f;  // NaN once a result is not finite
+    [[maybe_unused]] float least = __builtin_inff();  // the smallest that is not 0
 #pragma unroll
     for (uint32_t t = 0; t < kMine; ++t)
 #pragma unroll
         for (uint32_t e = 0; e < 16; ++e) {
             mine[t][e] *= inv;
-            finite = finite && fabsf(mine[t][e]) < __builtin_inff();
+            const float size = fabsf(mine[t][e]);
+            zero = __builtin_fmaf(size, 0.0f, zero);
+            if constexpr (kF) least = fminf(least, size == 0.0f ? __builtin_inff() : size);
         }
-    // rows that are not finite in some column
-    uint64_t bad = __ballot(valid && !finite);
+    // a sum of 0: no key seen, or only scores below the first reference
+    bool good = zero == 0.0f && sum < __builtin_inff() && (sum > 0.0f || limit <= int(s0 * kStage));
+    if constexpr (kF) good = good && least >= (split ? kSmallest * sum : kSmallest);  // (a split's are not divided yet)
+    // rows that are not good in some column
+    uint64_t bad = __ballot(valid && !good);
     uint32_t again = uint32_t(bad | (bad >> 32));
     if constexpr (kKeys) {
         if (again && l == 0) atomicOr(&bad_rows, again);
@@ -830,7 +840,7 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
     }
     // (by keys all waves have the same rows: each takes its share of these)
     if constexpr (kKeys) again &= (0xFFFFFFFFu / ((1u << kWaves) - 1)) << wave;
-    while (again) {
+    while (__builtin_expect(again != 0, 0)) {
         const uint32_t lane = uint32_t(__builtin_ctz(again));
         again &= again - 1;
         const int ri = query(first + lane);
