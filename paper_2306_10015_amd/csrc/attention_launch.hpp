@@ -31,7 +31,7 @@ struct AttentionPlan {
     uint64_t workspace;
 };
 AttentionPlan plan_attention(uint32_t docs, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t max_q,
-                             uint32_t max_k, uint32_t dtype);
+                             uint32_t max_k);
 
 hipError_t launch_attention(const AttentionArgs& args, hipStream_t stream);
 

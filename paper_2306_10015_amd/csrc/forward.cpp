@@ -189,7 +189,7 @@ bool attention_fits(const mezo_attention_t& a)
 mezo::AttentionPlan attention_plan(const mezo_attention_t& a)
 {
     return mezo::plan_attention(a.n_docs, a.heads, a.kv_heads, a.dim, static_cast<uint32_t>(most_q(a)),
-                                static_cast<uint32_t>(most_k(a)), a.dtype);
+                                static_cast<uint32_t>(most_k(a)));
 }
 
 int attention(const mezo_attention_t* p, void* workspace, uint64_t workspace_bytes, void* stream)
