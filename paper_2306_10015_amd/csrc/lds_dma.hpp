@@ -13,25 +13,14 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p)
     return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)(p)));
 }
 
-// Start a load of 16 bytes a lane: lane l's go from its addr to LDS byte
-// lds + 16 l (lds is the wave's, uniform). The instruction is written out because
-// after the builtin the compiler waits for every such load before the next LDS
-// read of the kernel, also of another buffer, which undoes the overlap of loads
+// Start a load of 16 bytes a lane: lane l's go from base + its offset to LDS byte
+// lds + 16 l (base and lds are the wave's, uniform). The instruction is written out
+// because after the builtin the compiler waits for every such load before the next
+// LDS read of the kernel, also of another buffer, which undoes the overlap of loads
 // with the work on the stage before. It has no result register, so nothing but
 // the LDS bytes is in flight: dma_wait() before they are read. m0 is a reserved
 // register: the compiler sets it right before each use of its own and keeps
 // nothing in it.
-__device__ __forceinline__ void dma_to_lds(uint64_t addr, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %1\n\t"
-                 "s_nop 0\n\t"
-                 "global_load_lds_dwordx4 %0, off"
-                 :
-                 : "v"(addr), "s"(__builtin_amdgcn_readfirstlane(lds))
-                 : "memory");
-}
-
-// The same with the address as a uniform base and a lane's 32-bit offset.
 __device__ __forceinline__ void dma_to_lds(uint64_t base, uint32_t offset, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %2\n\t"
