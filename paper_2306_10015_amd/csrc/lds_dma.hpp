@@ -20,13 +20,17 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p)
 // with the work on the stage before. It has no result register, so nothing but
 // the LDS bytes is in flight: dma_wait() before they are read. m0 is a reserved
 // register: the compiler sets it right before each use of its own and keeps
-// nothing in it.
+// nothing in it. The copy of base gives m0 its wait state, and it is what makes the load
+// safe wherever base comes from: a memory instruction may read a scalar register that a
+// vector instruction wrote (v_readfirstlane_b32) only five wait states later, which the
+// compiler does not see to in here; a scalar instruction waits by itself.
 __device__ __forceinline__ void dma_to_lds(uint64_t base, uint32_t offset, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %2\n\t"
-                 "s_nop 0\n\t"
-                 "global_load_lds_dwordx4 %0, %1"
-                 :
+    uint64_t at;
+    asm volatile("s_mov_b32 m0, %3\n\t"
+                 "s_mov_b64 %0, %2\n\t"
+                 "global_load_lds_dwordx4 %1, %0"
+                 : "=&s"(at)
                  : "v"(offset), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds))
                  : "memory");
 }
@@ -34,10 +38,11 @@ __device__ __forceinline__ void dma_to_lds(uint64_t base, uint32_t offset, uint3
 // 4 bytes a lane: lane l's go to LDS byte lds + 4 l.
 __device__ __forceinline__ void dma_word_to_lds(uint64_t base, uint32_t offset, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %2\n\t"
-                 "s_nop 0\n\t"
-                 "global_load_lds_dword %0, %1"
-                 :
+    uint64_t at;
+    asm volatile("s_mov_b32 m0, %3\n\t"
+                 "s_mov_b64 %0, %2\n\t"
+                 "global_load_lds_dword %1, %0"
+                 : "=&s"(at)
                  : "v"(offset), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds))
                  : "memory");
 }
