@@ -908,38 +908,6 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a)
     if (l == 0) store_lse(a, token, h, top, logf(sum));
 }
 
-// Few rows: the waves of a workgroup share out the keys.
-bool by_keys(uint64_t rows) { return rows <= 32; }
-
-AttentionPlan plan_attention(uint32_t docs, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t max_q,
-                             uint32_t max_k)
-{
-    const uint64_t rows = uint64_t(max_q) * (heads / kv_heads);
-    const uint64_t tiles = by_keys(rows) ? 1 : (rows + 127) / 128;
-    const uint64_t groups = uint64_t(docs) * kv_heads * tiles;
-    // Split where the groups alone leave CUs idle, into chunks of keys rather than parts
-    // of a document: documents of any length then give equal work. A few rows leave little
-    // behind for the join, and eight workgroups a CU keep the memory busy. Of many rows the
-    // join costs as much as 256 keys do, so they are split where there are fewer groups
-    // than CUs, to two a CU. Against the rule of few rows for both, bf16: 8 documents of 512
-    // tokens, 16 heads of 64, 52 -> 16 us; 2048 tokens, 32 heads of 128, 102 -> 62; 64 tokens
-    // over 16000 keys, 32 heads of 128, 91 -> 57. fp32: the same three 90 -> 49, 339 -> 260,
-    // 292 -> 244, 4 documents of 1000 tokens, 16 heads of 128, 220 -> 147; single documents
-    // of few heads lose (2048 tokens, 12 heads of 64, 92 -> 102; 3000, 4 heads, 67 -> 78).
-    AttentionPlan p = {1, 64, 0};
-    const uint64_t wanted = by_keys(rows) ? 2048 : 512;
-    if (groups >= wanted / 2 || max_k <= 256) return p;
-    uint64_t chunk = (max_k * groups / wanted + 63) / 64 * 64;
-    chunk = chunk < 256 ? 256 : chunk;
-    while ((max_k + chunk - 1) / chunk > 64) chunk += 64;
-    const uint64_t splits = (max_k + chunk - 1) / chunk, kept = splits * docs * max_q * heads;
-    if (splits == 1) return p;
-    p.splits = uint32_t(splits);
-    p.chunk = uint32_t(chunk);
-    p.workspace = (kept + 1) / 2 * 16 + kept * dim * 4;
-    return p;
-}
-
 template <bool kF, uint32_t kD>
 hipError_t launch(AttentionArgs a, hipStream_t stream)
 {

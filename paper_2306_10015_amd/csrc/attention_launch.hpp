@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "plans.hpp"
+
 namespace mezo {
 
 constexpr uint32_t kMaxHeadDim = 128;
@@ -23,15 +25,6 @@ struct AttentionArgs {
     uint32_t causal, dtype;
     float scale, softcap;
 };
-
-// How a call is cut: the most workgroups that share a document's keys, the keys of
-// each, and the bytes of `partial`.
-struct AttentionPlan {
-    uint32_t splits, chunk;
-    uint64_t workspace;
-};
-AttentionPlan plan_attention(uint32_t docs, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t max_q,
-                             uint32_t max_k);
 
 hipError_t launch_attention(const AttentionArgs& args, hipStream_t stream);
 

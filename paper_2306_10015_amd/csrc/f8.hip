@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(kWM* kWN * 64) f8_matmul_kernel(F8MatmulArgs a
 // into registers would need neither LDS nor barriers, but there neighbouring lanes
 // read different rows, and the address units take such a load apart line by line:
 // 25 us for 24 activations and 16384 x 4096 weights, as slow with all weights in L2.
-constexpr uint32_t kThinRows = 64, kThinBlocks = 2, kThinBytes = kThinBlocks * 128;
+constexpr uint32_t kThinBlocks = 2, kThinBytes = kThinBlocks * 128;
 
 template <uint32_t kFM, bool kWide>
 __global__ void __launch_bounds__(256) f8_thin_kernel(F8MatmulArgs a)
@@ -609,57 +609,16 @@ __global__ void __launch_bounds__(256) f8_join_kernel(F8MatmulArgs a)
     store4<kWide>(a, whole_groups<kWide>(a), row, col, sum);
 }
 
-// The kernels, and how a product is cut into them: its tile, and the workgroups that
-// share out k.
-enum Tile8 { kThin, k64x64, k128x128, k256x256 };
-
-struct Cut {
-    Tile8 tile;
-    uint32_t splits;
-};
-
-constexpr uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t bm, uint64_t bn)
-{
-    return ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
-}
-
-Cut cut_product(uint64_t m, uint64_t n, uint64_t k, bool wide)
-{
-    if (m <= 64) {
-        // Split where that brings two workgroups to a CU that would have none or one, each with
-        // 8 blocks at least: the join costs a launch (one token: 4096 x 16384 weights 20.7 us
-        // in 256 workgroups, 18.5 in 512; 12345 x 5000 in 193 14.2, in 386 16.8).
-        const uint64_t tiles = tiles_of(m, n, 64, kThinRows);
-        const uint64_t want = tiles >= 160 ? 1 : 512 / tiles, most = f8_blocks(k) / 8;
-        const uint64_t splits = want < most ? want : most;
-        return {kThin, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits))};
-    }
-    // Rounds of workgroups over the 256 CUs, one of 256 x 256 or two of 128 x 128 each: a
-    // round of the former takes 1.8 times one of the latter (60 and 33 us at k = 4096), for
-    // twice the work. 3000 x 5000 x 4096: 56 us in 240 large tiles, 61 in 960 small ones;
-    // 300 x 50272 x 768: 36 in 394 large ones, 27 in 1179.
-    const uint64_t t128 = tiles_of(m, n, 128, 128);
-    const uint64_t rounds128 = (t128 + 511) / 512, rounds256 = (tiles_of(m, n, 256, 256) + 255) / 256;
-    if (!wide && 9 * rounds256 <= 5 * rounds128) return {k256x256, 1};
-    if (t128 >= 200) return {k128x128, 1};
-    // Too few of those for the CUs: smaller tiles, and k split where it is long, in parts of
-    // 16 blocks at least (128 x 4096 x 16384 to bf16: 79 us in 32 tiles of 128, 60 in 128 of
-    // 64, 24 with k in four; 1024 x 768 x 3000: 18, 9, 13 with k in two).
-    const uint64_t want = 512 / tiles_of(m, n, 64, 64), most = f8_blocks(k) / 16;
-    const uint64_t splits = want < most ? want : most;
-    return {k64x64, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits))};
-}
-
 uint64_t f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t out_dtype)
 {
-    const Cut c = cut_product(m, n, k, out_dtype == kF32);
+    const F8Cut c = cut_product(m, n, k, out_dtype == kF32);
     return c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 16) : 0;
 }
 
 template <bool kWide>
 hipError_t launch_product(F8MatmulArgs a, hipStream_t stream)
 {
-    const Cut cut = cut_product(a.m, a.n, a.k, kWide);
+    const F8Cut cut = cut_product(a.m, a.n, a.k, kWide);
     a.splits = cut.splits;
     void* params[] = {&a};
     auto go = [&](auto* f, uint64_t bm, uint64_t bn, uint32_t lanes) {

@@ -5,13 +5,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-namespace mezo {
+#include "plans.hpp"
 
-// Elements of a row that share a scale, and the bytes of a stored row.
-constexpr uint64_t kF8Block = 128;
-constexpr uint64_t f8_blocks(uint64_t cols) { return (cols + kF8Block - 1) / kF8Block; }
-constexpr uint64_t f8_code_stride(uint64_t cols) { return f8_blocks(cols) * kF8Block; }
-constexpr uint64_t f8_scale_stride(uint64_t cols) { return (f8_blocks(cols) + 3) / 4 * 4; }
+namespace mezo {
 
 struct F8QuantArgs {
     uint64_t values;  // device address, fp32 or bf16

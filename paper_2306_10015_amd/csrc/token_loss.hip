@@ -247,25 +247,6 @@ __global__ void __launch_bounds__(kFinishThreads) loss_all_kernel(LossArgs a)
     if (threadIdx.x == 0 && a.mean) *a.mean = count ? float(sum / double(count)) : 0.0f;
 }
 
-// One or two rows of together so many logits at most: one workgroup. A row of 50272 fp32
-// logits takes 6.8 us in it, 7.5 in 12 workgroups and a second launch, which costs the
-// host 4 us more.
-constexpr uint64_t kOneGroup = 65536;
-constexpr bool one_group(uint64_t rows, uint64_t vocab) { return rows <= 2 && vocab <= kOneGroup / rows; }
-
-// Rows shorter than this take a wave each.
-constexpr uint64_t kWaveRow = 2048;
-
-uint32_t loss_parts(uint64_t rows, uint64_t vocab)
-{
-    if (one_group(rows, vocab)) return 1;
-    // enough workgroups that the last round over the CUs is a small part of all, each with a
-    // few KB at least
-    const uint64_t want = (2048 + rows - 1) / rows, most = vocab / 4096;
-    const uint64_t parts = want < most ? want : most;
-    return vocab < kWaveRow || parts < 1 ? 1u : uint32_t(parts < 16 ? parts : 16);
-}
-
 template <uint32_t kDtype>
 hipError_t launch(LossArgs a, hipStream_t stream)
 {

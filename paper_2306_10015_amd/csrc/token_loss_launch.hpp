@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "plans.hpp"
+
 namespace mezo {
 
 struct LossArgs {
@@ -19,9 +21,6 @@ struct LossArgs {
     uint32_t parts;   // of a row, each a workgroup
     uint32_t dtype;
 };
-
-// How many workgroups share a row (1: the row's own workgroup writes its loss).
-uint32_t loss_parts(uint64_t rows, uint64_t vocab);
 
 hipError_t launch_token_loss(const LossArgs& args, hipStream_t stream);
 
