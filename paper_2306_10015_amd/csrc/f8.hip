@@ -609,12 +609,6 @@ __global__ void __launch_bounds__(256) f8_join_kernel(F8MatmulArgs a)
     store4<kWide>(a, whole_groups<kWide>(a), row, col, sum);
 }
 
-uint64_t f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t out_dtype)
-{
-    const F8Cut c = cut_product(m, n, k, out_dtype == kF32);
-    return c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 16) : 0;
-}
-
 template <bool kWide>
 hipError_t launch_product(F8MatmulArgs a, hipStream_t stream)
 {

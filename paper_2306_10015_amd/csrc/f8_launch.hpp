@@ -32,8 +32,6 @@ struct F8MatmulArgs {
 
 hipError_t launch_f8_quantize(const F8QuantArgs& args, hipStream_t stream);
 
-// Bytes of `partial` a product of these sizes needs (0: not split).
-uint64_t f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t out_dtype);
 hipError_t launch_f8_matmul(const F8MatmulArgs& args, hipStream_t stream);
 
 }  // namespace mezo

@@ -35,6 +35,9 @@ struct Range {
     uint64_t at, bytes;
 };
 
+// Whether a buffer ends within the address space.
+bool whole(Range r) { return r.bytes <= ~r.at; }
+
 bool overlap(Range a, Range b) { return a.at < b.at + b.bytes && b.at < a.at + a.bytes; }
 
 // Whether a buffer that is written shares memory with one of n others.
@@ -75,6 +78,7 @@ int check_quantize(const void* src, uint32_t dtype, uint64_t rows, uint64_t cols
     if (!matrix_bytes(rows, cols, ld, element_bytes(dtype), bytes)) return MEZO_EINVAL;
     const Range in = {address(src), bytes}, c = f8_codes(codes, rows, cols), s = f8_scales(scales, rows, cols);
     const Range read[2] = {in, c};
+    if (!whole(in) || !whole(c) || !whole(s)) return MEZO_EINVAL;
     if (clashes(c, &in, 1) || clashes(s, read, 2)) return MEZO_EOVERLAP;
     a.values = in.at;
     a.ld = ld;
@@ -98,13 +102,16 @@ int check_matmul(const void* x_codes, const void* x_scales, const void* w_codes,
     if (!aligned(x_codes, 16) || !aligned(w_codes, 16) || !aligned(x_scales, 4) || !aligned(w_scales, 4) ||
         !aligned(c, element_bytes(c_dtype)))
         return MEZO_EINVAL;
-    const uint64_t need = mezo::f8_matmul_workspace(m, n, k, c_dtype);
+    const uint64_t need = mezo::f8_matmul_workspace(m, n, k, c_dtype == MEZO_F32);
     if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return MEZO_EINVAL;
     uint64_t bytes;
     if (!matrix_bytes(m, n, ldc, element_bytes(c_dtype), bytes)) return MEZO_EINVAL;
     const Range out = {address(c), bytes}, scratch = {address(workspace), need};
     const Range read[5] = {f8_codes(x_codes, m, k), f8_scales(x_scales, m, k), f8_codes(w_codes, n, k),
                            f8_scales(w_scales, n, k), out};
+    for (const Range& r : read)
+        if (!whole(r)) return MEZO_EINVAL;
+    if (need && !whole(scratch)) return MEZO_EINVAL;
     if (clashes(out, read, 4) || (need && clashes(scratch, read, 5))) return MEZO_EOVERLAP;
     a.x = read[0].at;
     a.xs = read[1].at;
@@ -130,7 +137,7 @@ LinearSpace linear_space(uint64_t m, uint64_t n, uint64_t k, uint32_t c_dtype)
     LinearSpace s;
     s.scales = m * mezo::f8_code_stride(k);
     s.product = s.scales + (m * mezo::f8_scale_stride(k) + 15) / 16 * 16;
-    s.bytes = s.product + mezo::f8_matmul_workspace(m, n, k, c_dtype);
+    s.bytes = s.product + mezo::f8_matmul_workspace(m, n, k, c_dtype == MEZO_F32);
     return s;
 }
 
@@ -141,7 +148,7 @@ int f8_linear(const void* x, uint32_t x_dtype, uint64_t ldx, const void* w_codes
     if (!dense(x_dtype) || !dense(c_dtype)) return MEZO_EDTYPE;
     if (!workspace || !aligned(workspace, 16) || !f8_sizes(m, k) || !f8_sizes(n, k)) return MEZO_EINVAL;
     const LinearSpace s = linear_space(m, n, k, c_dtype);
-    if (workspace_bytes < s.bytes) return MEZO_EINVAL;
+    if (workspace_bytes < s.bytes || !whole({address(workspace), s.bytes})) return MEZO_EINVAL;
     char* const codes = static_cast<char*>(workspace);
     mezo::F8QuantArgs q;
     mezo::F8MatmulArgs a;
@@ -220,6 +227,7 @@ int attention(const mezo_attention_t* p, void* workspace, uint64_t workspace_byt
                        __builtin_add_overflow(n, a.dim, &n) || __builtin_mul_overflow(n, e, &n)))
             return MEZO_EINVAL;
         r[i] = {address(at[i]), n};
+        if (!whole(r[i])) return MEZO_EINVAL;
     }
     using wide = unsigned __int128;
     const wide oh = a.o_head, ot = a.o_token, h1 = a.heads - 1, t1 = a.q_tokens - 1;
@@ -232,6 +240,7 @@ int attention(const mezo_attention_t* p, void* workspace, uint64_t workspace_byt
                 scratch = {address(workspace), plan.workspace};
     const Range read[7] = {r[0], r[1], r[2], {address(a.docs), a.n_docs * 40ull},
                            {address(a.slopes), a.slopes ? a.heads * 4ull : 0}, r[3], lse};
+    if (!whole(read[3]) || !whole(read[4]) || !whole(lse) || !whole(scratch)) return MEZO_EINVAL;
     if (clashes(r[3], read, 5) || (a.lse && clashes(lse, read, 6)) || (plan.workspace && clashes(scratch, read, 7)))
         return MEZO_EOVERLAP;
     mezo::AttentionArgs g;
@@ -294,6 +303,8 @@ int token_loss(const void* logits, uint32_t dtype, uint64_t rows, uint64_t vocab
     if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return MEZO_EINVAL;
     const Range read[5] = {{address(logits), bytes}, {address(targets), rows * 8}, {address(losses), rows * 4},
                            {address(mean), mean ? 4u : 0u}, {address(workspace), need}};
+    for (const Range& r : read)
+        if (!whole(r)) return MEZO_EINVAL;
     if (clashes(read[2], read, 2) || (mean && clashes(read[3], read, 3)) || (need && clashes(read[4], read, 4)))
         return MEZO_EOVERLAP;
     mezo::LossArgs a;
@@ -329,7 +340,7 @@ int mezo_f8_quantize(const void* src, uint32_t src_dtype, uint64_t rows, uint64_
 
 uint64_t mezo_f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t c_dtype)
 {
-    return dense(c_dtype) && f8_sizes(m, k) && f8_sizes(n, k) ? mezo::f8_matmul_workspace(m, n, k, c_dtype) : 0;
+    return dense(c_dtype) && f8_sizes(m, k) && f8_sizes(n, k) ? mezo::f8_matmul_workspace(m, n, k, c_dtype == MEZO_F32) : 0;
 }
 
 int mezo_f8_matmul(const void* x_codes, const uint8_t* x_scales, const void* w_codes, const uint8_t* w_scales,

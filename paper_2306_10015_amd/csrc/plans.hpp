@@ -57,6 +57,13 @@ inline F8Cut cut_product(uint64_t m, uint64_t n, uint64_t k, bool wide)
     return {k64x64, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits))};
 }
 
+// Bytes of a split product's partial sums (0: not split); wide: to fp32.
+inline uint64_t f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, bool wide)
+{
+    const F8Cut c = cut_product(m, n, k, wide);
+    return c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 16) : 0;
+}
+
 // ---- attention -------------------------------------------------------------------
 
 // How a call is cut: the most workgroups that share a document's keys, the keys of
