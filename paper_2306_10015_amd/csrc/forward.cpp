@@ -38,7 +38,11 @@ struct Range {
 // Whether a buffer ends within the address space.
 bool whole(Range r) { return r.bytes <= ~r.at; }
 
-bool overlap(Range a, Range b) { return a.at < b.at + b.bytes && b.at < a.at + a.bytes; }
+// (an empty one shares memory with nothing)
+bool overlap(Range a, Range b)
+{
+    return a.bytes && b.bytes && a.at < b.at + b.bytes && b.at < a.at + a.bytes;
+}
 
 // Whether a buffer that is written shares memory with one of n others.
 bool clashes(Range out, const Range* others, int n)

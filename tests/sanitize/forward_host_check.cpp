@@ -312,6 +312,24 @@ static void attention()
               });
 }
 
+// An array of no elements shares memory with nothing, wherever its pointer points.
+static void empty_arrays()
+{
+    mezo_attention_t a = {};
+    a.q = P(buffer(0));
+    a.out = P(buffer(1));
+    a.k = a.v = P(buffer(1) + 64);
+    a.docs = static_cast<const int64_t*>(P(buffer(2)));
+    a.q_tokens = a.max_q = 4;
+    a.q_token = a.o_token = a.q_head = a.o_head = a.k_token = a.k_head = a.v_token = a.v_head = 64;
+    a.n_docs = a.heads = a.kv_heads = 1;
+    a.dim = 64;
+    a.scale = 1.0f;
+    CHECK(made(0, 0, [&] { return mezo_attention(&a, nullptr, 0, nullptr); }) == MEZO_OK);
+    a.k_tokens = a.max_k = 1;
+    CHECK(made(0, 0, [&] { return mezo_attention(&a, nullptr, 0, nullptr); }) == MEZO_EOVERLAP);
+}
+
 static void loss()
 {
     for (uint64_t vocab : {100ull, 50272ull})
@@ -335,6 +353,7 @@ int main()
     products();
     const unsigned long b = g_launches;
     attention();
+    empty_arrays();
     const unsigned long c = g_launches;
     loss();
     CHECK(a > 100 && b - a > 100 && c - b > 100 && g_launches - c > 100);  // the sweeps reach the launches
