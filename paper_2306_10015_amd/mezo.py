@@ -270,6 +270,10 @@ def nf4_dequantize(t: NF4Tensor, dtype=None, out=None, stream=None):
 
 
 # ---- the forward pass ------------------------------------------------------
+#
+# None of these operators has a backward pass. They may be called on tensors that
+# require a gradient (a model's parameters do unless told otherwise); a backward
+# pass through their outputs raises.
 
 _NO_SWITCH = contextlib.nullcontext()
 _DEVICES = 0
@@ -324,6 +328,28 @@ def _scratch(nbytes: int, device):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+class _NoBackward(torch.autograd.Function):
+    """Stands for an operator in autograd's graph: differentiating through it is
+    an error, not a gradient left out."""
+
+    @staticmethod
+    def forward(ctx, name, count, *tensors):
+        ctx.name = name
+        ctx.mark_dirty(*tensors[:count])  # (the operator wrote them)
+        return tensors[:count]
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError(f"mezo.{ctx.name} has no backward pass (the method takes no derivative): "
+                           "call it under torch.no_grad(), or on detached tensors")
+
+
+def _no_backward(name, outputs, *inputs):
+    """Outputs of inputs that require a gradient require one too."""
+    if any(t is not None and t.requires_grad for t in inputs) and torch.is_grad_enabled():
+        _NoBackward.apply(name, len(outputs), *outputs, *inputs)
 
 
 class F8Matrix:
@@ -421,6 +447,8 @@ def f8_linear(x, w: F8Matrix, dtype=None, out=None, stream=None):
         ws = _scratch(nbytes, x.device)
         _check(lib.mezo_f8_linear(x.data_ptr(), x_code, ldx, w.codes.data_ptr(), w.scales.data_ptr(), m, n, k,
                                   out.data_ptr(), code, ldc, _ptr(ws), nbytes, _stream_ptr(None)), "mezo_f8_linear")
+    if x.requires_grad:
+        _no_backward("f8_linear", (out,), x)
     return out
 
 
@@ -524,6 +552,8 @@ def attention(q, k, v, docs: Documents, causal: bool = True, scale: float | None
         nbytes = lib.mezo_attention_workspace(a)
         ws = _scratch(nbytes, q.device)
         _check(lib.mezo_attention(a, _ptr(ws), nbytes, _stream_ptr(None)), "mezo_attention")
+    if q.requires_grad or k.requires_grad or v.requires_grad or (slopes is not None and slopes.requires_grad):
+        _no_backward("attention", (out, lse) if return_lse else (out,), q, k, v, slopes)
     return (out, lse) if return_lse else out
 
 
@@ -546,6 +576,8 @@ def token_loss(logits, targets, stream=None):
         ws = _scratch(nbytes, logits.device)
         _check(lib.mezo_token_loss(logits.data_ptr(), dtype, rows, vocab, ld, targets.data_ptr(), losses.data_ptr(),
                                    mean.data_ptr(), _ptr(ws), nbytes, _stream_ptr(None)), "mezo_token_loss")
+    if logits.requires_grad:
+        _no_backward("token_loss", (losses, mean), logits)
     return losses, mean
 
 
