@@ -456,9 +456,10 @@ class Documents:
     """The documents of an attention call: ``table``, a device tensor int64
     [documents, 5] of (q_first, q_len, k_first, k_len, prefix) as in mezo.h, and
     the most queries and keys a document has. Use ``Documents.of`` to make one
-    from lengths, checked."""
+    from lengths, checked. ``covered``: the documents' queries are tokens 0 ..
+    covered - 1, each of one document (None: not known)."""
 
-    def __init__(self, table, max_q: int, max_k: int):
+    def __init__(self, table, max_q: int, max_k: int, covered: int | None = None):
         if table.dtype != torch.int64:
             raise TypeError(f"table must be int64, got {table.dtype}")
         shape = table.shape
@@ -467,6 +468,7 @@ class Documents:
         if max_q < 0 or max_k < 0:
             raise ValueError("max_q and max_k must not be negative")
         self.table, self.count, self.max_q, self.max_k = table, shape[0], int(max_q), int(max_k)
+        self.covered = covered
 
     @classmethod
     def of(cls, q_lens, k_lens=None, prefix=None, q_first=None, k_first=None, device="cuda") -> "Documents":
@@ -496,7 +498,8 @@ class Documents:
             raise ValueError("the documents' queries overlap")
         rows = list(zip(q_first, q_lens, k_first, k_lens, ints(prefix, [0] * len(q_lens))))
         table = torch.tensor(rows, dtype=torch.int64, device=device).reshape(len(rows), 5)
-        return cls(table, max(q_lens, default=0), max(k_lens, default=0))
+        gaps = sum(q_lens) != max((b for _, b in spans), default=0)
+        return cls(table, max(q_lens, default=0), max(k_lens, default=0), 0 if gaps else sum(q_lens))
 
 
 def _heads_of(t, what: str):
@@ -521,7 +524,9 @@ def attention(q, k, v, docs: Documents, causal: bool = True, scale: float | None
     and head strides that are multiples of 16 bytes. scale is 1 / sqrt(dim) by
     default; slopes, fp32 [heads], biases scores by -slope * distance. Returns
     out, like q, and with return_lse the pair (out, lse), lse fp32 [tokens, heads].
-    Tokens of no document are not written."""
+    Tokens of no document: 0 and -inf, as of a query that sees no key; but with
+    ``out`` given they keep what it holds, and with documents whose ``covered``
+    is not known they are not written."""
     tq, heads, dim, q_token, q_head = _heads_of(q, "q")
     tk, kv_heads, k_dim, k_token, k_head = _heads_of(k, "k")
     tv, v_heads, v_dim, v_token, v_head = _heads_of(v, "v")
@@ -535,8 +540,9 @@ def attention(q, k, v, docs: Documents, causal: bool = True, scale: float | None
     if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (heads,) or not slopes.is_contiguous()):
         raise ValueError(f"slopes: a contiguous float32 tensor of {heads}")
     with _on(q.device, stream):
+        bare = docs.covered is not None and docs.covered < tq  # some tokens are of no document
         if out is None:
-            out = torch.empty((tq, heads, dim), dtype=q.dtype, device=q.device)
+            out = (torch.zeros if bare else torch.empty)((tq, heads, dim), dtype=q.dtype, device=q.device)
             o_token, o_head = heads * dim, dim
         else:
             if out.dtype != q.dtype or out.shape != q.shape:
@@ -544,6 +550,8 @@ def attention(q, k, v, docs: Documents, causal: bool = True, scale: float | None
             _, _, _, o_token, o_head = _heads_of(out, "out")
         _same_device(q, k, v, out, slopes, docs.table)
         lse = torch.empty((tq, heads), dtype=torch.float32, device=q.device) if return_lse else None
+        if bare and return_lse:
+            lse.fill_(-math.inf)
         a = _ATTENTION.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse) or 0,
                             docs.table.data_ptr(), _ptr(slopes) or 0, tq, tk, q_token, q_head, k_token, k_head,
                             v_token, v_head, o_token, o_head, docs.max_q, docs.max_k, docs.count, heads,

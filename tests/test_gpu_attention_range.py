@@ -233,3 +233,27 @@ def test_small_values_keep_their_digits(mz, size, nq, nk, dtype):
     for queries in (q, q * 0):
         check(mz, queries, k, (v + 3 * v.sign()) * size, table([nq], [nk]),
               floor=nk * 2.0 ** -149 if dtype == "f32" else 2.0 ** -133)
+
+
+# ---- tokens of no document -------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("q_lens,q_first", [([20, 30], [10, 60]), ([20, 30], None), ([0, 0], None), ([], None),
+                                            ([60, 50], [40, 100]), ([100], None)])
+def test_tokens_of_no_document_come_back_empty(mz, q_lens, q_first, dtype):
+    """0 and -inf, whatever the memory held that the output was made in."""
+    import torch
+    q, k, v = tensors(100, 160, 2, 2, 64, dtype)
+    docs = mz.Documents.of(q_lens, q_first=q_first)
+    for _ in range(3):
+        torch.full((100, 2, 64), 7.0, dtype=q.dtype, device="cuda")  # (freed at once: the next allocations' memory)
+        torch.full((100, 2), 7.0, device="cuda")
+        out, lse = mz.attention(q, k, v, docs, return_lse=True)
+        bare = torch.ones(100, dtype=torch.bool)
+        at = 0
+        for i, n in enumerate(q_lens):
+            first = q_first[i] if q_first else at
+            bare[first:first + n] = False
+            at += n
+        assert bool((out[bare] == 0).all()) and bool((lse[bare] == -math.inf).all())
+        assert bool(torch.isfinite(out[~bare].float()).all()) and bool(torch.isfinite(lse[~bare]).all())
