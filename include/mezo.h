@@ -404,10 +404,12 @@ MEZO_API int mezo_f8_quantize(const void* src, uint32_t src_dtype, uint64_t rows
 /* c = x w^T: x [m, k] and w [n, k] (a layer's weights, one row per output) in
  * 8-bit storage, c [m, n] of storage c_dtype (MEZO_F32 or MEZO_BF16), rows ldc
  * elements apart. The values of both are multiplied exactly. For MEZO_F32 they
- * are summed in fp32; for MEZO_BF16 the matrix instruction sums a block's 128
- * products to about 16 bits, the blocks in fp32, and the sum is rounded once.
- * Sizes as in mezo_f8_quantize, m * n <= MEZO_MAX_NUMEL, ldc >= n (MEZO_EINVAL); c and the workspace
- * must not overlap the operands (MEZO_EOVERLAP). */
+ * are summed in fp32 (and values in blocks of a scale below 2^-124 are rounded
+ * to multiples of 2^-133 first); for MEZO_BF16 the matrix instruction sums a
+ * block's 128 products to about 16 bits, the blocks in fp32, and the sum is
+ * rounded once. Sizes as in mezo_f8_quantize, m * n <= MEZO_MAX_NUMEL, ldc >= n
+ * (MEZO_EINVAL); c and the workspace must not overlap the operands
+ * (MEZO_EOVERLAP). */
 MEZO_API uint64_t mezo_f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t c_dtype);
 MEZO_API int mezo_f8_matmul(const void* x_codes, const uint8_t* x_scales, const void* w_codes,
                             const uint8_t* w_scales, uint64_t m, uint64_t n, uint64_t k, void* c, uint32_t c_dtype,

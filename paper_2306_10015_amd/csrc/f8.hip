@@ -12,9 +12,11 @@
 //        inner sum of 128 products keeps about 16 bits (2-norm error of a product
 //        of normal rows 1.5e-5, with a few loud channels 5e-5, the same from 1 to
 //        128 blocks; measured), far below bf16's own rounding of 1.7e-3.
-//  fp32: the codes are widened to bf16 in registers, exactly, their scales
-//        applied, and v_mfma_f32_16x16x32_bf16 sums the exact products in fp32
-//        (error 1e-8 to 2e-7, as a chain of fp32 additions), at half the rate.
+//  fp32: the codes are widened to bf16 in registers, their scales applied, and
+//        v_mfma_f32_16x16x32_bf16 sums the exact products in fp32 (error 1e-8 to
+//        2e-7, as a chain of fp32 additions), at half the rate. Widening is exact
+//        down to bf16's last bit, 2^-133: of blocks with scales below 2^-124, whose
+//        largest value is below 2^-115, it rounds what lies under that.
 #include <type_traits>
 
 #include "f8_launch.hpp"

@@ -60,3 +60,26 @@ def test_product_of_every_kernel(mz, m, n, k, out, tile, splits, wide):
     off = (c.double() - exact).abs()
     assert bool((off <= bound).all()), float((off / bound).max())
     assert float(off.norm() / exact.norm()) <= (1e-6 if out == "f32" else 2.0 ** -9 + 1e-4)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("m", [4, 100])
+@pytest.mark.parametrize("size", [1e-34, 1e-36, 1e-38, 1e-40])
+def test_the_smallest_values(mz, size, m, out):
+    """Scales down to the smallest, values down to fp32's subnormal ones. fp32 output takes
+    what is below bf16's last bit, 2^-133, to the nearer side."""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(m)
+    x = mz.f8_quantize(torch.empty(m, 256, device="cuda").normal_(0, 1, generator=g) * size)
+    w = mz.f8_quantize(torch.empty(64, 256, device="cuda").normal_(0, 1e20, generator=g))
+    c = mz.f8_matmul(x, w, torch.float32 if out == "f32" else torch.bfloat16).double()
+    xv, wv = stored(x), stored(w)
+    exact = xv @ wv.t().contiguous()
+    sums = xv.abs() @ wv.abs().t().contiguous()
+    if out == "f32":
+        bound = 256 * 2.0 ** -23 * sums + 2.0 ** -134 * wv.abs().sum(1)[None, :]
+    else:
+        tops = [v.abs().unflatten(1, (-1, 128)).amax(2) for v in (xv, wv)]
+        bound = 2.0 ** -8 * exact.abs() + (1 + 2.0 ** -8) * 128 * 2.0 ** -15 * (tops[0] @ tops[1].t().contiguous())
+    assert bool(((c - exact).abs() <= bound).all()), float(((c - exact).abs() / bound).max())
