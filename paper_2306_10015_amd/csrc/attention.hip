@@ -109,14 +109,12 @@ __device__ __forceinline__ int visible(const AttentionArgs& a, const Document& d
     return pos + 1 > d.prefix ? pos + 1 : d.prefix;  // pos < nk, prefix >= 0
 }
 
-constexpr float kMostCap = 96.0f / kLog2e;  // of the short form of a capped score
-
 // The score function's constants, for scores in units of log 2.
 struct Score {
     float c;      // scale log2 e
     float k, w;   // capped: x = w - 2 w / (1 + 2^(k s)), k = 2 scale log2 e / cap, w = cap log2 e
-    float cap, scale;
-    bool capped, small;
+    float cap, scale, share;  // share = scale / cap
+    bool capped;
 };
 
 __device__ __forceinline__ Score score_of(const AttentionArgs& a)
@@ -125,37 +123,46 @@ __device__ __forceinline__ Score score_of(const AttentionArgs& a)
     s.scale = a.scale;
     s.cap = a.softcap;
     s.capped = a.softcap > 0.0f;
-    s.small = a.softcap <= kMostCap;
     s.c = a.scale * kLog2e;
     // (finite, so that a score of 0 stays 0 under the smallest caps)
-    constexpr float kLargest = 3.4e38f;
-    s.k = s.capped ? fminf(fmaxf(2.0f * a.scale * kLog2e / a.softcap, -kLargest), kLargest) : 0.0f;
+    constexpr float kLargest = 1e38f;
+    s.share = s.capped ? fminf(fmaxf(a.scale / a.softcap, -kLargest), kLargest) : 0.0f;
+    s.k = 2.0f * kLog2e * s.share;
     s.w = a.softcap * kLog2e;
     return s;
 }
 
 // The cap by two transcendentals: a capped score before the bias is w - 2 w r. Its error is
-// 2^-23 cap, since 1 + 2^(k x) keeps no more of x: for results of bf16 and caps up to kMostCap.
+// 2^-23 cap, since 1 + 2^(k x) keeps no more of x.
 __device__ __forceinline__ float cap_share(const Score& s, float x)
 {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * s.k));
 }
 
-// A capped score before the bias, of any cap, in its own units. By the library's tanh, and
-// what is far below the cap as it is (tanh y is y to 2^-25 of it below 2^-12; y itself loses
-// digits where the cap is near the largest float).
-__device__ __forceinline__ float capped_any(const Score& s, float x)
-{
-    const float y = x * s.scale / s.cap;
-    return fabsf(y) < 0x1p-12f ? x * s.scale : s.cap * tanhf(y);
-}
+// A capped score before the bias, in units of log 2. bf16 takes the short form as long as its
+// error does not show in a result of bf16, fp32 the library's tanh as long as neither w nor
+// x scale / cap can leave the range in which they keep their digits.
+template <bool kF>
+constexpr float kMostCap = kF ? 0x1p64f : 256.0f;
 
-// The same in units of log 2, by the short form where that will do.
 template <bool kF>
 __device__ __forceinline__ float capped(const Score& s, float x)
 {
-    if (!kF && s.small) return __builtin_fmaf(cap_share(s, x), -2.0f * s.w, s.w);  // (uniform)
-    return capped_any(s, x) * kLog2e;
+    if constexpr (kF) return s.w * tanhf(x * s.scale / s.cap);
+    return __builtin_fmaf(cap_share(s, x), -2.0f * s.w, s.w);
+}
+
+// The same in its own units, of any cap, to 2^-21 of the score itself: tanh y by its series
+// below a quarter, (1 - t) / (1 + t) with t = exp(-2 |y|) above.
+__device__ __forceinline__ float capped_any(const Score& s, float x)
+{
+    const float y = x * s.share, y2 = y * y, t = __builtin_amdgcn_exp2f(fabsf(y) * (-2.0f * kLog2e));
+    float series = __builtin_fmaf(y2, 62.0f / 2835, -17.0f / 315);
+    series = __builtin_fmaf(y2, series, 2.0f / 15);
+    series = __builtin_fmaf(y2, series, -1.0f / 3);
+    series = __builtin_fmaf(y2, series, 1.0f);
+    const float above = copysignf((1.0f - t) * __builtin_amdgcn_rcpf(1.0f + t), y);
+    return fabsf(y) < 0.25f ? x * s.scale * series : s.cap * above;
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -248,7 +255,10 @@ __device__ __forceinline__ void careful_row(const AttentionArgs& a, const Docume
                                    __uint_as_float(bits), s);
             }
         }
-        s = sc.capped ? capped_any(sc, s) : s * sc.scale;
+        if (sc.capped)
+            s = sc.cap <= kMostCap<true> ? sc.cap * tanhf(s * sc.scale / sc.cap) : capped_any(sc, s);
+        else
+            s *= sc.scale;
         if (a.slopes) s -= slope * fabsf(float(d.nk - d.nq + i - j));
         if (int(l) >= n) s = -__builtin_inff();
         float top = s;
@@ -461,8 +471,8 @@ struct Tile {
 //  kBiased: no cap, scale > 0. Away from the diagonal the bias is linear in the key: a
 //           constant of each of a lane's 16 results, which the products are added to
 //           instead of to zero, and one term a stage, which joins the reference.
-//  kCapped: no bias, and a cap up to kMostCap. No score can pass the cap, so the maximum is
-//           taken only until a row's reference is within kHeadroom of it (for nearly all
+//  kCapped: no bias, and a cap up to 66 (under larger ones most rows would be followed to
+//           their end). No score can pass the cap, so the maximum is taken only until a row's reference is within kHeadroom of it (for nearly all
 //           rows that is the first stage), and the cap's last fma subtracts the reference.
 //           Terms are then at most 2^kHeadroom; a row whose sums overflow all the same
 //           (values above 2^34 after a rise of that much) is one for careful_row.
@@ -652,8 +662,13 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys>())
                 }
                 if constexpr (kMode == kGeneral || kMode == kUncapped) {
                     if (kMode == kGeneral && sc.capped) {
+                        if (sc.cap <= kMostCap<kF>) {  // (uniform)
 #pragma unroll
-                        for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped<kF>(sc, x[t][e]);
+                            for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped<kF>(sc, x[t][e]);
+                        } else {
+#pragma unroll
+                            for (uint32_t e = 0; e < 16; ++e) x[t][e] = capped_any(sc, x[t][e]) * kLog2e;
+                        }
                     } else {
 #pragma unroll
                         for (uint32_t e = 0; e < 16; ++e) x[t][e] *= sc.c;
@@ -924,7 +939,7 @@ hipError_t launch(AttentionArgs a, hipStream_t stream)
             f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kPlain>);
         else if (a.softcap == 0.0f && a.scale > 0.0f)
             f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kBiased>);
-        else if (a.softcap > 0.0f && a.softcap <= kMostCap && !a.slopes)
+        else if (a.softcap > 0.0f && a.softcap <= 66.0f && !a.slopes)
             f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kCapped>);
     } else if (a.softcap == 0.0f) {
         f = reinterpret_cast<const void*>(attention_kernel<kF, kD, 4, false, kUncapped>);
