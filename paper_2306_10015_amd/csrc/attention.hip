@@ -464,8 +464,10 @@ struct Tile {
 // the vector instructions of the softmax bound (the others use kGeneral: fp32 is bound by
 // splitting its operands, calls by keys by memory; but the code of tanh, even where it is not
 // run, costs fp32 3%, so uncapped scores have kUncapped there: 16 documents of 50 to 2048
-// tokens, 16 heads of 128, 1242 -> 1202 us). Per score, in issue slots of a wave
-// (4 cycles, a transcendental 8): plain and biased 5.5, capped 11; general 8 to 15.
+// tokens, 16 heads of 128, 1242 -> 1202 us). Vector instructions a score that counts, over
+// calls of 8192 causal tokens: plain 6.0 (heads of 64) to 6.9 (128), biased 9.6, capped 9.8,
+// of which two transcendentals take two slots each; kGeneral 15.8 with a cap and a bias, 17.3
+// with a cap past the short form.
 //  kPlain:  no cap, no bias, scale > 0: the maximum is taken of the products themselves,
 //           and one fma scales a product and subtracts the reference.
 //  kBiased: no cap, scale > 0. Away from the diagonal the bias is linear in the key: a
