@@ -449,7 +449,8 @@ MEZO_API int mezo_f8_linear(const void* x, uint32_t x_dtype, uint64_t ldx, const
  * max_k < 2^31 - 256, max_q * heads / kv_heads <= 65535 * 128, n_docs * kv_heads < 2^24,
  * n_docs * max_q * heads < 2^40 (MEZO_EINVAL). The documents' queries must not overlap.
  * Rows of docs that point outside the arrays are cut to them. Scores and sums are fp32; with
- * MEZO_BF16 each probability is rounded to bf16 before it multiplies v.
+ * MEZO_BF16 each probability is rounded to bf16 before it multiplies v, and
+ * a capped score may be off by 2^-15, or 2^-21 of itself.
  *
  * heads a multiple of kv_heads, heads <= MEZO_ATTENTION_MAX_HEADS, dim a
  * multiple of 8 up to 128, pointers 16-byte aligned, strides multiples of 16
