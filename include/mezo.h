@@ -479,6 +479,90 @@ typedef struct {
 MEZO_API uint64_t mezo_attention_workspace(const mezo_attention_t* a);
 MEZO_API int mezo_attention(const mezo_attention_t* a, void* workspace, uint64_t workspace_bytes, void* stream);
 
+/* ---- generation over a paged cache ---------------------------------------
+ *
+ * A cache of keys and values in pages of `rows` rows (a power of two from
+ * MEZO_PAGE_MIN_ROWS to MEZO_PAGE_MAX_ROWS), n_pages of them: arrays of storage
+ * dtype given by the elements from one page, one row and one head to the next,
+ * a head's dim elements contiguous. A list of int32 entries (device memory)
+ * names the pages of each document in order: its key j is row j % rows of page
+ * list[k_first + j / rows], k_first being the third column of the document's
+ * row of `docs` (as under mezo_attention_t otherwise). Documents may share pages
+ * that they only read. What follows are forward operators like those above. */
+#define MEZO_PAGE_MIN_ROWS 8u
+#define MEZO_PAGE_MAX_ROWS 65536u
+
+/* Append: token i of a document with nq new tokens of nk stands at place r =
+ * nk - nq + i, and its key and value go to that row of the document's pages.
+ * Keys (and queries, if q is not NULL, into q_out) are turned on the way: with
+ * t = position * freqs[j], the pair (x_a, x_b) j of a head's first `rot`
+ * columns becomes (x_a cos t - x_b sin t, x_a sin t + x_b cos t), a and b being
+ * j and j + rot / 2, or 2 j and 2 j + 1 with `interleaved`; the other columns
+ * are copied. position is r, or positions[token] where that is not NULL (the
+ * depth in a tree, say). The angle is formed in fp64 (positions up to 2^31 keep
+ * their angles to 1e-6), sine, cosine and the turned values in fp32, rounded
+ * once. rot = 0 turns nothing.
+ *
+ * tokens: the rows of q, k, v, q_out and positions. A place below 0 and an entry
+ * outside the cache store nothing (the query is turned all the same). Tokens of
+ * no document, and those of a document past its max_q first, are left out. Rows of docs that
+ * point outside the arrays are cut to them. Two tokens of a call must not have
+ * the same row of the cache.
+ *
+ * dim a multiple of 8 up to 128, rot even and at most dim, heads and kv_heads
+ * up to MEZO_ATTENTION_MAX_HEADS, pointers 16-byte aligned (docs and positions 8,
+ * pages and freqs 4), strides multiples of 16 bytes, max_q * n_docs <= 2^28 with max_q
+ * taken as at most tokens (MEZO_EINVAL). What is written must not overlap
+ * itself or anything else (MEZO_EOVERLAP), but q_out may be q with its strides,
+ * arrays of one stride may lie in each other's gaps (parts of one projection's
+ * output), and so may the keys' and the values' pages (not their rows).
+ * n_docs = 0, max_q = 0 and tokens = 0 enqueue nothing. */
+typedef struct {
+    const void* q; /* or NULL */
+    const void* k;
+    const void* v;
+    void*       q_out;
+    void*       k_cache;
+    void*       v_cache;
+    const int64_t* docs;
+    const int32_t* pages;     /* the list, n_entries long */
+    const float*   freqs;     /* fp32 [rot / 2]; may be NULL if rot = 0 */
+    const int64_t* positions; /* int64 [tokens], or NULL */
+    uint64_t tokens, n_pages, n_entries, max_q;
+    uint64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;
+    uint64_t kc_page, kc_row, kc_head, vc_page, vc_row, vc_head;
+    uint32_t n_docs, heads, kv_heads, dim;
+    uint32_t page_rows, rot, interleaved, dtype;
+} mezo_append_t;
+
+MEZO_API int mezo_cache_append(const mezo_append_t* a, void* stream);
+
+/* mezo_attention over such a cache: a->k and a->v are its arrays, k_token and
+ * v_token the elements from one row of a page to the next, k_page and v_page
+ * those from one page to the next; a->k_tokens is not read, and max_k counts as
+ * at most n_entries * rows. A document's keys are cut to the list; entries outside
+ * the cache are read as its last page.
+ *
+ * With `tree`, a document's queries are tokens drafted in a tree: query i sees
+ * the nk - nq keys before them, keys j < prefix, and key nk - nq + t (the
+ * document's new token t) where bit t % 64 of tree[(q_first + i) * tree_words +
+ * t / 64] is set, its own bit as any other; tokens past tree_words * 64 are not
+ * seen. slopes must then be NULL and causal set (MEZO_EINVAL): a key's place in
+ * the cache is not its position. 1 <= tree_words <= MEZO_TREE_MAX_WORDS.
+ *
+ * Limits, errors, arithmetic and workspace are mezo_attention's. */
+#define MEZO_TREE_MAX_WORDS 1024u
+typedef struct {
+    const int32_t*  list;
+    const uint64_t* tree; /* uint64 [q_tokens, tree_words], or NULL */
+    uint64_t n_entries, n_pages, k_page, v_page;
+    uint32_t rows, tree_words;
+} mezo_pages_t;
+
+MEZO_API uint64_t mezo_paged_attention_workspace(const mezo_attention_t* a, const mezo_pages_t* pages);
+MEZO_API int mezo_paged_attention(const mezo_attention_t* a, const mezo_pages_t* pages, void* workspace,
+                                  uint64_t workspace_bytes, void* stream);
+
 /* The loss of a forward pass: for each of `rows` tokens with target y =
  * targets[t] >= 0, losses[t] = ln sum_v exp(x_tv) - x_ty over the token's
  * `vocab` logits (storage dtype, rows ld elements apart); tokens with a

@@ -13,6 +13,7 @@ import re
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
@@ -44,7 +45,7 @@ def _run(cmd) -> list[str]:
     r = subprocess.run(cmd, capture_output=True, text=True)
     # hipcc's host pass reports the device-only feature flag as unknown: harmless
     noise = "'-packed-fp32-ops' is not a recognized feature"
-    lines = [l for l in r.stderr.splitlines() if noise not in l]
+    lines = [l for l in r.stderr.splitlines() if noise not in l and not l.startswith("In file included from")]
     remarks = [l for l in lines if RESOURCE_REMARK in l]
     # the remarks' source excerpts ("  42 | {", "     | ^") go with them
     err = "\n".join(l for l in lines if RESOURCE_REMARK not in l and not _EXCERPT.match(l))
@@ -82,9 +83,9 @@ KERNEL_UNITS = ["engine_dense.hip", "engine_nf4.hip", "nf4_convert.hip", "checks
 #: Those of the forward pass's operators. Their matrix tiles fill a wave's
 #: registers on purpose, so they are recorded apart from the engine's kernels,
 #: which keep to 128.
-FORWARD_UNITS = ["attention.hip", "f8.hip", "token_loss.hip"]
+FORWARD_UNITS = ["attention.hip", "paged_attention.hip", "cache_append.hip", "f8.hip", "token_loss.hip"]
 #: Host units.
-HOST_UNITS = ["api.cpp", "forward.cpp"]
+HOST_UNITS = ["api.cpp", "forward.cpp", "generation.cpp"]
 
 
 def build(verbose: bool = False) -> Path:
@@ -94,13 +95,17 @@ def build(verbose: bool = False) -> Path:
     BUILD_DIR.mkdir(exist_ok=True)
     cc = hipcc()
     objs = []
+    # the units side by side: most of the time goes into two of them
+    pool = ThreadPoolExecutor(min(8, os.cpu_count() or 1))
+    flags = {unit: [*DEVICE, RESOURCE_REMARK] for unit in KERNEL_UNITS + FORWARD_UNITS}
+    jobs = {unit: pool.submit(_run, [cc, *COMMON, *flags.get(unit, []), "-c", str(CSRC / unit), "-o",
+                                     str(BUILD_DIR / (Path(unit).stem + ".o"))])
+            for unit in sorted(KERNEL_UNITS + FORWARD_UNITS + HOST_UNITS, key=lambda u: "attention" not in u)}
     for units, record in ((KERNEL_UNITS, "kernel_resources.txt"), (FORWARD_UNITS, "forward_resources.txt")):
         table = []
         for unit in units:
-            obj = BUILD_DIR / (Path(unit).stem + ".o")
-            remarks = _run([cc, *COMMON, *DEVICE, RESOURCE_REMARK, "-c", str(CSRC / unit), "-o", str(obj)])
-            table += [dict(unit=unit, **k) for k in kernel_resources(remarks)]
-            objs.append(str(obj))
+            table += [dict(unit=unit, **k) for k in kernel_resources(jobs[unit].result())]
+            objs.append(str(BUILD_DIR / (Path(unit).stem + ".o")))
         # every kernel keeps its values in registers: a spill to per-lane scratch
         # memory is a build error
         with open(BUILD_DIR / record, "w") as f:
@@ -112,9 +117,9 @@ def build(verbose: bool = False) -> Path:
             raise RuntimeError("kernels using scratch memory: "
                                + (", ".join(k["kernel"] for k in spills) if table else "(no resource remarks)"))
     for unit in HOST_UNITS:
-        obj = BUILD_DIR / (Path(unit).stem + ".o")
-        _run([cc, *COMMON, "-c", str(CSRC / unit), "-o", str(obj)])
-        objs.append(str(obj))
+        jobs[unit].result()
+        objs.append(str(BUILD_DIR / (Path(unit).stem + ".o")))
+    pool.shutdown()
     tmp = LIB.with_suffix(".so.tmp")
     _run([cc, "-shared", "-fPIC", *DEVICE, *objs, "-o", str(tmp)])
     os.replace(tmp, LIB)

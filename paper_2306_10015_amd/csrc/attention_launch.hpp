@@ -1,5 +1,5 @@
-// attention_launch.hpp — interface between the C-ABI host code (forward.cpp) and
-// the attention kernels (attention.hip).
+// attention_launch.hpp — interface between the C-ABI host code (forward.cpp,
+// generation.cpp) and the attention kernels (attention.hip, paged_attention.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -26,6 +26,18 @@ struct AttentionArgs {
     float scale, softcap;
 };
 
+// The keys and values of a paged cache: k and v are its first page's, k_token and v_token the
+// bytes from one row of a page to the next, and a document's k_first its first entry in `pages`.
+struct PagedArgs : AttentionArgs {
+    uint64_t pages;           // uint32 [entries]
+    uint64_t entries;
+    uint64_t k_page, v_page;  // bytes from one page to the next
+    uint64_t tree;            // uint64 [q_tokens, tree_words], or 0
+    uint32_t n_pages, page_shift, tree_words;
+};
+
 hipError_t launch_attention(const AttentionArgs& args, hipStream_t stream);
+
+hipError_t launch_paged_attention(const PagedArgs& args, hipStream_t stream);
 
 }  // namespace mezo

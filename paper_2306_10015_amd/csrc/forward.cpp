@@ -8,49 +8,14 @@
 
 #include "../../include/mezo.h"
 #include "attention_launch.hpp"
+#include "checks.hpp"
 #include "f8_launch.hpp"
 #include "host.hpp"
 #include "token_loss_launch.hpp"
 
 namespace {
 
-using mezo::guarded;
-
-uint64_t address(const void* p) { return reinterpret_cast<uint64_t>(p); }
-
-bool aligned(const void* p, uint64_t bytes) { return (address(p) & (bytes - 1)) == 0; }
-
-bool dense(uint32_t dtype) { return dtype == MEZO_F32 || dtype == MEZO_BF16; }
-
-uint64_t element_bytes(uint32_t dtype) { return dtype == MEZO_F32 ? 4 : 2; }
-
-// The bytes of rows rows of cols elements, ld apart (false: past 64 bits).
-bool matrix_bytes(uint64_t rows, uint64_t cols, uint64_t ld, uint64_t element, uint64_t& bytes)
-{
-    return !__builtin_mul_overflow(rows - 1, ld, &bytes) && !__builtin_add_overflow(bytes, cols, &bytes) &&
-           !__builtin_mul_overflow(bytes, element, &bytes);
-}
-
-struct Range {
-    uint64_t at, bytes;
-};
-
-// Whether a buffer ends within the address space.
-bool whole(Range r) { return r.bytes <= ~r.at; }
-
-// (an empty one shares memory with nothing)
-bool overlap(Range a, Range b)
-{
-    return a.bytes && b.bytes && a.at < b.at + b.bytes && b.at < a.at + a.bytes;
-}
-
-// Whether a buffer that is written shares memory with one of n others.
-bool clashes(Range out, const Range* others, int n)
-{
-    for (int i = 0; i < n; ++i)
-        if (overlap(out, others[i])) return true;
-    return false;
-}
+using namespace mezo;
 
 // ---- 8-bit storage -----------------------------------------------------------
 

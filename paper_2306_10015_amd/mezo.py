@@ -60,6 +60,12 @@ class Codec(ctypes.Structure):
 
 #: Layout of mezo_attention_t: 7 pointers, 12 u64, 6 u32, 2 floats.
 _ATTENTION = struct.Struct("=7Q12Q6I2f")
+#: Layout of mezo_pages_t: 2 pointers, 4 u64, 2 u32.
+_PAGES = struct.Struct("=2Q4Q2I")
+#: Layout of mezo_append_t: 10 pointers, 18 u64, 8 u32.
+_APPEND = struct.Struct("=10Q18Q8I")
+#: Rows of a cache's page: a power of two in between.
+PAGE_MIN_ROWS, PAGE_MAX_ROWS = 8, 65536
 
 
 class Step(ctypes.Structure):
@@ -77,6 +83,7 @@ EXPORTS = ("mezo_paramset_create", "mezo_paramset_destroy", "mezo_paramset_numel
            "mezo_f8_quantize", "mezo_f8_matmul_workspace", "mezo_f8_matmul",
            "mezo_f8_linear_workspace", "mezo_f8_linear",
            "mezo_attention_workspace", "mezo_attention",
+           "mezo_cache_append", "mezo_paged_attention_workspace", "mezo_paged_attention",
            "mezo_token_loss_workspace", "mezo_token_loss", "mezo_debug_generate", "mezo_debug_box_muller",
            "mezo_strerror", "mezo_last_error", "mezo_version")
 
@@ -137,6 +144,12 @@ def _load() -> ctypes.CDLL:
     L.mezo_attention_workspace.restype = u64
     L.mezo_attention.argtypes = [vp, vp, u64, vp]
     L.mezo_attention.restype = i32
+    L.mezo_cache_append.argtypes = [vp, vp]
+    L.mezo_cache_append.restype = i32
+    L.mezo_paged_attention_workspace.argtypes = [vp, vp]
+    L.mezo_paged_attention_workspace.restype = u64
+    L.mezo_paged_attention.argtypes = [vp, vp, vp, u64, vp]
+    L.mezo_paged_attention.restype = i32
     L.mezo_token_loss_workspace.argtypes = [u64, u64]
     L.mezo_token_loss_workspace.restype = u64
     L.mezo_token_loss.argtypes = [vp, u32, u64, u64, u64, vp, vp, vp, vp, u64, vp]
@@ -562,6 +575,205 @@ def attention(q, k, v, docs: Documents, causal: bool = True, scale: float | None
         _check(lib.mezo_attention(a, _ptr(ws), nbytes, _stream_ptr(None)), "mezo_attention")
     if q.requires_grad or k.requires_grad or v.requires_grad or (slopes is not None and slopes.requires_grad):
         _no_backward("attention", (out, lse) if return_lse else (out,), q, k, v, slopes)
+    return (out, lse) if return_lse else out
+
+
+# ---- generation over a paged cache -------------------------------------------
+
+class PagedCache:
+    """Keys and values of many documents in pages: ``k`` and ``v``, device
+    tensors [pages, rows, kv_heads, dim] of fp32 or bf16 with contiguous heads
+    and other strides that are multiples of 16 bytes (rows a power of two from 8
+    to 65536; both may be parts of one array), and ``pages``, an int32 device
+    tensor that lists the pages of each document in order: [documents, entries],
+    or flat where their numbers differ. It is read when the work runs."""
+
+    def __init__(self, k, v, pages):
+        shape = k.shape
+        if len(shape) != 4 or v.shape != shape or not k.is_cuda or not v.is_cuda:
+            raise ValueError("k and v: CUDA tensors [pages, rows, kv_heads, dim]")
+        if k.dtype != v.dtype:
+            raise TypeError(f"k is {k.dtype}, v {v.dtype}")
+        self.dtype = _dtype_code(k)
+        n_pages, rows, self.kv_heads, self.dim = shape
+        if rows & (rows - 1) or not PAGE_MIN_ROWS <= rows <= PAGE_MAX_ROWS:
+            raise ValueError(f"pages of {rows} rows: a power of two from {PAGE_MIN_ROWS} to {PAGE_MAX_ROWS}")
+        if pages.dtype != torch.int32:
+            raise TypeError(f"pages must be int32, got {pages.dtype}")
+        if pages.dim() not in (1, 2) or not pages.is_cuda or not pages.is_contiguous():
+            raise ValueError("pages: a contiguous CUDA tensor [documents, entries] or [entries]")
+        _same_device(k, v, pages)
+        self.k, self.v, self.pages, self.n_pages, self.rows = k, v, pages, n_pages, rows
+        self._k, self._v = self._strides(k, "k"), self._strides(v, "v")
+
+    @staticmethod
+    def _strides(t, what):
+        """Elements from one page, one row and one head to the next."""
+        n_pages, rows, heads, dim = t.shape
+        sp, sr, sh, sd = t.stride()
+        if dim > 1 and sd != 1:
+            raise ValueError(f"{what}: the elements of a head must be contiguous")
+        if min(sp, sr, sh) < 0:
+            raise ValueError(f"{what}: negative strides")
+        sh = sh if heads > 1 else dim
+        return sp if n_pages > 1 else rows * sr, sr, sh
+
+    @classmethod
+    def empty(cls, n_pages: int, rows: int, kv_heads: int, dim: int, pages, dtype=torch.bfloat16) -> "PagedCache":
+        """A cache of n_pages pages of `rows` rows on the device of `pages`."""
+        k, v = (torch.empty(n_pages, rows, kv_heads, dim, dtype=dtype, device=pages.device) for _ in range(2))
+        return cls(k, v, pages)
+
+    @property
+    def device(self):
+        return self.k.device
+
+    def documents(self, q_lens, k_lens, prefix=None) -> Documents:
+        """Documents.of for the rows of a two-dimensional ``pages``: row d lists
+        the pages of document d, of which the last q_lens[d] of k_lens[d] tokens are new."""
+        if self.pages.dim() != 2:
+            raise ValueError("pages is flat: use Documents.of with k_first, each document's first entry")
+        count, entries = self.pages.shape
+        if len(q_lens) != count:
+            raise ValueError(f"{len(q_lens)} documents, pages of {count}")
+        if any(n > entries * self.rows for n in k_lens):
+            raise ValueError(f"a document has more keys than its {entries} pages")
+        return Documents.of(q_lens, k_lens, prefix, k_first=[d * entries for d in range(count)], device=self.device)
+
+
+def tree_mask(parents, device="cuda"):
+    """Trees of drafted tokens: for each document a sequence of the parents of
+    its new tokens among themselves, each before its token (-1: the token before
+    them all). Returns (mask, depth): int64 [tokens, words], the tokens that each
+    one follows, itself included, as paged_attention takes them, and int64
+    [tokens], how many of them there are besides itself. The position of
+    a token is the document's old length plus its depth."""
+    words = max(1, (max((len(tree) for tree in parents), default=0) + 63) // 64)
+    rows, depth = [], []
+    for tree in parents:
+        own = []
+        for t, p in enumerate(tree):
+            if not -1 <= p < t:
+                raise ValueError(f"token {t}'s parent is {p}: an earlier token, or -1")
+            own.append((own[p] if p >= 0 else 0) | 1 << t)
+        rows += own
+        depth += [bin(bits).count("1") - 1 for bits in own]
+    mask = np.array([[bits >> 64 * w & 0xFFFFFFFFFFFFFFFF for w in range(words)] for bits in rows],
+                    dtype=np.uint64).reshape(len(rows), words)
+    return torch.from_numpy(mask.view(np.int64)).to(device), torch.tensor(depth, dtype=torch.int64, device=device)
+
+
+def cache_append(k, v, cache: PagedCache, docs: Documents, q=None, freqs=None, positions=None,
+                 interleaved: bool = False, out=None, stream=None):
+    """The keys and values of new tokens into a paged cache (mezo_cache_append):
+    k and v [tokens, kv_heads, dim] like the cache. Keys, and the queries q
+    [tokens, heads, dim] where given, are turned by their positions: freqs, fp32
+    [up to dim / 2], the angle a position adds to each pair (None: nothing
+    is turned). A token's position is its place in its document, or
+    positions, int64 [tokens]. Returns the turned queries (into `out`, which
+    may be q itself), or None. Queries of no document: 0; but with ``out`` given they
+    keep what it holds, and with documents whose ``covered`` is not known they are
+    not written."""
+    tk, kv_heads, dim, k_token, k_head = _heads_of(k, "k")
+    tv, v_heads, v_dim, v_token, v_head = _heads_of(v, "v")
+    if (tk, kv_heads, dim) != (tv, v_heads, v_dim):
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} do not fit together")
+    if (kv_heads, dim) != (cache.kv_heads, cache.dim):
+        raise ValueError(f"k {tuple(k.shape)}, a cache of {cache.kv_heads} heads of {cache.dim}")
+    if k.dtype != cache.k.dtype or v.dtype != cache.k.dtype:
+        raise TypeError(f"k and v are {k.dtype} and {v.dtype}, the cache {cache.k.dtype}")
+    rot = 0
+    if freqs is not None:
+        if freqs.dtype != torch.float32 or freqs.dim() != 1 or not freqs.is_contiguous() or 2 * len(freqs) > dim:
+            raise ValueError(f"freqs: a contiguous float32 tensor of at most {dim // 2}")
+        rot = 2 * len(freqs)
+    if positions is not None and (positions.dtype != torch.int64 or positions.shape != (tk,)
+                                  or not positions.is_contiguous()):
+        raise ValueError(f"positions: a contiguous int64 tensor of {tk}")
+    heads = q_token = q_head = o_token = o_head = 0
+    if q is not None:
+        tq, heads, q_dim, q_token, q_head = _heads_of(q, "q")
+        if (tq, q_dim) != (tk, dim) or heads == 0:
+            raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)} do not fit together")
+        if q.dtype != k.dtype:
+            raise TypeError(f"q is {q.dtype}, k {k.dtype}")
+    elif out is not None:
+        raise ValueError("out without q")
+    with _on(k.device, stream):
+        if q is not None:
+            if out is None:
+                bare = docs.covered is not None and docs.covered < tk
+                out = (torch.zeros if bare else torch.empty)(q.shape, dtype=q.dtype, device=q.device)
+                o_token, o_head = heads * dim, dim
+            else:
+                if out.dtype != q.dtype or out.shape != q.shape:
+                    raise ValueError("out must be like q")
+                _, _, _, o_token, o_head = _heads_of(out, "out")
+        _same_device(k, v, q, out, cache.k, freqs, positions, docs.table)
+        a = _APPEND.pack(_ptr(q) or 0, k.data_ptr(), v.data_ptr(), _ptr(out) or 0, cache.k.data_ptr(),
+                         cache.v.data_ptr(), docs.table.data_ptr(), cache.pages.data_ptr(), _ptr(freqs) or 0,
+                         _ptr(positions) or 0, tk, cache.n_pages, cache.pages.numel(), docs.max_q, q_token, q_head,
+                         k_token, k_head, v_token, v_head, o_token, o_head, *cache._k, *cache._v, docs.count, heads,
+                         kv_heads, dim, cache.rows, rot, 1 if interleaved else 0, cache.dtype)
+        _check(lib.mezo_cache_append(a, _stream_ptr(None)), "mezo_cache_append")
+    if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad):
+        for t in (out, cache.k, cache.v):
+            if t is not None:
+                _no_backward("cache_append", (t,), q, k, v)
+    return out
+
+
+def paged_attention(q, cache: PagedCache, docs: Documents, tree=None, causal: bool = True, scale: float | None = None,
+                    softcap: float = 0.0, slopes=None, out=None, return_lse: bool = False, stream=None):
+    """Attention of documents over a paged cache (mezo_paged_attention): q
+    [tokens, heads, dim] like the cache, docs with each document's first entry of
+    ``cache.pages`` as its k_first (``cache.documents`` makes them). tree, int64
+    [tokens, words] as of tree_mask: the documents' new tokens are drafted in
+    trees. Everything else as in attention."""
+    tq, heads, dim, q_token, q_head = _heads_of(q, "q")
+    if dim != cache.dim:
+        raise ValueError(f"q {tuple(q.shape)}, a cache of heads of {cache.dim}")
+    if cache.kv_heads == 0 or heads % cache.kv_heads:
+        raise ValueError(f"{heads} heads over {cache.kv_heads} key/value heads")
+    if q.dtype != cache.k.dtype:
+        raise TypeError(f"q is {q.dtype}, the cache {cache.k.dtype}")
+    if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (heads,) or not slopes.is_contiguous()):
+        raise ValueError(f"slopes: a contiguous float32 tensor of {heads}")
+    words = 0
+    if tree is not None:
+        if tree.dtype != torch.int64 or tree.dim() != 2 or tree.shape[0] != tq or not tree.is_contiguous():
+            raise ValueError(f"tree: a contiguous int64 tensor [{tq}, words]")
+        if slopes is not None or not causal:
+            raise ValueError("a tree's tokens have no distance and no other order: no slopes, causal")
+        words = tree.shape[1]
+        if words == 0 and tq:
+            raise ValueError("tree: no words")
+    with _on(q.device, stream):
+        bare = docs.covered is not None and docs.covered < tq  # some tokens are of no document
+        if out is None:
+            out = (torch.zeros if bare else torch.empty)((tq, heads, dim), dtype=q.dtype, device=q.device)
+            o_token, o_head = heads * dim, dim
+        else:
+            if out.dtype != q.dtype or out.shape != q.shape:
+                raise ValueError("out must be like q")
+            _, _, _, o_token, o_head = _heads_of(out, "out")
+        _same_device(q, cache.k, out, slopes, tree, docs.table)
+        lse = torch.empty((tq, heads), dtype=torch.float32, device=q.device) if return_lse else None
+        if bare and return_lse:
+            lse.fill_(-math.inf)
+        (k_page, k_row, k_head), (v_page, v_row, v_head) = cache._k, cache._v
+        a = _ATTENTION.pack(q.data_ptr(), cache.k.data_ptr(), cache.v.data_ptr(), out.data_ptr(), _ptr(lse) or 0,
+                            docs.table.data_ptr(), _ptr(slopes) or 0, tq, 0, q_token, q_head, k_row, k_head,
+                            v_row, v_head, o_token, o_head, docs.max_q, docs.max_k, docs.count, heads,
+                            cache.kv_heads, dim, cache.dtype, 1 if causal else 0,
+                            1.0 / math.sqrt(dim) if scale is None else scale, softcap)
+        c = _PAGES.pack(cache.pages.data_ptr(), _ptr(tree) or 0, cache.pages.numel(), cache.n_pages, k_page, v_page,
+                        cache.rows, words)
+        nbytes = lib.mezo_paged_attention_workspace(a, c)
+        ws = _scratch(nbytes, q.device)
+        _check(lib.mezo_paged_attention(a, c, _ptr(ws), nbytes, _stream_ptr(None)), "mezo_paged_attention")
+    if q.requires_grad or cache.k.requires_grad or cache.v.requires_grad or (slopes is not None and slopes.requires_grad):
+        _no_backward("paged_attention", (out, lse) if return_lse else (out,), q, cache.k, cache.v, slopes)
     return (out, lse) if return_lse else out
 
 
