@@ -563,6 +563,23 @@ MEZO_API uint64_t mezo_paged_attention_workspace(const mezo_attention_t* a, cons
 MEZO_API int mezo_paged_attention(const mezo_attention_t* a, const mezo_pages_t* pages, void* workspace,
                                   uint64_t workspace_bytes, void* stream);
 
+/* A layer's product with weights in 4-bit storage: c = x w^T, x [m, k] of storage
+ * x_dtype (rows ldx elements apart), w [n, k] an MEZO_NF4 tensor of n * k
+ * elements as under mezo_tensor_t (blocks of 64 of the flattened matrix, also where
+ * they run over the ends of rows), c [m, n] of storage c_dtype (rows ldc apart;
+ * MEZO_F32 or MEZO_BF16 both). w has the values that mezo_nf4_dequantize gives in
+ * x_dtype: v[code] * absmax rounded to fp32, and for MEZO_BF16 to bf16. The products are
+ * summed in fp32 (for MEZO_F32 but for parts below 2^-24 of a product, and what lies
+ * below 2^-133 of values below 2^-110) and the sum is rounded once. A row of x that holds NaN or
+ * an infinity, and a block whose absmax is one, give results that are not finite. 1 <= m, n <=
+ * MEZO_F8_MAX_ROWS, 1 <= k <= MEZO_F8_MAX_COLS, m * k, n * k and m * n <= MEZO_MAX_NUMEL,
+ * ldx >= k and ldc >= n where m > 1, codes and absmax 16-byte aligned (MEZO_EINVAL); c and the workspace
+ * must not overlap anything else (MEZO_EOVERLAP). */
+MEZO_API uint64_t mezo_nf4_linear_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t x_dtype, uint32_t c_dtype);
+MEZO_API int mezo_nf4_linear(const void* x, uint32_t x_dtype, uint64_t ldx, const void* codes, const float* absmax,
+                             uint64_t m, uint64_t n, uint64_t k, void* c, uint32_t c_dtype, uint64_t ldc,
+                             void* workspace, uint64_t workspace_bytes, void* stream);
+
 /* The loss of a forward pass: for each of `rows` tokens with target y =
  * targets[t] >= 0, losses[t] = ln sum_v exp(x_tv) - x_ty over the token's
  * `vocab` logits (storage dtype, rows ld elements apart); tokens with a

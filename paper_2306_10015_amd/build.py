@@ -83,7 +83,8 @@ KERNEL_UNITS = ["engine_dense.hip", "engine_nf4.hip", "nf4_convert.hip", "checks
 #: Those of the forward pass's operators. Their matrix tiles fill a wave's
 #: registers on purpose, so they are recorded apart from the engine's kernels,
 #: which keep to 128.
-FORWARD_UNITS = ["attention.hip", "paged_attention.hip", "cache_append.hip", "f8.hip", "token_loss.hip"]
+FORWARD_UNITS = ["attention.hip", "paged_attention.hip", "cache_append.hip", "f8.hip", "nf4_linear.hip",
+                 "token_loss.hip"]
 #: Host units.
 HOST_UNITS = ["api.cpp", "forward.cpp", "generation.cpp"]
 

@@ -11,6 +11,7 @@
 #include "cache_append_launch.hpp"
 #include "checks.hpp"
 #include "host.hpp"
+#include "nf4_linear_launch.hpp"
 
 namespace {
 
@@ -304,9 +305,67 @@ int paged_attention(const mezo_attention_t* pa, const mezo_pages_t* pc, void* wo
     return MEZO_OK;
 }
 
+// ---- products with 4-bit weights ---------------------------------------------------
+
+bool nf4_sizes(uint64_t m, uint64_t n, uint64_t k)
+{
+    return m >= 1 && n >= 1 && k >= 1 && m <= MEZO_F8_MAX_ROWS && n <= MEZO_F8_MAX_ROWS && k <= MEZO_F8_MAX_COLS &&
+           n <= MEZO_MAX_NUMEL / k && m <= MEZO_MAX_NUMEL / k && m <= MEZO_MAX_NUMEL / n;
+}
+
+int nf4_linear(const void* x, uint32_t x_dtype, uint64_t ldx, const void* codes, const float* absmax, uint64_t m,
+               uint64_t n, uint64_t k, void* c, uint32_t c_dtype, uint64_t ldc, void* workspace, uint64_t workspace_bytes,
+               void* stream)
+{
+    if (!dense(x_dtype) || !dense(c_dtype)) return MEZO_EDTYPE;
+    if (!x || !codes || !absmax || !c || !nf4_sizes(m, n, k) || (m > 1 && (ldx < k || ldc < n))) return MEZO_EINVAL;
+    if (!aligned(x, element_bytes(x_dtype)) || !aligned(c, element_bytes(c_dtype)) || !aligned(codes, 16) ||
+        !aligned(absmax, 16))
+        return MEZO_EINVAL;
+    const uint64_t need = nf4_space(m, n, k, x_dtype == MEZO_F32).bytes;
+    if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return MEZO_EINVAL;
+    uint64_t in = 0, out = 0;
+    if (!matrix_bytes(m, k, ldx, element_bytes(x_dtype), in) || !matrix_bytes(m, n, ldc, element_bytes(c_dtype), out))
+        return MEZO_EINVAL;
+    const Range all[5] = {{address(x), in}, {address(codes), (n * k + 1) / 2}, {address(absmax), (n * k + 63) / 64 * 4},
+                          {address(c), out}, {address(workspace), need}};
+    for (const Range& r : all)
+        if (!whole(r)) return MEZO_EINVAL;
+    if (clashes(all[3], all, 3) || (need && clashes(all[4], all, 4))) return MEZO_EOVERLAP;
+    NF4LinearArgs g;
+    g.x = address(x);
+    g.ldx = m > 1 ? ldx : k;
+    g.codes = address(codes);
+    g.absmax = address(absmax);
+    g.c = address(c);
+    g.ldc = m > 1 ? ldc : n;
+    g.workspace = address(workspace);
+    g.m = m;
+    g.n = n;
+    g.k = k;
+    g.x_dtype = x_dtype;
+    g.c_dtype = c_dtype;
+    MEZO_HIP(launch_nf4_linear(g, static_cast<hipStream_t>(stream)));
+    return MEZO_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+uint64_t mezo_nf4_linear_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t x_dtype, uint32_t c_dtype)
+{
+    return dense(x_dtype) && dense(c_dtype) && nf4_sizes(m, n, k) ? nf4_space(m, n, k, x_dtype == MEZO_F32).bytes : 0;
+}
+
+int mezo_nf4_linear(const void* x, uint32_t x_dtype, uint64_t ldx, const void* codes, const float* absmax, uint64_t m,
+                    uint64_t n, uint64_t k, void* c, uint32_t c_dtype, uint64_t ldc, void* workspace,
+                    uint64_t workspace_bytes, void* stream)
+{
+    return guarded("mezo_nf4_linear", [&] {
+        return nf4_linear(x, x_dtype, ldx, codes, absmax, m, n, k, c, c_dtype, ldc, workspace, workspace_bytes, stream);
+    });
+}
 
 int mezo_cache_append(const mezo_append_t* a, void* stream)
 {

@@ -1,0 +1,388 @@
+// nf4_linear.hip — c = x w^T with weights in 4-bit storage, which are not written out in full:
+// w_e = v[code_e] absmax[e / 64] of the flattened matrix [n, k], as mezo_nf4_dequantize gives
+// it in the type of x (fp32, or that rounded to bf16). Products are summed in fp32 and the sum
+// is rounded once.
+//
+// bf16: the products of bf16 are exact in v_mfma_f32_16x16x32_bf16. fp32: each operand is
+// three bf16, its 24 bits in 8 and 8 and 8 by cutting (so that the largest floats stay finite),
+// and six of the nine products are summed, all above 2^-24 of the whole. The parts of a value
+// below 2^-110 end at bf16's last bit, 2^-133; one that is infinite or NaN makes its row NaN.
+//
+// Many rows: a slab of the weights is expanded into the workspace (2 bytes an element, 6 for
+// fp32), and a tiled product reads it. Expanding costs 2.5 bytes an element once, the product
+// 2 m operations: from a few hundred rows on it does not show.
+#include <type_traits>
+
+#include "lds_dma.hpp"
+#include "nf4.hpp"
+#include "nf4_linear_launch.hpp"
+#include "records.hpp"
+#include "stream_io.hpp"
+
+namespace mezo {
+
+typedef float v4f_t __attribute__((ext_vector_type(4)));
+typedef __bf16 v4bf_t __attribute__((ext_vector_type(4)));
+typedef __bf16 v8bf_t __attribute__((ext_vector_type(8)));
+typedef MEZO_GLOBAL uint8_t gu8_t;
+typedef MEZO_GLOBAL uint32_t gu32_t;
+
+// ---- laying out ------------------------------------------------------------------
+
+// The upper 16 bits of two floats.
+__device__ __forceinline__ uint32_t upper_halves(float lo, float hi)
+{
+    return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+}
+
+// What is left of a float after its first 8 bits; 0 where it is not finite (its first part
+// says all there is).
+__device__ __forceinline__ float after_first(float x)
+{
+    const float r = x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+    return r == r ? r : 0.0f;
+}
+
+// Eight values as one or three planes of bf16, 16 bytes each.
+template <bool kWide>
+__device__ __forceinline__ void store_planes(uint64_t at, uint64_t plane, const float (&x)[8])
+{
+    if constexpr (kWide) {
+        float r[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = x[i] == x[i] ? x[i] : __builtin_nanf("");  // (cut, a NaN's bits must not be an infinity's)
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            uint32_t u[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = upper_halves(r[2 * i], r[2 * i + 1]);
+            *reinterpret_cast<gu32x4_t*>(at + p * plane) = u32x4_t{u[0], u[1], u[2], u[3]};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[i] = after_first(r[i]);
+        }
+    } else {
+        v8bf_t b;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = static_cast<__bf16>(x[i]);
+        *reinterpret_cast<gu32x4_t*>(at) = __builtin_bit_cast(u32x4_t, b);
+    }
+}
+
+struct LayArgs {
+    uint64_t from, absmax;  // values and nothing, or codes and scales
+    uint64_t ld;            // values: elements from one row to the next
+    uint64_t to, plane;     // rows of `columns` bf16; bytes from one plane to the next
+    uint64_t first, last;   // codes: the first row's first element, and the end of all
+    uint64_t rows, k, columns;
+};
+
+// Rows of values into planes: a lane 8 columns.
+template <bool kF>
+__global__ void __launch_bounds__(256) nf4_lay_values_kernel(LayArgs a)
+{
+    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x, per_row = a.columns / 8;
+    if (i >= a.rows * per_row) return;
+    const uint64_t row = i / per_row, c = (i - row * per_row) * 8;
+    float x[8];
+#pragma unroll
+    for (uint32_t j = 0; j < 8; ++j) {
+        x[j] = 0.0f;
+        if (c + j < a.k) {
+            const uint64_t e = row * a.ld + c + j;
+            if constexpr (kF)
+                x[j] = reinterpret_cast<const gfloat_t*>(a.from)[e];
+            else
+                x[j] = __uint_as_float(uint32_t(reinterpret_cast<const gu16_t*>(a.from)[e]) << 16);
+        }
+    }
+    store_planes<kF>(a.to + i * 16, a.plane, x);
+}
+
+// The codes of elements e .. e + 7, of `last` in all.
+__device__ __forceinline__ uint32_t eight_codes(uint64_t codes, uint64_t e, uint64_t last)
+{
+    auto word = [&](uint64_t i) {
+        const uint64_t bytes = (last + 1) / 2;
+        if (4 * i + 4 <= bytes) return reinterpret_cast<const gu32_t*>(codes)[i];
+        uint32_t w = 0;
+        for (uint64_t b = 4 * i; b < bytes; ++b) w |= uint32_t(reinterpret_cast<const gu8_t*>(codes)[b]) << (8 * (b - 4 * i));
+        return w;
+    };
+    const uint32_t shift = uint32_t(e & 7u) * 4;
+    const uint32_t lo = word(e >> 3);
+    if (shift == 0) return lo;
+    return uint32_t((uint64_t(word((e >> 3) + 1)) << 32 | lo) >> shift);
+}
+
+// Rows of weights into planes: a lane 8 columns.
+template <bool kWide>
+__global__ void __launch_bounds__(256) nf4_expand_kernel(LayArgs a)
+{
+    __shared__ float table[kNF4Codes];
+    if (threadIdx.x < kNF4Codes) table[threadIdx.x] = kNF4Values[threadIdx.x];
+    __syncthreads();
+    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x, per_row = a.columns / 8;
+    if (i >= a.rows * per_row) return;
+    const uint64_t row = i / per_row, c = (i - row * per_row) * 8;
+    float x[8] = {};
+    if (c < a.k) {
+        const uint64_t e = a.first + row * a.k + c, top = (a.last - 1) / kNF4Block;
+        const uint32_t d = eight_codes(a.from, e, a.last);
+        const uint64_t b0 = e / kNF4Block, b1 = b0 < top ? b0 + 1 : top;
+        const float s0 = reinterpret_cast<const gfloat_t*>(a.absmax)[b0], s1 = reinterpret_cast<const gfloat_t*>(a.absmax)[b1];
+        const uint32_t left = kNF4Block - uint32_t(e % kNF4Block);
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+            if (c + j < a.k) x[j] = table[d >> (4 * j) & 15u] * (j < left ? s0 : s1);
+    }
+    store_planes<kWide>(a.to + i * 16, a.plane, x);
+}
+
+// ---- the product of what was laid out ------------------------------------------------
+
+struct NF4MatmulArgs {
+    uint64_t x, w;              // first planes
+    uint64_t x_plane, w_plane;  // bytes from one plane to the next
+    uint64_t c, ldc;
+    uint64_t partial;           // fp32 [splits, m, n rounded up to 4] of a split product
+    uint32_t m, n, stages;      // 64 columns each
+    uint32_t x_row, w_row;      // bytes
+    uint32_t splits;
+};
+
+template <bool kWideOut>
+__device__ __forceinline__ void store4(const NF4MatmulArgs& a, bool whole, uint32_t row, uint32_t col, v4f_t v)
+{
+    using Out = std::conditional_t<kWideOut, float, __bf16>;
+    typedef Out out4_t __attribute__((ext_vector_type(4)));
+    const out4_t b = __builtin_convertvector(v, out4_t);
+    MEZO_GLOBAL Out* p = reinterpret_cast<MEZO_GLOBAL Out*>(a.c) + row * a.ldc + col;
+    if (whole && col + 4 <= a.n) {
+        *reinterpret_cast<MEZO_GLOBAL out4_t*>(p) = b;
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            if (col + i < a.n) p[i] = b[i];
+    }
+}
+
+template <bool kWideOut>
+__device__ __forceinline__ bool whole_groups(const NF4MatmulArgs& a)
+{
+    constexpr uint64_t kBytes = kWideOut ? 4 : 2;
+    return ((a.c | (a.ldc * kBytes)) & (4 * kBytes - 1)) == 0;
+}
+
+__device__ __forceinline__ uint64_t partial_at(const NF4MatmulArgs& a, uint32_t split, uint32_t row, uint32_t col)
+{
+    return a.partial + ((uint64_t(split) * a.m + row) * ((a.n + 3) / 4) + col / 4) * 16;
+}
+
+// The pairs of planes of an fp32 product, the smallest first: (x's, w's).
+__device__ __forceinline__ uint32_t plane_of_x(uint32_t pair) { return 0x001021u >> (4 * pair) & 15u; }
+__device__ __forceinline__ uint32_t plane_of_w(uint32_t pair) { return 0x010201u >> (4 * pair) & 15u; }
+
+// Tiles of kBM activations x kBN weights, kWM x kWN waves. Weights are the matrix
+// instruction's rows and activations its columns, so that a lane's four results lie next to
+// each other in a row of c. A stage is 64 columns (128 bytes) of every row of the tile, loaded
+// straight into LDS, two stages, one computed on while the other loads. A row's eight 16-byte
+// chunks are stored at chunk ^ ((row / 2) & 7): the 16 rows of a fragment then spread over all
+// 64 banks. fp32: the loop goes over the pairs of planes one after another.
+template <uint32_t kBM, uint32_t kBN, uint32_t kWM, uint32_t kWN, bool kWide, bool kWideOut>
+__global__ void __launch_bounds__(kWM* kWN * 64) nf4_matmul_kernel(NF4MatmulArgs a)
+{
+    constexpr uint32_t kWaves = kWM * kWN, kRows = kBM + kBN;
+    constexpr uint32_t kFM = kBM / kWM / 16, kFN = kBN / kWN / 16;  // fragments of a wave
+    constexpr uint32_t kLoads = kRows / 8 / kWaves;                 // 8 rows a load
+    static_assert(kRows % (8 * kWaves) == 0 && kBM % 64 == 0 && kBN % 64 == 0);
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][kRows * 128];
+
+    const uint32_t l = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // workgroups go round the 8 XCDs: each XCD gets a compact part of c (its L2 then holds the
+    // rows its workgroups share), in groups of 8 tile rows
+    const uint32_t tm = (a.m + kBM - 1) / kBM, tn = (a.n + kBN - 1) / kBN, tiles = tm * tn;
+    const uint32_t xcd = blockIdx.x % 8, each = tiles / 8, rest = tiles % 8;
+    const uint32_t id = blockIdx.x / 8 + xcd * each + (xcd < rest ? xcd : rest);
+    const uint32_t band = id / (8 * tn), height = tm - band * 8 < 8 ? tm - band * 8 : 8;
+    const uint32_t in = id - band * 8 * tn;
+    const uint32_t m0 = (band * 8 + in % height) * kBM, n0 = in / height * kBN;
+
+    const uint32_t all = (kWide ? 6 : 1) * a.stages;
+    const uint32_t begin = uint32_t(uint64_t(all) * blockIdx.y / a.splits),
+                   end = uint32_t(uint64_t(all) * (blockIdx.y + 1) / a.splits);
+    // a load is 8 rows of x or of w; rows past the end: the last one's again
+    const uint64_t x0 = a.x + uint64_t(m0) * a.x_row, w0 = a.w + uint64_t(n0) * a.w_row;
+    const uint32_t xlast = a.m - m0 - 1, wlast = a.n - n0 - 1;
+    uint32_t src[kLoads];  // this lane's 16 bytes of each of its rows
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) {
+        const uint32_t first = (wave * kLoads + i) * 8;
+        const bool ofx = first < kBM;
+        const uint32_t r = first + (l >> 3) - (ofx ? 0 : kBM), last = ofx ? xlast : wlast;
+        const uint32_t swizzle = (first / 2 + (l >> 4)) & 7u;  // (row / 2) & 7
+        src[i] = (r < last ? r : last) * (ofx ? a.x_row : a.w_row) + ((l & 7u) ^ swizzle) * 16;
+    }
+    const uint32_t lds0 = lds_offset(&lds[0][0]) + wave * kLoads * 1024;
+    auto stage = [&](uint32_t s, uint32_t buffer) {
+        uint64_t xs = x0, ws = w0;
+        uint32_t kb = s;
+        if constexpr (kWide) {
+            const uint32_t pair = s / a.stages;
+            kb = s - pair * a.stages;
+            xs += plane_of_x(pair) * a.x_plane;
+            ws += plane_of_w(pair) * a.w_plane;
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i)
+            dma_to_lds(((wave * kLoads + i) * 8 < kBM ? xs : ws) + uint64_t(kb) * 128, src[i],
+                       lds0 + buffer * kRows * 128 + i * 1024);
+    };
+
+    const uint32_t fr = l & 15u, fg = l >> 4;
+    const uint32_t wm = (wave / kWN) * kFM * 16, wn = (wave % kWN) * kFN * 16;
+    v4f_t acc[kFM][kFN] = {};
+    stage(begin, 0);
+    for (uint32_t s = begin; s < end; ++s) {
+        const uint32_t buffer = (s - begin) & 1u;
+        dma_wait();
+        lds_barrier();  // stage s is there, and nobody reads the other one any more
+        if (s + 1 < end) stage(s + 1, buffer ^ 1u);
+        const uint8_t* t = lds[buffer];
+        struct Fragment {
+            v8bf_t v[2];
+        };
+        auto fragment = [&](uint32_t row) {
+            const uint32_t r = row + fr;
+            Fragment f;
+            f.v[0] = *reinterpret_cast<const v8bf_t*>(t + r * 128 + ((fg ^ (fr >> 1)) * 16));
+            f.v[1] = *reinterpret_cast<const v8bf_t*>(t + r * 128 + (((fg + 4) ^ (fr >> 1)) * 16));
+            return f;
+        };
+        Fragment w[kFN], next = fragment(wm);
+#pragma unroll
+        for (uint32_t j = 0; j < kFN; ++j) w[j] = fragment(kBM + wn + j * 16);
+#pragma unroll
+        for (uint32_t i = 0; i < kFM; ++i) {
+            const Fragment x = next;
+            if (i + 1 < kFM) next = fragment(wm + (i + 1) * 16);
+#pragma unroll
+            for (uint32_t j = 0; j < kFN; ++j)
+#pragma unroll
+                for (uint32_t h = 0; h < 2; ++h)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j].v[h], x.v[h], acc[i][j], 0, 0, 0);
+        }
+    }
+    const bool whole = whole_groups<kWideOut>(a);
+#pragma unroll
+    for (uint32_t i = 0; i < kFM; ++i) {
+        const uint32_t row = m0 + wm + i * 16 + fr;
+        if (row >= a.m) continue;
+#pragma unroll
+        for (uint32_t j = 0; j < kFN; ++j) {
+            const uint32_t col = n0 + wn + j * 16 + fg * 4;
+            if (a.splits == 1)
+                store4<kWideOut>(a, whole, row, col, acc[i][j]);
+            else if (col < a.n)
+                *reinterpret_cast<MEZO_GLOBAL v4f_t*>(partial_at(a, blockIdx.y, row, col)) = acc[i][j];
+        }
+    }
+}
+
+// The sums of a product whose k was split, joined in the order of the splits.
+template <bool kWideOut>
+__global__ void __launch_bounds__(256) nf4_join_kernel(NF4MatmulArgs a)
+{
+    const uint32_t groups = (a.n + 3) / 4;
+    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= uint64_t(a.m) * groups) return;
+    const uint32_t row = uint32_t(i / groups), col = uint32_t(i % groups) * 4;
+    v4f_t sum = {};
+    for (uint32_t s = 0; s < a.splits; ++s)
+        sum += *reinterpret_cast<const MEZO_GLOBAL v4f_t*>(partial_at(a, s, row, col));
+    store4<kWideOut>(a, whole_groups<kWideOut>(a), row, col, sum);
+}
+
+// ---- launches ---------------------------------------------------------------------
+
+template <class Args>
+hipError_t run(const void* f, dim3 grid, uint32_t lanes, Args& a, hipStream_t stream)
+{
+    void* params[] = {&a};
+    return hipLaunchKernel(f, grid, dim3(lanes), params, 0, stream);
+}
+
+template <bool kWide, bool kWideOut>
+hipError_t launch_tiled(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t stream)
+{
+    const uint64_t columns = nf4_columns(a.k), row = columns * 2;
+    const NF4Space space = nf4_space(a.m, a.n, a.k, kWide);
+    // bf16 activations that lie as the loads want them are read where they are
+    const bool direct = !kWide && columns == a.k && ((a.x | (a.ldx * 2)) & 15u) == 0 && a.ldx * 2 <= (1u << 24);
+    LayArgs lay = {};
+    lay.k = a.k;
+    lay.columns = columns;
+    if (!direct) {
+        lay.from = a.x;
+        lay.ld = a.ldx;
+        lay.to = a.workspace;
+        lay.plane = a.m * row;
+        lay.rows = a.m;
+        const hipError_t e = run(reinterpret_cast<const void*>(nf4_lay_values_kernel<kWide>),
+                                 dim3(uint32_t((a.m * (columns / 8) + 255) / 256)), 256, lay, stream);
+        if (e != hipSuccess) return e;
+    }
+    NF4MatmulArgs g = {};
+    g.x = direct ? a.x : a.workspace;
+    g.x_row = uint32_t(direct ? a.ldx * 2 : row);
+    g.x_plane = a.m * row;
+    g.w = a.workspace + space.weights;
+    g.w_row = uint32_t(row);
+    g.w_plane = cut.slab * row;
+    g.ldc = a.ldc;
+    g.partial = a.workspace + space.partial;
+    g.m = uint32_t(a.m);
+    g.stages = uint32_t(columns / 64);
+    g.splits = cut.splits;
+    lay.from = a.codes;
+    lay.absmax = a.absmax;
+    lay.to = g.w;
+    lay.plane = g.w_plane;
+    lay.last = a.n * a.k;
+    for (uint64_t n0 = 0; n0 < a.n; n0 += cut.slab) {
+        lay.rows = a.n - n0 < cut.slab ? a.n - n0 : cut.slab;
+        lay.first = n0 * a.k;
+        hipError_t e = run(reinterpret_cast<const void*>(nf4_expand_kernel<kWide>),
+                           dim3(uint32_t((lay.rows * (columns / 8) + 255) / 256)), 256, lay, stream);
+        if (e != hipSuccess) return e;
+        g.n = uint32_t(lay.rows);
+        g.c = a.c + n0 * (kWideOut ? 4 : 2);
+        auto go = [&](auto* f, uint64_t bm, uint64_t bn, uint32_t lanes) {
+            return run(reinterpret_cast<const void*>(f), dim3(uint32_t(tiles_of(a.m, lay.rows, bm, bn)), cut.splits), lanes,
+                       g, stream);
+        };
+        e = go(nf4_matmul_kernel<64, 64, 2, 2, kWide, kWideOut>, 64, 64, 256);
+        if (e != hipSuccess) return e;
+        if (cut.splits > 1) {
+            const uint64_t groups = a.m * ((lay.rows + 3) / 4);
+            e = run(reinterpret_cast<const void*>(nf4_join_kernel<kWideOut>), dim3(uint32_t((groups + 255) / 256)), 256, g,
+                    stream);
+            if (e != hipSuccess) return e;
+        }
+    }
+    return hipSuccess;
+}
+
+template <bool kWide, bool kWideOut>
+hipError_t launch_any(const NF4LinearArgs& a, hipStream_t stream)
+{
+    return launch_tiled<kWide, kWideOut>(a, cut_nf4(a.m, a.n, a.k, kWide), stream);
+}
+
+hipError_t launch_nf4_linear(const NF4LinearArgs& a, hipStream_t stream)
+{
+    if (a.x_dtype == kF32)
+        return a.c_dtype == kF32 ? launch_any<true, true>(a, stream) : launch_any<true, false>(a, stream);
+    return a.c_dtype == kF32 ? launch_any<false, true>(a, stream) : launch_any<false, false>(a, stream);
+}
+
+}  // namespace mezo

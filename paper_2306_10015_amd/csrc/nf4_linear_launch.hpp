@@ -1,0 +1,67 @@
+// nf4_linear_launch.hpp — how a product with 4-bit weights is cut, and the interface
+// between the C-ABI host code (generation.cpp) and its kernels (nf4_linear.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "plans.hpp"
+
+namespace mezo {
+
+// Rows of expanded weights and of activations laid out for the matrix instructions: whole
+// stages of 64 columns, zeros after the last.
+constexpr uint64_t nf4_columns(uint64_t k) { return (k + 63) / 64 * 64; }
+
+// fp32 activations (and the weights beside them) are three bf16 each.
+constexpr uint64_t nf4_planes(bool wide_x) { return wide_x ? 3 : 1; }
+
+// A product's cut: its tile, the workgroups that share out k, and the weights' rows that are
+// expanded at a time.
+struct NF4Cut {
+    F8Tile tile;
+    uint32_t splits;
+    uint64_t slab;
+};
+
+// Bytes of expanded weights at a time: what the last-level cache holds.
+constexpr uint64_t kNF4SlabBytes = 1ull << 28;
+
+inline NF4Cut cut_nf4([[maybe_unused]] uint64_t m, uint64_t n, uint64_t k, bool wide_x)
+{
+    const uint64_t row = nf4_columns(k) * 2 * nf4_planes(wide_x);
+    uint64_t slab = kNF4SlabBytes / row / 256 * 256;
+    if (slab < 256) slab = 256;
+    if (slab > n) slab = n;
+    return {k64x64, 1, slab};
+}
+
+// The parts of a call's workspace, from its start: activations laid out, weights expanded,
+// partial sums; all multiples of 16 bytes.
+struct NF4Space {
+    uint64_t weights, partial, bytes;
+};
+
+inline NF4Space nf4_space(uint64_t m, uint64_t n, uint64_t k, bool wide_x)
+{
+    const NF4Cut c = cut_nf4(m, n, k, wide_x);
+    const uint64_t row = nf4_columns(k) * 2 * nf4_planes(wide_x);
+    NF4Space s;
+    s.weights = m * row;
+    s.partial = s.weights + c.slab * row;
+    s.bytes = s.partial + (c.splits > 1 ? c.splits * m * ((c.slab + 3) / 4 * 16) : 0);
+    return s;
+}
+
+struct NF4LinearArgs {
+    uint64_t x, ldx;    // activations [m, k], elements from one row to the next
+    uint64_t codes, absmax;
+    uint64_t c, ldc;    // [m, n]
+    uint64_t workspace;
+    uint64_t m, n, k;
+    uint32_t x_dtype, c_dtype;
+};
+
+hipError_t launch_nf4_linear(const NF4LinearArgs& args, hipStream_t stream);
+
+}  // namespace mezo

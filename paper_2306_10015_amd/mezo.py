@@ -83,6 +83,7 @@ EXPORTS = ("mezo_paramset_create", "mezo_paramset_destroy", "mezo_paramset_numel
            "mezo_f8_quantize", "mezo_f8_matmul_workspace", "mezo_f8_matmul",
            "mezo_f8_linear_workspace", "mezo_f8_linear",
            "mezo_attention_workspace", "mezo_attention",
+           "mezo_nf4_linear_workspace", "mezo_nf4_linear",
            "mezo_cache_append", "mezo_paged_attention_workspace", "mezo_paged_attention",
            "mezo_token_loss_workspace", "mezo_token_loss", "mezo_debug_generate", "mezo_debug_box_muller",
            "mezo_strerror", "mezo_last_error", "mezo_version")
@@ -144,6 +145,10 @@ def _load() -> ctypes.CDLL:
     L.mezo_attention_workspace.restype = u64
     L.mezo_attention.argtypes = [vp, vp, u64, vp]
     L.mezo_attention.restype = i32
+    L.mezo_nf4_linear_workspace.argtypes = [u64, u64, u64, u32, u32]
+    L.mezo_nf4_linear_workspace.restype = u64
+    L.mezo_nf4_linear.argtypes = [vp, u32, u64, vp, vp, u64, u64, u64, vp, u32, u64, vp, u64, vp]
+    L.mezo_nf4_linear.restype = i32
     L.mezo_cache_append.argtypes = [vp, vp]
     L.mezo_cache_append.restype = i32
     L.mezo_paged_attention_workspace.argtypes = [vp, vp]
@@ -462,6 +467,36 @@ def f8_linear(x, w: F8Matrix, dtype=None, out=None, stream=None):
                                   out.data_ptr(), code, ldc, _ptr(ws), nbytes, _stream_ptr(None)), "mezo_f8_linear")
     if x.requires_grad:
         _no_backward("f8_linear", (out,), x)
+    return out
+
+
+def nf4_linear(x, w: NF4Tensor, dtype=None, out=None, stream=None):
+    """A layer's product with 4-bit weights: the activations x (fp32/bf16 [m, k],
+    contiguous rows) times w, an NF4 tensor of a [n, k] matrix: [m, n] of dtype (x's by
+    default). The values of w are those of nf4_dequantize(w, x.dtype), summed in
+    fp32 (mezo_nf4_linear)."""
+    m, k, ldx = _rows_of(x, "x")
+    if w.numel() == 0 or w.numel() % k:
+        raise ValueError(f"x has {k} columns, w {w.numel()} elements")
+    n, x_code = w.numel() // k, _dtype_code(x)
+    with _on(x.device, stream):
+        if out is None:
+            out = torch.empty(m, n, dtype=dtype or x.dtype, device=x.device)
+            ldc = n
+        else:
+            if dtype is not None and out.dtype != dtype:
+                raise TypeError(f"out is {out.dtype}, dtype {dtype}")
+            if out.shape != (m, n):
+                raise ValueError(f"out is {tuple(out.shape)}, the product {(m, n)}")
+            ldc = _rows_of(out, "out")[2]
+        _same_device(x, w.codes, w.absmax, out)
+        code = _dtype_code(out)
+        nbytes = lib.mezo_nf4_linear_workspace(m, n, k, x_code, code)
+        ws = _scratch(nbytes, x.device)
+        _check(lib.mezo_nf4_linear(x.data_ptr(), x_code, ldx, w.codes.data_ptr(), w.absmax.data_ptr(), m, n, k,
+                                   out.data_ptr(), code, ldc, _ptr(ws), nbytes, _stream_ptr(None)), "mezo_nf4_linear")
+    if x.requires_grad:
+        _no_backward("nf4_linear", (out,), x)
     return out
 
 

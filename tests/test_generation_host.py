@@ -152,3 +152,41 @@ def test_cache_refuses_what_it_cannot_hold():
 def test_error_of_a_missing_handle_is_a_code():
     assert L.mezo_paged_attention(None, None, None, 0, None) == mezo.EINVAL
     assert ctypes.sizeof(ctypes.c_void_p) == 8
+
+
+# ---- products with 4-bit weights -----------------------------------------------------
+
+def linear(x=Q, x_dtype=mezo.BF16, ldx=256, codes=K, absmax=V, m=4, n=8, k=256, c=O, c_dtype=mezo.F32, ldc=8, work=W,
+           size=None):
+    if size is None:
+        size = L.mezo_nf4_linear_workspace(m, n, k, x_dtype, c_dtype)
+    return L.mezo_nf4_linear(x, x_dtype, ldx, codes, absmax, m, n, k, c, c_dtype, ldc, work, size, None)
+
+
+def test_linear_refusals():
+    for bad in (dict(x=None), dict(codes=None), dict(absmax=None), dict(c=None), dict(m=0), dict(n=0), dict(k=0),
+                dict(ldx=255), dict(ldc=7), dict(x=Q + 1), dict(x_dtype=mezo.F32, x=Q + 2), dict(c=O + 2),
+                dict(codes=K + 8), dict(absmax=V + 4), dict(k=(1 << 23) + 1, ldx=1 << 24), dict(m=(1 << 30) + 1),
+                dict(n=(1 << 30) + 1, ldc=1 << 31), dict(n=1 << 20, k=1 << 20, ldx=1 << 20, ldc=1 << 20),
+                dict(m=1 << 20, n=1 << 20, ldc=1 << 20), dict(ldx=1 << 63), dict(ldc=1 << 62), dict(x=2 ** 64 - 64),
+                dict(c=2 ** 64 - 32)):
+        assert linear(**bad) == mezo.EINVAL, bad
+    assert linear(x_dtype=mezo.NF4) == mezo.EDTYPE
+    assert linear(c_dtype=5) == mezo.EDTYPE
+    for bad in (dict(c=Q), dict(c=K + 128), dict(c=V), dict(c=Q + 4 * 256 * 2 - 4)):
+        assert linear(**bad) == mezo.EOVERLAP, bad
+
+
+def test_linear_workspace():
+    big = dict(m=500, n=1000, k=1000, ldx=1000, ldc=1000)
+    need = L.mezo_nf4_linear_workspace(500, 1000, 1000, mezo.BF16, mezo.F32)
+    assert need > 0
+    assert linear(**big, work=None) == mezo.EINVAL
+    assert linear(**big, size=need - 1) == mezo.EINVAL
+    assert linear(**big, work=W + 8) == mezo.EINVAL
+    for other in (Q, K, V, O):
+        assert linear(**big, work=other) == mezo.EOVERLAP
+    for bad in ((0, 1, 1, 0, 0), (1, 0, 1, 0, 0), (1, 1, 0, 0, 0), (1, 1, 1, 2, 0), (1, 1, 1, 0, 9), (1 << 31, 1, 1, 0, 0)):
+        assert L.mezo_nf4_linear_workspace(*bad) == 0
+    # a matrix of any size is expanded a slab at a time
+    assert L.mezo_nf4_linear_workspace(100, 50272, 16384, mezo.BF16, mezo.BF16) < 300 << 20
