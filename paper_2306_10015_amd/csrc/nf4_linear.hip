@@ -98,6 +98,20 @@ __global__ void __launch_bounds__(256) nf4_lay_values_kernel(LayArgs a)
     store_planes<kF>(a.to + i * 16, a.plane, x);
 }
 
+// Rows of whole blocks of values, copied next to each other: a lane 8 columns.
+template <bool kF>
+__global__ void __launch_bounds__(256) nf4_copy_rows_kernel(LayArgs a)
+{
+    using element_t = std::conditional_t<kF, gu32_t, gu16_t>;
+    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x, per_row = a.columns / 8;
+    if (i >= a.rows * per_row) return;
+    const uint64_t row = i / per_row, c = (i - row * per_row) * 8;
+    const element_t* from = reinterpret_cast<const element_t*>(a.from) + row * a.ld + c;
+    element_t* to = reinterpret_cast<element_t*>(a.to) + i * 8;
+#pragma unroll
+    for (uint32_t j = 0; j < 8; ++j) to[j] = from[j];
+}
+
 // The codes of elements e .. e + 7, of `last` in all.
 __device__ __forceinline__ uint32_t eight_codes(uint64_t codes, uint64_t e, uint64_t last)
 {
@@ -302,6 +316,265 @@ __global__ void __launch_bounds__(256) nf4_join_kernel(NF4MatmulArgs a)
     store4<kWideOut>(a, whole_groups<kWideOut>(a), row, col, sum);
 }
 
+// ---- few rows -----------------------------------------------------------------------
+
+// A product of few activations reads each weight once and is bound by that as long as decoding
+// stays cheap. A byte of codes is looked up whole: `pairs` holds the two values of each byte,
+// 32 times over, a copy for each lane of a half wave, so that a lane's lookups never meet
+// another's bank; the address is the byte in bits 8 .. 15 and the lane below, one v_perm_b32.
+// Then a multiplication by the block's scale each and one conversion: 2 vector instructions a
+// weight in bf16 (selecting by v_perm_b32 out of registers takes 4).
+//
+// A workgroup takes kRowWaves * kRG * 16 of the weights' rows and a share of k; its waves are
+// kRowWaves x kKWaves: a stage is one block of 64 for each of the kKWaves, of all the rows,
+// with their scales and the activations beside them, loaded straight into LDS kDepth - 1
+// stages ahead. The order of k within a block does not matter as long as both operands agree:
+// a lane takes 16 weights next to each other. The waves' sums join in LDS, in their order.
+struct NF4ThinArgs {
+    uint64_t x, codes, absmax, c, ldc, partial;
+    uint32_t m, n, blocks;  // blocks of 64 of a row
+    uint32_t x_row;         // bytes
+    uint32_t splits;
+};
+
+typedef float v2f_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+
+// A float as three bf16 by cutting, eight at a time.
+struct Planes {
+    v8bf_t p[3];
+};
+
+__device__ __forceinline__ Planes planes_of(const float (&x)[8])
+{
+    Planes o;
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+        uint32_t u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = upper_halves(r[2 * i], r[2 * i + 1]);
+        o.p[p] = __builtin_bit_cast(v8bf_t, u32x4_t{u[0], u[1], u[2], u[3]});
+        if (p < 2)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[i] -= __uint_as_float(__float_as_uint(r[i]) & 0xFFFF0000u);
+    }
+    return o;
+}
+
+// c + w x of split operands, the smallest products first.
+__device__ __forceinline__ v4f_t product(const Planes& w, const Planes& x, v4f_t c)
+{
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.p[1], x.p[1], c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.p[0], x.p[2], c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.p[2], x.p[0], c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.p[0], x.p[1], c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.p[1], x.p[0], c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.p[0], x.p[0], c, 0, 0, 0);
+}
+
+constexpr uint32_t kThinWaves = 8;
+
+template <bool kF, uint32_t kRowWaves, uint32_t kRG, uint32_t kXRows, uint32_t kDepth, bool kWideOut>
+__global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a)
+{
+    constexpr uint32_t kKWaves = kThinWaves / kRowWaves, kRows = kRowWaves * kRG * 16;
+    constexpr uint32_t kFM = kXRows < 16 ? 1 : kXRows / 16;
+    constexpr uint32_t kElement = kF ? 4 : 2;
+    // a stage in LDS: codes [kRows][kCodeChunks], activations [kXRows][kXChunks] of 16 bytes,
+    // scales [kRows][kKWaves] of 4
+    constexpr uint32_t kCodeChunks = kKWaves * 2, kXChunks = kKWaves * 4 * kElement;
+    constexpr uint32_t kCodeLoads = kRows * kCodeChunks / 64, kXLoads = kXRows * kXChunks / 64,
+                       kScaleLoads = kRows * kKWaves / 64;
+    constexpr uint32_t kXAt = kCodeLoads * 1024, kScaleAt = kXAt + kXLoads * 1024,
+                       kStage = kScaleAt + kScaleLoads * 256;
+    static_assert(kRows * kCodeChunks % 64 == 0 && kXRows * kXChunks % 64 == 0 && kRows * kKWaves % 64 == 0);
+    constexpr uint32_t kLoads = kCodeLoads + kXLoads + kScaleLoads, kPerWave = (kLoads + kThinWaves - 1) / kThinWaves;
+    __shared__ __attribute__((aligned(1024))) v2f_t pairs[kNF4Pairs][32];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kDepth * kStage];
+    static_assert(kKWaves * kRows * kFM * 16 * 4 <= sizeof(lds), "the waves' sums fit");
+
+    const uint32_t l = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t n0 = blockIdx.x * kRows, m0 = blockIdx.z * kXRows;
+    const uint32_t stages = (a.blocks + kKWaves - 1) / kKWaves;
+    const uint32_t s0 = uint32_t(uint64_t(stages) * blockIdx.y / a.splits),
+                   s1 = uint32_t(uint64_t(stages) * (blockIdx.y + 1) / a.splits);
+
+    // The order of a row's chunks in LDS, such that the 16 rows that are read together lie on
+    // different banks.
+    auto code_swizzle = [](uint32_t r) { return kCodeChunks >= 16 ? r & 15u : (r >> 1) & 7u; };
+    auto x_swizzle = [](uint32_t r) { return r & 15u; };
+
+    // This wave's loads of a stage (those left over: the last one again). A lane's row never
+    // changes and its column moves on by `step` bytes a stage, to the row's end.
+    uint64_t base[kPerWave];
+    uint32_t row_at[kPerWave], col[kPerWave], step[kPerWave], end[kPerWave], to[kPerWave];
+    bool words[kPerWave];
+#pragma unroll
+    for (uint32_t j = 0; j < kPerWave; ++j) {
+        const uint32_t i0 = wave + j * kThinWaves, i = i0 < kLoads ? i0 : kLoads - 1;
+        words[j] = false;
+        if (i < kCodeLoads) {
+            const uint32_t g = i * 64 + l, r = g / kCodeChunks, last = a.n - n0 - 1;
+            base[j] = a.codes + uint64_t(n0) * a.blocks * 32;
+            row_at[j] = (r < last ? r : last) * (a.blocks * 32);
+            col[j] = ((g % kCodeChunks) ^ code_swizzle(r)) * 16;
+            step[j] = kCodeChunks * 16;
+            end[j] = a.blocks * 32 - 16;
+            to[j] = i * 1024;
+        } else if (i < kCodeLoads + kXLoads) {
+            const uint32_t g = (i - kCodeLoads) * 64 + l, r = g / kXChunks, last = a.m - m0 - 1;
+            base[j] = a.x + uint64_t(m0) * a.x_row;
+            row_at[j] = (r < last ? r : last) * a.x_row;
+            col[j] = ((g % kXChunks) ^ x_swizzle(r)) * 16;
+            step[j] = kXChunks * 16;
+            end[j] = a.blocks * 64 * kElement - 16;
+            to[j] = kXAt + (i - kCodeLoads) * 1024;
+        } else {
+            const uint32_t g = (i - kCodeLoads - kXLoads) * 64 + l, r = g / kKWaves, last = a.n - n0 - 1;
+            base[j] = a.absmax + uint64_t(n0) * a.blocks * 4;
+            row_at[j] = (r < last ? r : last) * (a.blocks * 4);
+            col[j] = g % kKWaves * 4;
+            step[j] = kKWaves * 4;
+            end[j] = a.blocks * 4 - 4;
+            to[j] = kScaleAt + (i - kCodeLoads - kXLoads) * 256;
+            words[j] = true;
+        }
+    }
+    const uint32_t lds0 = lds_offset(&lds[0]);
+    auto load = [&](uint32_t s, uint32_t buffer) {
+#pragma unroll
+        for (uint32_t j = 0; j < kPerWave; ++j) {
+            const uint32_t at = col[j] + s * step[j], off = row_at[j] + (at < end[j] ? at : end[j]);
+            if (words[j])
+                dma_word_to_lds(base[j], off, lds0 + buffer * kStage + to[j]);
+            else
+                dma_to_lds(base[j], off, lds0 + buffer * kStage + to[j]);
+        }
+    };
+    uint32_t ahead = s0;
+    for (uint32_t d = 0; d + 1 < kDepth && ahead < s1; ++d, ++ahead) load(ahead, (ahead - s0) % kDepth);
+    {
+        const uint32_t byte = threadIdx.x / 2;
+        v2f_t v = {0.0f, 0.0f};
+#pragma unroll
+        for (uint32_t i = 0; i < kNF4Codes; ++i) {
+            v.x = (byte & 15u) == i ? kNF4Values[i] : v.x;
+            v.y = (byte >> 4) == i ? kNF4Values[i] : v.y;
+        }
+        const v4f_t twice = {v.x, v.y, v.x, v.y};
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) *reinterpret_cast<v4f_t*>(&pairs[byte][(threadIdx.x & 1u) * 16 + 2 * i]) = twice;
+    }
+
+    const uint32_t fr = l & 15u, fg = l >> 4;
+    const uint32_t rw = wave / kKWaves, q = wave % kKWaves;
+    const uint32_t mine = (l & 31u) * 8;  // this lane's copy
+    v4f_t acc[kRG][kFM] = {};
+    for (uint32_t s = s0; s < s1; ++s) {
+        // stage s is there (all that is in flight after it: whole stages), and the one before it
+        // is read by all
+        if (ahead - s == kDepth - 1)
+            dma_wait<(kDepth - 2) * kPerWave>();
+        else
+            dma_wait();
+        lds_barrier();
+        const uint32_t buffer = (s - s0) % kDepth;
+        if (ahead < s1) {
+            load(ahead, (ahead - s0) % kDepth);
+            ++ahead;
+        }
+        if (s * kKWaves + q >= a.blocks) continue;  // (of the wave)
+        const uint8_t* t = lds + buffer * kStage;
+        // 16 weights of a row and what they are multiplied by
+        u32x2_t code[kRG];
+        float scale[kRG];
+#pragma unroll
+        for (uint32_t g = 0; g < kRG; ++g) {
+            const uint32_t r = (rw * kRG + g) * 16 + fr;
+            code[g] = *reinterpret_cast<const u32x2_t*>(t + (r * kCodeChunks + ((2 * q + (fg >> 1)) ^ code_swizzle(r))) * 16 +
+                                                        (fg & 1u) * 8);
+            scale[g] = *reinterpret_cast<const float*>(t + kScaleAt + (r * kKWaves + q) * 4);
+        }
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h) {  // 32 of the block's 64 columns: 8 of each lane
+            std::conditional_t<kF, Planes, v8bf_t> x[kFM];
+#pragma unroll
+            for (uint32_t f = 0; f < kFM; ++f) {
+                const uint32_t r = f * 16 + (kXRows < 16 ? fr % kXRows : fr);
+                const uint8_t* row = t + kXAt + r * kXChunks * 16;
+                const uint32_t chunk = (q * 8 + fg * 2 + h) * (kElement / 2);
+                if constexpr (kF) {
+                    const u32x4_t lo = *reinterpret_cast<const u32x4_t*>(row + (chunk ^ x_swizzle(r)) * 16);
+                    const u32x4_t hi = *reinterpret_cast<const u32x4_t*>(row + ((chunk + 1) ^ x_swizzle(r)) * 16);
+                    float v[8];
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        v[i] = __uint_as_float(lo[i]);
+                        v[i + 4] = __uint_as_float(hi[i]);
+                    }
+                    x[f] = planes_of(v);
+                } else {
+                    x[f] = *reinterpret_cast<const v8bf_t*>(row + (chunk ^ x_swizzle(r)) * 16);
+                }
+            }
+#pragma unroll
+            for (uint32_t g = 0; g < kRG; ++g) {
+                float w[8];
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    const uint32_t at = __builtin_amdgcn_perm(code[g][h], mine, 0x0C0C0000u | (4 + i) << 8);
+                    const v2f_t v = *reinterpret_cast<const v2f_t*>(reinterpret_cast<const uint8_t*>(&pairs[0][0]) + at);
+                    w[2 * i] = v.x * scale[g];
+                    w[2 * i + 1] = v.y * scale[g];
+                }
+                if constexpr (kF) {
+                    const Planes p = planes_of(w);
+#pragma unroll
+                    for (uint32_t f = 0; f < kFM; ++f) acc[g][f] = product(p, x[f], acc[g][f]);
+                } else {
+                    v8bf_t b;
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) b[i] = static_cast<__bf16>(w[i]);
+#pragma unroll
+                    for (uint32_t f = 0; f < kFM; ++f)
+                        acc[g][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, x[f], acc[g][f], 0, 0, 0);
+                }
+            }
+        }
+    }
+
+    // the waves' sums, joined in the order of their blocks
+    lds_barrier();  // the last stage is read
+    constexpr uint32_t kTiles = kRowWaves * kRG * kFM;
+    v4f_t* room = reinterpret_cast<v4f_t*>(lds);  // [kKWaves][kTiles][64]
+#pragma unroll
+    for (uint32_t g = 0; g < kRG; ++g)
+#pragma unroll
+        for (uint32_t f = 0; f < kFM; ++f) room[(q * kTiles + (rw * kRG + g) * kFM + f) * 64 + l] = acc[g][f];
+    lds_barrier();
+    NF4MatmulArgs o;
+    o.c = a.c;
+    o.ldc = a.ldc;
+    o.partial = a.partial;
+    o.m = a.m;
+    o.n = a.n;
+    const bool whole = whole_groups<kWideOut>(o);
+    for (uint32_t t = wave; t < kTiles; t += kThinWaves) {
+        v4f_t sum = room[t * 64 + l];
+#pragma unroll
+        for (uint32_t w = 1; w < kKWaves; ++w) sum += room[(w * kTiles + t) * 64 + l];
+        const uint32_t row = m0 + t % kFM * 16 + fr, column = n0 + t / kFM * 16 + fg * 4;
+        if ((kXRows < 16 && fr >= kXRows) || row >= a.m || column >= a.n) continue;
+        if (a.splits == 1)
+            store4<kWideOut>(o, whole, row, column, sum);
+        else
+            *reinterpret_cast<MEZO_GLOBAL v4f_t*>(partial_at(o, blockIdx.y, row, column)) = sum;
+    }
+}
+
 // ---- launches ---------------------------------------------------------------------
 
 template <class Args>
@@ -360,7 +633,11 @@ hipError_t launch_tiled(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t s
             return run(reinterpret_cast<const void*>(f), dim3(uint32_t(tiles_of(a.m, lay.rows, bm, bn)), cut.splits), lanes,
                        g, stream);
         };
-        e = go(nf4_matmul_kernel<64, 64, 2, 2, kWide, kWideOut>, 64, 64, 256);
+        switch (cut.tile) {
+        case k256x256: e = go(nf4_matmul_kernel<256, 256, 2, 4, kWide, kWideOut>, 256, 256, 512); break;
+        case k128x128: e = go(nf4_matmul_kernel<128, 128, 2, 2, kWide, kWideOut>, 128, 128, 256); break;
+        default: e = go(nf4_matmul_kernel<64, 64, 2, 2, kWide, kWideOut>, 64, 64, 256);
+        }
         if (e != hipSuccess) return e;
         if (cut.splits > 1) {
             const uint64_t groups = a.m * ((lay.rows + 3) / 4);
@@ -373,9 +650,75 @@ hipError_t launch_tiled(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t s
 }
 
 template <bool kWide, bool kWideOut>
+hipError_t launch_thin(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t stream)
+{
+    constexpr uint64_t kElement = kWide ? 4 : 2;
+    const NF4Space space = nf4_space(a.m, a.n, a.k, kWide);
+    NF4ThinArgs g = {};
+    g.x = a.x;
+    g.x_row = uint32_t(a.ldx * kElement);
+    if (((a.x | (a.ldx * kElement)) & 15u) || a.ldx * kElement > (1u << 24)) {  // the loads want whole 16 bytes
+        LayArgs lay = {};
+        lay.from = a.x;
+        lay.ld = a.ldx;
+        lay.to = a.workspace;
+        lay.rows = a.m;
+        lay.k = lay.columns = a.k;
+        const hipError_t e = run(reinterpret_cast<const void*>(nf4_copy_rows_kernel<kWide>),
+                                 dim3(uint32_t((a.m * (a.k / 8) + 255) / 256)), 256, lay, stream);
+        if (e != hipSuccess) return e;
+        g.x = a.workspace;
+        g.x_row = uint32_t(a.k * kElement);
+    }
+    g.codes = a.codes;
+    g.absmax = a.absmax;
+    g.c = a.c;
+    g.ldc = a.ldc;
+    g.partial = a.workspace + space.partial;
+    g.m = uint32_t(a.m);
+    g.n = uint32_t(a.n);
+    g.blocks = uint32_t(a.k / kNF4Block);
+    g.splits = cut.splits;
+    auto go = [&](auto* f, uint64_t rows, uint64_t x_rows) {
+        return run(reinterpret_cast<const void*>(f),
+                   dim3(uint32_t((a.n + rows - 1) / rows), cut.splits, uint32_t((a.m + x_rows - 1) / x_rows)),
+                   kThinWaves * 64, g, stream);
+    };
+    hipError_t e;
+    if (cut.thin_rows == 16) {
+        if (a.m <= 4)
+            e = go(nf4_thin_kernel<kWide, 1, 1, 4, 4, kWideOut>, 16, 4);
+        else
+            e = go(nf4_thin_kernel<kWide, 1, 1, 16, kWide ? 2 : 4, kWideOut>, 16, 16);
+    } else {
+        if (a.m <= 4)
+            e = go(nf4_thin_kernel<kWide, 2, 2, 4, 4, kWideOut>, 64, 4);
+        else if (a.m <= 16 || kWide)
+            e = go(nf4_thin_kernel<kWide, 2, 2, 16, kWide ? 3 : 4, kWideOut>, 64, 16);
+        else if constexpr (!kWide) {
+            if (a.m <= 32)
+                e = go(nf4_thin_kernel<false, 2, 2, 32, 3, kWideOut>, 64, 32);
+            else
+                e = go(nf4_thin_kernel<false, 2, 2, 64, 2, kWideOut>, 64, 64);
+        }
+    }
+    if (e != hipSuccess || cut.splits == 1) return e;
+    NF4MatmulArgs j = {};
+    j.c = a.c;
+    j.ldc = a.ldc;
+    j.partial = g.partial;
+    j.m = g.m;
+    j.n = g.n;
+    j.splits = cut.splits;
+    const uint64_t groups = a.m * ((a.n + 3) / 4);
+    return run(reinterpret_cast<const void*>(nf4_join_kernel<kWideOut>), dim3(uint32_t((groups + 255) / 256)), 256, j, stream);
+}
+
+template <bool kWide, bool kWideOut>
 hipError_t launch_any(const NF4LinearArgs& a, hipStream_t stream)
 {
-    return launch_tiled<kWide, kWideOut>(a, cut_nf4(a.m, a.n, a.k, kWide), stream);
+    const NF4Cut cut = cut_nf4(a.m, a.n, a.k, kWide);
+    return cut.tile == kThin ? launch_thin<kWide, kWideOut>(a, cut, stream) : launch_tiled<kWide, kWideOut>(a, cut, stream);
 }
 
 hipError_t launch_nf4_linear(const NF4LinearArgs& a, hipStream_t stream)

@@ -19,21 +19,37 @@ constexpr uint64_t nf4_planes(bool wide_x) { return wide_x ? 3 : 1; }
 // A product's cut: its tile, the workgroups that share out k, and the weights' rows that are
 // expanded at a time.
 struct NF4Cut {
-    F8Tile tile;
+    F8Tile tile;  // kThin: weights read as they are, thin_rows rows of them a workgroup
     uint32_t splits;
     uint64_t slab;
+    uint32_t thin_rows;
 };
 
 // Bytes of expanded weights at a time: what the last-level cache holds.
 constexpr uint64_t kNF4SlabBytes = 1ull << 28;
 
-inline NF4Cut cut_nf4([[maybe_unused]] uint64_t m, uint64_t n, uint64_t k, bool wide_x)
+inline NF4Cut cut_nf4(uint64_t m, uint64_t n, uint64_t k, bool wide_x)
 {
     const uint64_t row = nf4_columns(k) * 2 * nf4_planes(wide_x);
     uint64_t slab = kNF4SlabBytes / row / 256 * 256;
     if (slab < 256) slab = 256;
     if (slab > n) slab = n;
-    return {k64x64, 1, slab};
+    if (m <= 64 && k % 64 == 0) {
+        const uint64_t rows = m <= 16 && n <= 4096 ? 16 : 64, stages = (k / 64 + (rows == 16 ? 7 : 3)) / (rows == 16 ? 8 : 4);
+        const uint64_t groups = (n + rows - 1) / rows * (wide_x ? (m + 15) / 16 : 1);
+        const uint64_t want = groups >= 160 ? 1 : 256 / groups, most = stages / 4;
+        const uint64_t splits = want < most ? want : most;
+        return {kThin, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits)), 0, uint32_t(rows)};
+    }
+    // as the 8-bit product is cut
+    const uint64_t t128 = tiles_of(m, slab, 128, 128);
+    const uint64_t rounds128 = (t128 + 511) / 512, rounds256 = (tiles_of(m, slab, 256, 256) + 255) / 256;
+    if (9 * rounds256 <= 5 * rounds128) return {k256x256, 1, slab, 0};
+    if (t128 >= 200) return {k128x128, 1, slab, 0};
+    const uint64_t stages = nf4_columns(k) / 64 * (wide_x ? 6 : 1);
+    const uint64_t want = 512 / tiles_of(m, slab, 64, 64), most = stages / 16;
+    const uint64_t splits = want < most ? want : most;
+    return {k64x64, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits)), slab, 0};
 }
 
 // The parts of a call's workspace, from its start: activations laid out, weights expanded,
@@ -47,9 +63,10 @@ inline NF4Space nf4_space(uint64_t m, uint64_t n, uint64_t k, bool wide_x)
     const NF4Cut c = cut_nf4(m, n, k, wide_x);
     const uint64_t row = nf4_columns(k) * 2 * nf4_planes(wide_x);
     NF4Space s;
-    s.weights = m * row;
+    // (few rows are laid out in their own type where they do not lie on 16 bytes)
+    s.weights = c.tile == kThin ? m * k * (wide_x ? 4 : 2) : m * row;
     s.partial = s.weights + c.slab * row;
-    s.bytes = s.partial + (c.splits > 1 ? c.splits * m * ((c.slab + 3) / 4 * 16) : 0);
+    s.bytes = s.partial + (c.splits > 1 ? c.splits * m * (((c.tile == kThin ? n : c.slab) + 3) / 4 * 16) : 0);
     return s;
 }
 
