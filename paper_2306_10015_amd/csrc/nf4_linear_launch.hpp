@@ -35,7 +35,7 @@ inline NF4Cut cut_nf4(uint64_t m, uint64_t n, uint64_t k, bool wide_x)
     if (slab < 256) slab = 256;
     if (slab > n) slab = n;
     if (m <= 64 && k % 64 == 0) {
-        const uint64_t rows = m <= 16 && n <= 4096 ? 16 : 64, stages = (k / 64 + (rows == 16 ? 7 : 3)) / (rows == 16 ? 8 : 4);
+        const uint64_t rows = m <= 4 && n <= 4096 ? 16 : 64, stages = (k / 64 + (rows == 16 ? 15 : 3)) / (rows == 16 ? 16 : 4);
         const uint64_t groups = (n + rows - 1) / rows * (wide_x ? (m + 15) / 16 : 1);
         const uint64_t want = groups >= 160 ? 1 : 256 / groups, most = stages / 4;
         const uint64_t splits = want < most ? want : most;
