@@ -325,11 +325,18 @@ __global__ void __launch_bounds__(256) nf4_join_kernel(NF4MatmulArgs a)
 // Then a multiplication by the block's scale each and one conversion: 2 vector instructions a
 // weight in bf16 (selecting by v_perm_b32 out of registers takes 4).
 //
-// A workgroup takes kRowWaves * 16 of the weights' rows and a share of k; its waves are
-// kRowWaves x kKWaves: a stage is kSpan blocks of 64 for each of the kKWaves, of all the rows,
-// with their scales and the activations beside them, loaded straight into LDS kDepth - 1
-// stages ahead. The order of k within a block does not matter as long as both operands agree:
-// a lane takes 16 weights next to each other. The waves' sums join in LDS, in their order.
+// A workgroup takes kRowWaves * kRG * 16 of the weights' rows and a share of k; its waves are
+// kRowWaves x kKWaves: a stage is a block of 64 for each of the kKWaves, of all the rows, with
+// their scales and the activations beside them, loaded straight into LDS kDepth - 1 stages
+// ahead. The order of k within a block does not matter as long as both operands agree: a lane
+// takes 16 weights next to each other. The waves' sums join in LDS, in their order.
+//
+// What bounds it is LDS: 8 bytes a lookup of two weights, and the activations, which each
+// group of kRG * 16 rows reads again (1 x 16384 x 4096: 13.2 us in groups of 16, 12.6 in 32;
+// the loads alone take 9.7, the rest alone 12.1). With 16 copies of the table instead of 32
+// lookups meet, and the room is another stage's: 32 activations 16.8 -> 16.1 us, one 12.6 ->
+// 14.2. Issuing a stage's lookups under the products of the one before, 8 waves instead of 16,
+// and two workgroups a CU with half a table each lost.
 struct NF4ThinArgs {
     uint64_t x, codes, absmax, c, ldc, partial;
     uint32_t m, n, blocks;  // blocks of 64 of a row
@@ -377,30 +384,30 @@ __device__ __forceinline__ v4f_t product(const Planes& w, const Planes& x, v4f_t
 
 constexpr uint32_t kThinWaves = 16;
 
-template <bool kF, uint32_t kRowWaves, uint32_t kSpan, uint32_t kXRows, uint32_t kDepth, bool kWideOut>
+template <bool kF, uint32_t kRowWaves, uint32_t kRG, uint32_t kXRows, uint32_t kDepth, uint32_t kCopies, bool kWideOut>
 __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a)
 {
-    constexpr uint32_t kKWaves = kThinWaves / kRowWaves, kBlocks = kKWaves * kSpan, kRows = kRowWaves * 16;
+    constexpr uint32_t kKWaves = kThinWaves / kRowWaves, kRows = kRowWaves * kRG * 16;
     constexpr uint32_t kFM = kXRows < 16 ? 1 : kXRows / 16;
     constexpr uint32_t kElement = kF ? 4 : 2;
     // a stage in LDS: codes [kRows][kCodeChunks], activations [kXRows][kXChunks] of 16 bytes,
-    // scales [kRows][kBlocks] of 4
-    constexpr uint32_t kCodeChunks = kBlocks * 2, kXChunks = kBlocks * 4 * kElement;
+    // scales [kRows][kKWaves] of 4
+    constexpr uint32_t kCodeChunks = kKWaves * 2, kXChunks = kKWaves * 4 * kElement;
     constexpr uint32_t kCodeLoads = kRows * kCodeChunks / 64, kXLoads = kXRows * kXChunks / 64,
-                       kScaleLoads = kRows * kBlocks / 64;
+                       kScaleLoads = kRows * kKWaves / 64;
     constexpr uint32_t kXAt = kCodeLoads * 1024, kScaleAt = kXAt + kXLoads * 1024,
                        kStage = kScaleAt + kScaleLoads * 256;
-    static_assert(kRows * kCodeChunks % 64 == 0 && kXRows * kXChunks % 64 == 0 && kRows * kBlocks % 64 == 0);
+    static_assert(kRows * kCodeChunks % 64 == 0 && kXRows * kXChunks % 64 == 0 && kRows * kKWaves % 64 == 0);
     constexpr uint32_t kLoads = kCodeLoads + kXLoads + kScaleLoads, kPerWave = (kLoads + kThinWaves - 1) / kThinWaves;
     // (one object, the table first: its addresses then need no base)
-    constexpr uint32_t kTable = kNF4Pairs * 32 * sizeof(v2f_t);
+    constexpr uint32_t kTable = kNF4Pairs * kCopies * sizeof(v2f_t);
     __shared__ __attribute__((aligned(1024))) uint8_t memory[kTable + kDepth * kStage];
     uint8_t* const lds = memory + kTable;
-    static_assert(kKWaves * kRows * kFM * 16 * 4 <= kDepth * kStage, "the waves' sums fit");
+    static_assert(kKWaves * kRows * kFM * 16 * 4 <= sizeof(memory), "the waves' sums fit");
 
     const uint32_t l = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t n0 = blockIdx.x * kRows, m0 = blockIdx.z * kXRows;
-    const uint32_t stages = (a.blocks + kBlocks - 1) / kBlocks;
+    const uint32_t stages = (a.blocks + kKWaves - 1) / kKWaves;
     const uint32_t s0 = uint32_t(uint64_t(stages) * blockIdx.y / a.splits),
                    s1 = uint32_t(uint64_t(stages) * (blockIdx.y + 1) / a.splits);
 
@@ -435,11 +442,11 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
             end[j] = a.blocks * 64 * kElement - 16;
             to[j] = kXAt + (i - kCodeLoads) * 1024;
         } else {
-            const uint32_t g = (i - kCodeLoads - kXLoads) * 64 + l, r = g / kBlocks, last = a.n - n0 - 1;
+            const uint32_t g = (i - kCodeLoads - kXLoads) * 64 + l, r = g / kKWaves, last = a.n - n0 - 1;
             base[j] = a.absmax + uint64_t(n0) * a.blocks * 4;
             row_at[j] = (r < last ? r : last) * (a.blocks * 4);
-            col[j] = g % kBlocks * 4;
-            step[j] = kBlocks * 4;
+            col[j] = g % kKWaves * 4;
+            step[j] = kKWaves * 4;
             end[j] = a.blocks * 4 - 4;
             to[j] = kScaleAt + (i - kCodeLoads - kXLoads) * 256;
             words[j] = true;
@@ -459,7 +466,9 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
     uint32_t ahead = s0;
     for (uint32_t d = 0; d + 1 < kDepth && ahead < s1; ++d, ++ahead) load(ahead, (ahead - s0) % kDepth);
     {
-        const uint32_t byte = threadIdx.x / 4;
+        // (a lane writes its part of a byte's copies)
+        constexpr uint32_t kEach = kThinWaves * 64 / kNF4Pairs;
+        const uint32_t byte = threadIdx.x / kEach;
         v2f_t v = {0.0f, 0.0f};
 #pragma unroll
         for (uint32_t i = 0; i < kNF4Codes; ++i) {
@@ -468,25 +477,26 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
         }
         const v4f_t twice = {v.x, v.y, v.x, v.y};
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) *reinterpret_cast<v4f_t*>(memory + byte * 256 + (threadIdx.x & 3u) * 64 + i * 16) = twice;
+        for (uint32_t i = 0; i < kCopies / 2 / kEach; ++i)
+            *reinterpret_cast<v4f_t*>(memory + (byte * (kCopies / 2) + i * kEach + threadIdx.x % kEach) * 16) = twice;
     }
 
     const uint32_t fr = l & 15u, fg = l >> 4;
     const uint32_t rw = wave / kKWaves, q = wave % kKWaves;
-    const uint32_t mine = (l & 31u) * 8;  // this lane's copy
-    // where this lane reads in a stage
-    const uint32_t r = rw * 16 + fr, xr = kXRows < 16 ? fr % kXRows : fr;
-    uint32_t code_at[kSpan], scale_at[kSpan], x_at[kSpan][2];
+    const uint32_t mine = (l % kCopies) * 8;  // this lane's copy
+    // where this lane reads in a stage: of each of its groups of 16 rows, and of the activations
+    const uint32_t xr = kXRows < 16 ? fr % kXRows : fr;
+    uint32_t code_at[kRG], scale_at[kRG], x_at[2];
 #pragma unroll
-    for (uint32_t u = 0; u < kSpan; ++u) {
-        const uint32_t b = u * kKWaves + q;  // of the stage's blocks
-        code_at[u] = (r * kCodeChunks + ((2 * b + (fg >> 1)) ^ code_swizzle(r))) * 16 + (fg & 1u) * 8;
-        scale_at[u] = kScaleAt + (r * kBlocks + b) * 4;
-#pragma unroll
-        for (uint32_t h = 0; h < 2; ++h)
-            x_at[u][h] = kXAt + (xr * kXChunks + (((b * 8 + fg * 2 + h) * (kElement / 2)) ^ x_swizzle(xr))) * 16;
+    for (uint32_t g = 0; g < kRG; ++g) {
+        const uint32_t r = (rw * kRG + g) * 16 + fr;
+        code_at[g] = (r * kCodeChunks + ((2 * q + (fg >> 1)) ^ code_swizzle(r))) * 16 + (fg & 1u) * 8;
+        scale_at[g] = kScaleAt + (r * kKWaves + q) * 4;
     }
-    v4f_t acc[kFM] = {};
+#pragma unroll
+    for (uint32_t h = 0; h < 2; ++h)
+        x_at[h] = kXAt + (xr * kXChunks + (((q * 8 + fg * 2 + h) * (kElement / 2)) ^ x_swizzle(xr))) * 16;
+    v4f_t acc[kRG][kFM] = {};
     for (uint32_t s = s0; s < s1; ++s) {
         // stage s is there (all that is in flight after it: whole stages), and the one before it
         // is read by all
@@ -495,42 +505,59 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
         else
             dma_wait();
         lds_barrier();
-        const uint32_t buffer = (s - s0) % kDepth;
         if (ahead < s1) {
             load(ahead, (ahead - s0) % kDepth);
             ++ahead;
         }
-        const uint8_t* t = lds + buffer * kStage;
-        // 16 weights of a row for each of the wave's blocks, all lookups under way before the
-        // first is used
-        u32x2_t code[kSpan];
-        float scale[kSpan];
-        v2f_t w[kSpan][2][4];
+        if (s * kKWaves + q >= a.blocks) continue;  // (of the wave)
+        const uint8_t* t = lds + (s - s0) % kDepth * kStage;
+        // 16 weights of a row for each group, all lookups under way before the first is used
+        u32x2_t code[kRG];
+        float scale[kRG];
+        v2f_t w[kRG][2][4];
 #pragma unroll
-        for (uint32_t u = 0; u < kSpan; ++u) {
-            code[u] = *reinterpret_cast<const u32x2_t*>(t + code_at[u]);
-            scale[u] = *reinterpret_cast<const float*>(t + scale_at[u]);
+        for (uint32_t g = 0; g < kRG; ++g) {
+            code[g] = *reinterpret_cast<const u32x2_t*>(t + code_at[g]);
+            scale[g] = *reinterpret_cast<const float*>(t + scale_at[g]);
         }
 #pragma unroll
-        for (uint32_t u = 0; u < kSpan; ++u)
+        for (uint32_t g = 0; g < kRG; ++g)
 #pragma unroll
             for (uint32_t h = 0; h < 2; ++h)
 #pragma unroll
                 for (uint32_t i = 0; i < 4; ++i) {
-                    const uint32_t at = __builtin_amdgcn_perm(code[u][h], mine, 0x0C0C0000u | (4 + i) << 8);
-                    w[u][h][i] = *reinterpret_cast<const v2f_t*>(memory + at);
+                    const uint32_t at = kCopies == 32 ? __builtin_amdgcn_perm(code[g][h], mine, 0x0C0C0000u | (4 + i) << 8)
+                                                      : (code[g][h] >> (8 * i) & 255u) * (kCopies * 8) | mine;
+                    w[g][h][i] = *reinterpret_cast<const v2f_t*>(memory + at);
                 }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (uint32_t u = 0; u < kSpan; ++u) {
-            if (s * kBlocks + u * kKWaves + q >= a.blocks) continue;  // (of the wave)
+        for (uint32_t h = 0; h < 2; ++h) {  // 32 of the block's 64 columns: 8 of each lane
+            std::conditional_t<kF, Planes, v8bf_t> x[kFM];
 #pragma unroll
-            for (uint32_t h = 0; h < 2; ++h) {  // 32 of the block's 64 columns: 8 of each lane
+            for (uint32_t f = 0; f < kFM; ++f) {
+                const uint8_t* at = t + x_at[h] + f * 16 * kXChunks * 16;
+                if constexpr (kF) {
+                    const u32x4_t lo = *reinterpret_cast<const u32x4_t*>(at);
+                    const u32x4_t hi = *reinterpret_cast<const u32x4_t*>(t + (x_at[h] ^ 16u) + f * 16 * kXChunks * 16);
+                    float v[8];
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        v[i] = __uint_as_float(lo[i]);
+                        v[i + 4] = __uint_as_float(hi[i]);
+                    }
+                    x[f] = planes_of(v);
+                } else {
+                    x[f] = *reinterpret_cast<const v8bf_t*>(at);
+                }
+            }
+#pragma unroll
+            for (uint32_t g = 0; g < kRG; ++g) {
                 float v[8];
 #pragma unroll
                 for (uint32_t i = 0; i < 4; ++i) {
-                    v[2 * i] = w[u][h][i].x * scale[u];
-                    v[2 * i + 1] = w[u][h][i].y * scale[u];
+                    v[2 * i] = w[g][h][i].x * scale[g];
+                    v[2 * i + 1] = w[g][h][i].y * scale[g];
                 }
                 std::conditional_t<kF, Planes, v8bf_t> wide;
                 if constexpr (kF) {
@@ -541,21 +568,10 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
                 }
 #pragma unroll
                 for (uint32_t f = 0; f < kFM; ++f) {
-                    const uint8_t* at = t + x_at[u][h] + f * 16 * kXChunks * 16;
-                    if constexpr (kF) {
-                        const u32x4_t lo = *reinterpret_cast<const u32x4_t*>(at);
-                        const u32x4_t hi = *reinterpret_cast<const u32x4_t*>(t + (x_at[u][h] ^ 16u) + f * 16 * kXChunks * 16);
-                        float x[8];
-#pragma unroll
-                        for (uint32_t i = 0; i < 4; ++i) {
-                            x[i] = __uint_as_float(lo[i]);
-                            x[i + 4] = __uint_as_float(hi[i]);
-                        }
-                        acc[f] = product(wide, planes_of(x), acc[f]);
-                    } else {
-                        const v8bf_t x = *reinterpret_cast<const v8bf_t*>(at);
-                        acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide, x, acc[f], 0, 0, 0);
-                    }
+                    if constexpr (kF)
+                        acc[g][f] = product(wide, x[f], acc[g][f]);
+                    else
+                        acc[g][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide, x[f], acc[g][f], 0, 0, 0);
                 }
             }
         }
@@ -563,10 +579,12 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
 
     // the waves' sums, joined in the order of their blocks
     lds_barrier();  // the last stage is read
-    constexpr uint32_t kTiles = kRowWaves * kFM;
-    v4f_t* room = reinterpret_cast<v4f_t*>(lds);  // [kKWaves][kTiles][64]
+    constexpr uint32_t kTiles = kRowWaves * kRG * kFM;
+    v4f_t* room = reinterpret_cast<v4f_t*>(memory);  // [kKWaves][kTiles][64]
 #pragma unroll
-    for (uint32_t f = 0; f < kFM; ++f) room[(q * kTiles + rw * kFM + f) * 64 + l] = acc[f];
+    for (uint32_t g = 0; g < kRG; ++g)
+#pragma unroll
+        for (uint32_t f = 0; f < kFM; ++f) room[(q * kTiles + (rw * kRG + g) * kFM + f) * 64 + l] = acc[g][f];
     lds_barrier();
     NF4MatmulArgs o;
     o.c = a.c;
@@ -698,17 +716,27 @@ hipError_t launch_thin(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t st
                    kThinWaves * 64, g, stream);
     };
     hipError_t e = hipErrorInvalidValue;
-    if (cut.thin_rows == 16) {
-        e = go(nf4_thin_kernel<kWide, 1, 1, 4, kWide ? 3 : 4, kWideOut>, 16, 4);
-    } else if (a.m <= 4) {
-        e = go(nf4_thin_kernel<kWide, 4, kWide ? 1 : 2, 4, 3, kWideOut>, 64, 4);
-    } else if (a.m <= 16 || kWide) {
-        e = go(nf4_thin_kernel<kWide, 4, 1, 16, kWide ? 3 : 4, kWideOut>, 64, 16);
-    } else if constexpr (!kWide) {
-        if (a.m <= 32)
-            e = go(nf4_thin_kernel<false, 4, 1, 32, 3, kWideOut>, 64, 32);
-        else
-            e = go(nf4_thin_kernel<false, 4, 1, 64, 2, kWideOut>, 64, 64);
+    switch (cut.thin_rows) {
+    case 16: e = go(nf4_thin_kernel<kWide, 1, 1, 4, kWide ? 3 : 4, 32, kWideOut>, 16, 4); break;
+    case 128:
+        if constexpr (!kWide) {
+            if (a.m <= 4)
+                e = go(nf4_thin_kernel<false, 2, 4, 4, 2, 32, kWideOut>, 128, 4);
+            else
+                e = go(nf4_thin_kernel<false, 4, 2, 32, 2, 32, kWideOut>, 128, 32);
+        }
+        break;
+    default:
+        if (a.m <= 4)
+            e = go(nf4_thin_kernel<kWide, 2, 2, 4, 3, kWide ? 16 : 32, kWideOut>, 64, 4);
+        else if (a.m <= 16 || kWide)
+            e = go(nf4_thin_kernel<kWide, 4, 1, 16, kWide ? 3 : 4, 32, kWideOut>, 64, 16);
+        else if constexpr (!kWide) {
+            if (a.m <= 32)
+                e = go(nf4_thin_kernel<false, 2, 2, 32, 2, 16, kWideOut>, 64, 32);
+            else
+                e = go(nf4_thin_kernel<false, 4, 1, 64, 2, 32, kWideOut>, 64, 64);
+        }
     }
     if (e != hipSuccess || cut.splits == 1) return e;
     NF4MatmulArgs j = {};

@@ -109,7 +109,8 @@ def test_rows_apart(mz, pad, m, dtype):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("m,n,k", [(1, 768, 768), (1, 2048, 8192), (24, 768, 4096), (64, 50, 16384), (300, 1000, 1024),
-                                   (700, 520, 640), (513, 2100, 512), (2000, 777, 448)])
+                                   (700, 520, 640), (513, 2100, 512), (2000, 777, 448), (1, 50001, 192), (4, 50001, 64),
+                                   (30, 50001, 128)])
 def test_larger_products(mz, m, n, k, dtype):
     check(mz, m, n, k, dtype, dtype)
 
