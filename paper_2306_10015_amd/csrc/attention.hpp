@@ -170,12 +170,16 @@ __device__ __forceinline__ uint32_t row_bits(const PagedArgs& a, const Document&
     return bits & (left <= 0 ? 0u : (left >= 32 ? ~0u : (1u << left) - 1u));
 }
 
-// The page that holds key j (the same for all lanes); entries outside the cache: its last page.
+// The entry of the page that holds key j (the same for all lanes), and its page: of entries
+// outside the cache its last one.
 typedef __attribute__((address_space(4))) const uint32_t list_t;
-__device__ __forceinline__ uint32_t page_of(const PagedArgs& a, const Document& d, uint32_t j)
+__device__ __forceinline__ uint32_t entry_of(const PagedArgs& a, const Document& d, uint32_t j)
 {
-    const uint32_t e = reinterpret_cast<list_t*>(a.pages)[d.k_first + (j >> a.page_shift)];
-    return e < a.n_pages ? e : a.n_pages - 1;
+    return reinterpret_cast<list_t*>(a.pages)[d.k_first + (j >> a.page_shift)];
+}
+__device__ __forceinline__ uint32_t page_of(const PagedArgs& a, uint32_t entry)
+{
+    return entry < a.n_pages ? entry : a.n_pages - 1;
 }
 
 // Where key j of head kvh lies in the arrays of keys and of values.
@@ -650,6 +654,12 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys, !k
         const uint64_t at = a.q + (d.q_first + uint64_t(i)) * a.q_token + h * a.q_head;
 #pragma unroll
         for (uint32_t c = 0; c < T::kQ; ++c) q[c] = T::query(at, c, a.dim, l);
+        // (They are there before the loop: the compiler waits for a load where its result is first
+        // used, which would be in the loop, in every round, and for the stages in flight too.)
+        if constexpr (!kF) {
+#pragma unroll
+            for (uint32_t c = 0; c < T::kQ; ++c) asm volatile("" : "+v"(q[c]));
+        }
     }
     const uint64_t kbase = kPaged ? a.k + kvh * a.k_head : a.k + d.k_first * a.k_token + kvh * a.k_head;
     const uint64_t vbase = kPaged ? a.v + kvh * a.v_head : a.v + d.k_first * a.v_token + kvh * a.v_head;
@@ -671,6 +681,17 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys, !k
         koff[n] = r * uint32_t(a.k_token) + column(false, n * T::kLoadRows + r);
         voff[n] = r * uint32_t(a.v_token) + column(true, n * T::kLoadRows + r);
     }
+    // (paged) the entries of a stage's loads, read a stage ahead: they wait for nothing then
+    [[maybe_unused]] uint32_t entry[kLoads];
+    auto fetch = [&](uint32_t s) {
+        if constexpr (kPaged) {
+#pragma unroll
+            for (uint32_t n = 0; n < kLoads; ++n) {
+                const uint32_t j = s * kStage + ((kKeys ? 0 : wave * kLoads) + n) * T::kLoadRows;
+                entry[n] = entry_of(a, d, j < uint32_t(d.nk) ? j : uint32_t(d.nk) - 1);
+            }
+        }
+    };
     auto load = [&](auto isv, uint32_t s, uint32_t b) {
         constexpr bool kV = decltype(isv)::value;
         const uint64_t token = kV ? a.v_token : a.k_token;
@@ -681,12 +702,9 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys, !k
             const uint64_t page_bytes = kV ? a.v_page : a.k_page;
             if ((s + 1) * kStage <= uint32_t(d.nk)) {
                 const uint32_t j0 = s * kStage + at0 * T::kLoadRows;
-                uint32_t page[kLoads];  // (all of them under way before the first is used)
-#pragma unroll
-                for (uint32_t n = 0; n < kLoads; ++n) page[n] = page_of(a, d, j0 + n * T::kLoadRows);
 #pragma unroll
                 for (uint32_t n = 0; n < kLoads; ++n)
-                    dma_to_lds((kV ? vbase : kbase) + page[n] * page_bytes + ((j0 + n * T::kLoadRows) & in_page) * token,
+                    dma_to_lds((kV ? vbase : kbase) + page_of(a, entry[n]) * page_bytes + ((j0 + n * T::kLoadRows) & in_page) * token,
                                (kV ? voff : koff)[n % kPatterns], to + (at0 + n) * 1024);
             } else {
                 // rows past the last one: the last one again
@@ -696,7 +714,7 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys, !k
                     const uint32_t r = (at0 + n) * T::kLoadRows, key = s * kStage + r, from = l / T::kChunks;
                     const uint32_t j = key < last_key ? key : last_key / T::kLoadRows * T::kLoadRows;
                     const uint32_t mine = key + from < last_key ? key + from : last_key;
-                    dma_to_lds((kV ? vbase : kbase) + page_of(a, d, j) * page_bytes + (j & in_page) * token,
+                    dma_to_lds((kV ? vbase : kbase) + page_of(a, entry_of(a, d, j)) * page_bytes + (j & in_page) * token,
                                (mine - j) * uint32_t(token) + column(kV, r + from), to + (at0 + n) * 1024);
                 }
             }
@@ -738,8 +756,10 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys, !k
 
     const uint32_t step = kKeys ? kWaves : 1, begin = s0 + (kKeys ? wave : 0);
     if (begin < s1) {
+        fetch(begin);
         load(kOfK, begin, 0);
         load(kOfV, begin, 0);
+        fetch(begin + step);
     }
     uint32_t b = 0;
     for (uint32_t s = begin; s < s1; s += step, b ^= kBuffers - 1) {
@@ -752,6 +772,7 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys, !k
             if (more) {
                 load(kOfK, s + step, b ^ 1);
                 load(kOfV, s + step, b ^ 1);
+                fetch(s + 2 * step);
             }
         }
         const int k0 = int(s * kStage);
@@ -901,7 +922,10 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys, !k
                 T::values(vt, t * 32, x[t], acc, l);
                 if constexpr (kKeys) {
                     lds_wait();
-                    if (more) load(kOfV, s + step, 0);
+                    if (more) {
+                        load(kOfV, s + step, 0);
+                        fetch(s + 2 * step);
+                    }
                 }
             }
         }
