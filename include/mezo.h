@@ -541,7 +541,8 @@ MEZO_API int mezo_cache_append(const mezo_append_t* a, void* stream);
  * v_token the elements from one row of a page to the next, k_page and v_page
  * those from one page to the next; a->k_tokens is not read, and max_k counts as
  * at most n_entries * rows. A document's keys are cut to the list; entries outside
- * the cache are read as its last page.
+ * the cache are read as its last page. k_page, v_page, rows * k_token and rows * v_token
+ * are less than 4 GiB (MEZO_EINVAL).
  *
  * With `tree`, a document's queries are tokens drafted in a tree: query i sees
  * the nk - nq keys before them, keys j < prefix, and key nk - nq + t (the

@@ -681,15 +681,28 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys, !k
         koff[n] = r * uint32_t(a.k_token) + column(false, n * T::kLoadRows + r);
         voff[n] = r * uint32_t(a.v_token) + column(true, n * T::kLoadRows + r);
     }
-    // (paged) the entries of a stage's loads, read a stage ahead: they wait for nothing then
-    [[maybe_unused]] uint32_t entry[kLoads];
+    // (paged) The wave's rows of a stage lie in groups of 16, or of 8 where pages are of 8 rows:
+    // a group is within a page, so its address is computed once. The groups' entries are read
+    // a stage ahead: nothing waits for them.
+    constexpr uint32_t kSpan = kLoads * T::kLoadRows, kWide = kSpan < 16 ? kSpan : 16;
+    [[maybe_unused]] uint32_t entry[kSpan / 8];
+    [[maybe_unused]] const uint32_t row0 = (kKeys ? 0 : wave) * kSpan;
+    [[maybe_unused]] bool wide = false;
+    if constexpr (kPaged) wide = a.page_shift >= 4;
     auto fetch = [&](uint32_t s) {
         if constexpr (kPaged) {
+            auto each = [&](auto rows) {
+                constexpr uint32_t kRows = decltype(rows)::value;
 #pragma unroll
-            for (uint32_t n = 0; n < kLoads; ++n) {
-                const uint32_t j = s * kStage + ((kKeys ? 0 : wave * kLoads) + n) * T::kLoadRows;
-                entry[n] = entry_of(a, d, j < uint32_t(d.nk) ? j : uint32_t(d.nk) - 1);
-            }
+                for (uint32_t g = 0; g < kSpan / kRows; ++g) {
+                    const uint32_t j = s * kStage + row0 + g * kRows;
+                    entry[g] = entry_of(a, d, j < uint32_t(d.nk) ? j : uint32_t(d.nk) - 1);
+                }
+            };
+            if (wide)
+                each(std::integral_constant<uint32_t, kWide>{});
+            else
+                each(std::integral_constant<uint32_t, 8>{});
         }
     };
     auto load = [&](auto isv, uint32_t s, uint32_t b) {
@@ -699,13 +712,25 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys, !k
         const uint32_t to = lds0 + (2 * b + (kV ? 1 : 0)) * kBytes, at0 = kKeys ? 0 : wave * kLoads;
         if constexpr (kPaged) {
             const uint32_t in_page = (1u << a.page_shift) - 1;
-            const uint64_t page_bytes = kV ? a.v_page : a.k_page;
+            const uint32_t page_bytes = kV ? a.v_page : a.k_page, row_bytes = uint32_t(token);
             if ((s + 1) * kStage <= uint32_t(d.nk)) {
-                const uint32_t j0 = s * kStage + at0 * T::kLoadRows;
+                auto each = [&](auto rows) {
+                    constexpr uint32_t kRows = decltype(rows)::value, kPer = kRows / T::kLoadRows;
 #pragma unroll
-                for (uint32_t n = 0; n < kLoads; ++n)
-                    dma_to_lds((kV ? vbase : kbase) + page_of(a, entry[n]) * page_bytes + ((j0 + n * T::kLoadRows) & in_page) * token,
-                               (kV ? voff : koff)[n % kPatterns], to + (at0 + n) * 1024);
+                    for (uint32_t g = 0; g < kSpan / kRows; ++g) {
+                        uint64_t at = (kV ? vbase : kbase) + uint64_t(page_of(a, entry[g])) * page_bytes +
+                                      ((s * kStage + row0 + g * kRows) & in_page) * row_bytes;
+#pragma unroll
+                        for (uint32_t i = 0; i < kPer; ++i, at += T::kLoadRows * row_bytes) {
+                            const uint32_t n = g * kPer + i;
+                            dma_to_lds(at, (kV ? voff : koff)[n % kPatterns], to + (at0 + n) * 1024);
+                        }
+                    }
+                };
+                if (wide)
+                    each(std::integral_constant<uint32_t, kWide>{});
+                else
+                    each(std::integral_constant<uint32_t, 8>{});
             } else {
                 // rows past the last one: the last one again
                 const uint32_t last_key = uint32_t(d.nk) - 1;
@@ -714,8 +739,8 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys, !k
                     const uint32_t r = (at0 + n) * T::kLoadRows, key = s * kStage + r, from = l / T::kChunks;
                     const uint32_t j = key < last_key ? key : last_key / T::kLoadRows * T::kLoadRows;
                     const uint32_t mine = key + from < last_key ? key + from : last_key;
-                    dma_to_lds((kV ? vbase : kbase) + page_of(a, entry_of(a, d, j)) * page_bytes + (j & in_page) * token,
-                               (mine - j) * uint32_t(token) + column(kV, r + from), to + (at0 + n) * 1024);
+                    dma_to_lds((kV ? vbase : kbase) + uint64_t(page_of(a, entry_of(a, d, j))) * page_bytes + (j & in_page) * row_bytes,
+                               (mine - j) * row_bytes + column(kV, r + from), to + (at0 + n) * 1024);
                 }
             }
         } else if ((s + 1) * kStage <= uint32_t(d.nk)) {

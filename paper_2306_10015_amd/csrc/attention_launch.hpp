@@ -29,10 +29,10 @@ struct AttentionArgs {
 // The keys and values of a paged cache: k and v are its first page's, k_token and v_token the
 // bytes from one row of a page to the next, and a document's k_first its first entry in `pages`.
 struct PagedArgs : AttentionArgs {
-    uint64_t pages;           // uint32 [entries]
+    uint64_t pages;  // uint32 [entries]
     uint64_t entries;
-    uint64_t k_page, v_page;  // bytes from one page to the next
-    uint64_t tree;            // uint64 [q_tokens, tree_words], or 0
+    uint64_t tree;   // uint64 [q_tokens, tree_words], or 0
+    uint32_t k_page, v_page;  // bytes from one page to the next
     uint32_t n_pages, page_shift, tree_words;
 };
 

@@ -239,6 +239,10 @@ int paged_attention(const mezo_attention_t* pa, const mezo_pages_t* pc, void* wo
     if (a.k_token * e >= MEZO_ATTENTION_MAX_STRIDE || a.v_token * e >= MEZO_ATTENTION_MAX_STRIDE ||
         a.k_token >= MEZO_ATTENTION_MAX_STRIDE || a.v_token >= MEZO_ATTENTION_MAX_STRIDE)
         return MEZO_EINVAL;
+    // a page's rows, and the next page, by 32 bits
+    constexpr uint64_t kMost = 1ull << 32;
+    if (c.k_page >= kMost / e || c.v_page >= kMost / e || a.k_token * c.rows >= kMost / e || a.v_token * c.rows >= kMost / e)
+        return MEZO_EINVAL;
     Strided s[4];
     if (!parts_of(a.q, a.q_tokens, a.q_token, a.heads, a.q_head, a.dim, e, s[0]) ||
         !parts_of(a.out, a.q_tokens, a.o_token, a.heads, a.o_head, a.dim, e, s[3]) ||
@@ -278,8 +282,8 @@ int paged_attention(const mezo_attention_t* pa, const mezo_pages_t* pc, void* wo
     g.v_head = a.v_head * e;
     g.o_token = a.o_token * e;
     g.o_head = a.o_head * e;
-    g.k_page = c.k_page * e;
-    g.v_page = c.v_page * e;
+    g.k_page = static_cast<uint32_t>(c.k_page * e);
+    g.v_page = static_cast<uint32_t>(c.v_page * e);
     g.q_tokens = a.q_tokens;
     g.k_tokens = 0;  // (the pages say what there is)
     g.pages = address(c.list);

@@ -100,7 +100,8 @@ def test_attention_refusals():
                 dict(out=O + 8), dict(lse=E + 2), dict(docs=T + 4), dict(list=P + 2), dict(tree=F + 4, tree_words=1),
                 dict(tree=F), dict(tree=F, tree_words=1025), dict(tree=F, tree_words=1, slopes=S),
                 dict(tree=F, tree_words=1, causal=0), dict(q_token=260), dict(k_page=2044), dict(v_page=1),
-                dict(k_token=1 << 25), dict(v_token=1 << 63), dict(k_page=1 << 62), dict(n_pages=1 << 32),
+                dict(k_token=1 << 25), dict(v_token=1 << 63), dict(k_page=1 << 62), dict(k_page=1 << 31),
+                dict(v_page=1 << 31), dict(k_token=1 << 24, rows=256), dict(n_pages=1 << 32),
                 dict(n_entries=1 << 35), dict(n_docs=1 << 23), dict(max_k=1 << 31, n_entries=1 << 30)):
         assert attend(**bad) == mezo.EINVAL, bad
     assert attend(dtype=mezo.NF4) == mezo.EDTYPE
