@@ -16,6 +16,8 @@
 // largest power of two that divides it): a vector of a pair's first columns and the one of
 // their partners, or a vector of whole pairs. Neighbouring lanes take neighbouring vectors of
 // a head, then heads, then tokens.
+#include <type_traits>
+
 #include "cache_append_launch.hpp"
 #include "records.hpp"
 #include "stream_io.hpp"
@@ -23,7 +25,8 @@
 namespace mezo {
 
 constexpr uint32_t kAppendThreads = 256;
-constexpr uint32_t kMostAngles = 4096;  // of a workgroup, in LDS
+constexpr uint32_t kMostAngles = 1024;  // of a workgroup, in LDS (8 KB: eight workgroups a CU)
+constexpr uint32_t kTileBytes = 32768;
 constexpr uint32_t kMostTile = 64;      // tokens of a workgroup
 
 template <uint32_t kBytes>
@@ -44,8 +47,15 @@ struct Vector {
     typedef element_t type __attribute__((ext_vector_type(kW)));
     type v;
 
-    __device__ __forceinline__ void load(uint64_t at) { v = *reinterpret_cast<const MEZO_GLOBAL type*>(at); }
-    __device__ __forceinline__ void store(uint64_t at) const { *reinterpret_cast<MEZO_GLOBAL type*>(at) = v; }
+    __device__ __forceinline__ void load(uint64_t at) { v = __builtin_nontemporal_load(reinterpret_cast<const MEZO_GLOBAL type*>(at)); }
+    template <bool kStream>
+    __device__ __forceinline__ void store(uint64_t at) const
+    {
+        if constexpr (kStream)
+            __builtin_nontemporal_store(v, reinterpret_cast<MEZO_GLOBAL type*>(at));
+        else
+            *reinterpret_cast<MEZO_GLOBAL type*>(at) = v;
+    }
     __device__ __forceinline__ float get(uint32_t i) const
     {
         if constexpr (kF) return __uint_as_float(v[i]);
@@ -64,8 +74,15 @@ template <bool kF>
 struct Vector<kF, 1> {
     typedef typename Bits<kF ? 4 : 2>::type type;
     type v;
-    __device__ __forceinline__ void load(uint64_t at) { v = *reinterpret_cast<const MEZO_GLOBAL type*>(at); }
-    __device__ __forceinline__ void store(uint64_t at) const { *reinterpret_cast<MEZO_GLOBAL type*>(at) = v; }
+    __device__ __forceinline__ void load(uint64_t at) { v = __builtin_nontemporal_load(reinterpret_cast<const MEZO_GLOBAL type*>(at)); }
+    template <bool kStream>
+    __device__ __forceinline__ void store(uint64_t at) const
+    {
+        if constexpr (kStream)
+            __builtin_nontemporal_store(v, reinterpret_cast<MEZO_GLOBAL type*>(at));
+        else
+            *reinterpret_cast<MEZO_GLOBAL type*>(at) = v;
+    }
     __device__ __forceinline__ float get(uint32_t) const
     {
         if constexpr (kF) return __uint_as_float(v);
@@ -85,29 +102,42 @@ struct Slot {
     uint64_t k, v;  // their rows of the cache; 0: nowhere
 };
 
-// Lanes over (token, head, vector) of `count` vectors a head, in this order from the last:
-// each lane keeps its vector and steps through the heads.
-template <class F>
-__device__ __forceinline__ void over_heads(uint32_t tokens, uint32_t heads, uint32_t count, F&& body)
+// Lanes over (token, head, vector) of `count` vectors a head: each keeps its vector and steps
+// through the heads, kAhead of them at a time, whose loads are all under way before the first
+// is used.
+constexpr uint32_t kAhead = 2;
+
+template <class S, class L, class F>
+__device__ __forceinline__ void over_heads(uint32_t tokens, uint32_t heads, uint32_t count, L&& load, F&& finish)
 {
     const uint32_t step = kAppendThreads / count, lane_head = threadIdx.x / count, c = threadIdx.x - lane_head * count;
     if (lane_head >= step) return;
     uint32_t h = lane_head, t = 0;
-    while (h >= heads) {
-        h -= heads;
-        ++t;
-    }
-    while (t < tokens) {
-        body(t, h, c);
-        h += step;
+    auto wrap = [&] {
         while (h >= heads) {
             h -= heads;
             ++t;
         }
+    };
+    wrap();
+    while (t < tokens) {
+        S s[kAhead];
+        uint32_t st[kAhead], sh[kAhead];
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u) {
+            st[u] = t;
+            sh[u] = h;
+            if (t < tokens) load(s[u], t, h, c);
+            h += step;
+            wrap();
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u)
+            if (st[u] < tokens) finish(s[u], st[u], sh[u], c);
     }
 }
 
-template <bool kF, uint32_t kW, bool kPairs>
+template <bool kF, uint32_t kW, bool kPairs, bool kStream>
 __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(AppendArgs a)
 {
     constexpr uint32_t kElement = kF ? 4 : 2;
@@ -156,73 +186,80 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(AppendArgs
     const uint32_t h0 = a.heads * part / a.parts, heads = a.heads * (part + 1) / a.parts - h0;
     const uint32_t g0 = a.kv_heads * part / a.parts, kv_heads = a.kv_heads * (part + 1) / a.parts - g0;
 
-    // one vector of a head that is turned, and the one of its partners, from `in` to `out`
-    auto turned = [&](uint64_t in, uint64_t out, uint32_t t, uint32_t c) {
+    // a vector of a head that is turned, and the one of its partners
+    struct Both {
+        V x, y;
+    };
+    const uint32_t half = pairs * kElement;
+    auto load = [&](Both& s, uint64_t in, uint32_t c) {
+        s.x.load(in + c * kVector);
+        if constexpr (!kPairs) s.y.load(in + half + c * kVector);
+    };
+    auto turned = [&](const Both& s, uint64_t out, uint32_t t, uint32_t c) {
         const float2* cs = turn + t * pairs;
+        Both o = s;
         if constexpr (kPairs) {
-            V x;
-            x.load(in + c * kVector);
-            V y = x;
 #pragma unroll
             for (uint32_t i = 0; i + 1 < kW; i += 2) {
                 const float2 u = cs[(c * kW + i) / 2];
-                const float p = x.get(i), q = x.get(i + 1);
-                y.set(i, __builtin_fmaf(p, u.x, -(q * u.y)));
-                y.set(i + 1, __builtin_fmaf(p, u.y, q * u.x));
+                const float p = s.x.get(i), q = s.x.get(i + 1);
+                o.x.set(i, __builtin_fmaf(p, u.x, -(q * u.y)));
+                o.x.set(i + 1, __builtin_fmaf(p, u.y, q * u.x));
             }
-            y.store(out + c * kVector);
+            o.x.template store<kStream>(out + c * kVector);
         } else {
-            const uint32_t half = pairs * kElement;
-            V x, y;
-            x.load(in + c * kVector);
-            y.load(in + half + c * kVector);
-            V u = x, w = y;
 #pragma unroll
             for (uint32_t i = 0; i < kW; ++i) {
                 const float2 z = cs[c * kW + i];
-                const float p = x.get(i), q = y.get(i);
-                u.set(i, __builtin_fmaf(p, z.x, -(q * z.y)));
-                w.set(i, __builtin_fmaf(p, z.y, q * z.x));
+                const float p = s.x.get(i), q = s.y.get(i);
+                o.x.set(i, __builtin_fmaf(p, z.x, -(q * z.y)));
+                o.y.set(i, __builtin_fmaf(p, z.y, q * z.x));
             }
-            u.store(out + c * kVector);
-            w.store(out + half + c * kVector);
+            o.x.template store<kStream>(out + c * kVector);
+            o.y.template store<kStream>(out + half + c * kVector);
         }
     };
-    auto copied = [&](uint64_t in, uint64_t out) {
-        V x;
-        x.load(in);
-        x.store(out);
-    };
-    const uint32_t turning = kPairs ? a.rot / kW : pairs / kW, rest = (a.dim - a.rot) / kW;
+    const uint32_t turning = kPairs ? a.rot / kW : pairs / kW, rest = (a.dim - a.rot) / kW, rot = a.rot * kElement;
     if (a.q && heads) {
         const uint64_t in0 = a.q + token0 * a.q_token + h0 * a.q_head, out0 = a.q_out + token0 * a.o_token + h0 * a.o_head;
         if (turning)
-            over_heads(tokens, heads, turning, [&](uint32_t t, uint32_t h, uint32_t c) {
-                turned(in0 + t * a.q_token + h * a.q_head, out0 + t * a.o_token + h * a.o_head, t, c);
-            });
+            over_heads<Both>(
+                tokens, heads, turning,
+                [&](Both& s, uint32_t t, uint32_t h, uint32_t c) { load(s, in0 + t * a.q_token + h * a.q_head, c); },
+                [&](const Both& s, uint32_t t, uint32_t h, uint32_t c) {
+                    turned(s, out0 + t * a.o_token + h * a.o_head, t, c);
+                });
         if (rest)
-            over_heads(tokens, heads, rest, [&](uint32_t t, uint32_t h, uint32_t c) {
-                const uint32_t at = a.rot * kElement + c * kVector;
-                copied(in0 + t * a.q_token + h * a.q_head + at, out0 + t * a.o_token + h * a.o_head + at);
-            });
+            over_heads<V>(
+                tokens, heads, rest,
+                [&](V& s, uint32_t t, uint32_t h, uint32_t c) { s.load(in0 + t * a.q_token + h * a.q_head + rot + c * kVector); },
+                [&](const V& s, uint32_t t, uint32_t h, uint32_t c) {
+                    s.template store<kStream>(out0 + t * a.o_token + h * a.o_head + rot + c * kVector);
+                });
     }
     if (!kv_heads) return;
     const uint64_t k0 = a.k + token0 * a.k_token + g0 * a.k_head, v0 = a.v + token0 * a.v_token + g0 * a.v_head;
     if (turning)
-        over_heads(tokens, kv_heads, turning, [&](uint32_t t, uint32_t h, uint32_t c) {
-            if (slots[t].k) turned(k0 + t * a.k_token + h * a.k_head, slots[t].k + (g0 + h) * a.kc_head, t, c);
-        });
+        over_heads<Both>(
+            tokens, kv_heads, turning,
+            [&](Both& s, uint32_t t, uint32_t h, uint32_t c) { load(s, k0 + t * a.k_token + h * a.k_head, c); },
+            [&](const Both& s, uint32_t t, uint32_t h, uint32_t c) {
+                if (slots[t].k) turned(s, slots[t].k + (g0 + h) * a.kc_head, t, c);
+            });
     if (rest)
-        over_heads(tokens, kv_heads, rest, [&](uint32_t t, uint32_t h, uint32_t c) {
-            const uint32_t at = a.rot * kElement + c * kVector;
-            if (slots[t].k) copied(k0 + t * a.k_token + h * a.k_head + at, slots[t].k + (g0 + h) * a.kc_head + at);
+        over_heads<V>(
+            tokens, kv_heads, rest,
+            [&](V& s, uint32_t t, uint32_t h, uint32_t c) { s.load(k0 + t * a.k_token + h * a.k_head + rot + c * kVector); },
+            [&](const V& s, uint32_t t, uint32_t h, uint32_t c) {
+                if (slots[t].k) s.template store<kStream>(slots[t].k + (g0 + h) * a.kc_head + rot + c * kVector);
+            });
+    using Whole = Vector<kF, 16 / kElement>;
+    over_heads<Whole>(
+        tokens, kv_heads, a.dim * kElement / 16,
+        [&](Whole& s, uint32_t t, uint32_t h, uint32_t c) { s.load(v0 + t * a.v_token + h * a.v_head + c * 16); },
+        [&](const Whole& s, uint32_t t, uint32_t h, uint32_t c) {
+            if (slots[t].v) s.template store<kStream>(slots[t].v + (g0 + h) * a.vc_head + c * 16);
         });
-    over_heads(tokens, kv_heads, a.dim * kElement / 16, [&](uint32_t t, uint32_t h, uint32_t c) {
-        if (!slots[t].v) return;
-        Vector<kF, 16 / kElement> x;
-        x.load(v0 + t * a.v_token + h * a.v_head + c * 16);
-        x.store(slots[t].v + (g0 + h) * a.vc_head + c * 16);
-    });
 }
 
 template <bool kF, uint32_t kW>
@@ -238,7 +275,7 @@ hipError_t launch(AppendArgs& a, hipStream_t stream)
     // Tokens of a workgroup: about 32 KB of what is read, so that the angles' latency is a
     // small part, as long as that leaves work for all CUs; few tokens: their heads are shared out.
     const uint32_t bytes = (a.heads + 2 * a.kv_heads) * a.dim * (kF ? 4 : 2);
-    uint32_t tile = bytes >= 32768 ? 1 : 32768 / bytes;
+    uint32_t tile = bytes >= kTileBytes ? 1 : kTileBytes / bytes;
     tile = tile > kMostTile ? kMostTile : tile;
     if (pairs && tile > kMostAngles / pairs) tile = kMostAngles / pairs;
     const uint64_t tokens = uint64_t(a.docs) * a.max_q;
@@ -248,12 +285,15 @@ hipError_t launch(AppendArgs& a, hipStream_t stream)
     a.parts = groups >= 256 ? 1 : (groups >= 64 ? 2 : 4);
     if (a.parts > a.kv_heads) a.parts = a.kv_heads;
     void* params[] = {&a};
-    const void* f;
-    if constexpr (kW == 1)  // (pairs next to each other are even in number)
-        f = reinterpret_cast<const void*>(cache_append_kernel<kF, 1, false>);
-    else
-        f = a.interleaved ? reinterpret_cast<const void*>(cache_append_kernel<kF, kW, true>)
-                          : reinterpret_cast<const void*>(cache_append_kernel<kF, kW, false>);
+    // Calls larger than the caches write around them.
+    const bool stream_out = tokens * bytes > (64u << 20);
+    auto pick = [&](auto streams) {
+        constexpr bool kStream = decltype(streams)::value;
+        if constexpr (kW > 1)  // (pairs next to each other are even in number)
+            if (a.interleaved) return reinterpret_cast<const void*>(cache_append_kernel<kF, kW, true, kStream>);
+        return reinterpret_cast<const void*>(cache_append_kernel<kF, kW, false, kStream>);
+    };
+    const void* f = stream_out ? pick(std::integral_constant<bool, true>{}) : pick(std::integral_constant<bool, false>{});
     return hipLaunchKernel(f, dim3(uint32_t(groups * a.parts)), dim3(kAppendThreads), params, 0, stream);
 }
 
