@@ -76,13 +76,30 @@ struct LayArgs {
     uint64_t rows, k, columns;
 };
 
+// A unit of 8 columns by its number: its row and first column (32 bits where they hold the
+// number: a division in 64 takes as long as the rest).
+struct Unit {
+    uint64_t row, col;
+};
+__device__ __forceinline__ Unit unit_of(const LayArgs& a, uint64_t i)
+{
+    const uint64_t per_row = a.columns / 8;
+    if (a.rows * per_row <= 0xFFFFFFFFu) {  // (uniform)
+        const uint32_t row = uint32_t(i) / uint32_t(per_row);
+        return {row, (i - uint64_t(row) * per_row) * 8};
+    }
+    const uint64_t row = i / per_row;
+    return {row, (i - row * per_row) * 8};
+}
+
 // Rows of values into planes: a lane 8 columns.
 template <bool kF>
 __global__ void __launch_bounds__(256) nf4_lay_values_kernel(LayArgs a)
 {
-    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x, per_row = a.columns / 8;
-    if (i >= a.rows * per_row) return;
-    const uint64_t row = i / per_row, c = (i - row * per_row) * 8;
+    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= a.rows * (a.columns / 8)) return;
+    const Unit at = unit_of(a, i);
+    const uint64_t row = at.row, c = at.col;
     float x[8];
 #pragma unroll
     for (uint32_t j = 0; j < 8; ++j) {
@@ -103,10 +120,10 @@ template <bool kF>
 __global__ void __launch_bounds__(256) nf4_copy_rows_kernel(LayArgs a)
 {
     using element_t = std::conditional_t<kF, gu32_t, gu16_t>;
-    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x, per_row = a.columns / 8;
-    if (i >= a.rows * per_row) return;
-    const uint64_t row = i / per_row, c = (i - row * per_row) * 8;
-    const element_t* from = reinterpret_cast<const element_t*>(a.from) + row * a.ld + c;
+    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= a.rows * (a.columns / 8)) return;
+    const Unit at = unit_of(a, i);
+    const element_t* from = reinterpret_cast<const element_t*>(a.from) + at.row * a.ld + at.col;
     element_t* to = reinterpret_cast<element_t*>(a.to) + i * 8;
 #pragma unroll
     for (uint32_t j = 0; j < 8; ++j) to[j] = from[j];
@@ -128,28 +145,56 @@ __device__ __forceinline__ uint32_t eight_codes(uint64_t codes, uint64_t e, uint
     return uint32_t((uint64_t(word((e >> 3) + 1)) << 32 | lo) >> shift);
 }
 
-// Rows of weights into planes: a lane 8 columns.
-template <bool kWide>
+constexpr uint32_t kExpandUnits = 4;
+typedef float v2f_t __attribute__((ext_vector_type(2)));
+
+// Rows of weights into planes: a lane 8 columns at a time, kExpandUnits of them, whose loads
+// are all under way before the first is used. A code's value comes from the lane that holds it.
+// kWhole: k is a multiple of 8, so a unit is a whole word of codes under one scale.
+template <bool kWide, bool kWhole>
 __global__ void __launch_bounds__(256) nf4_expand_kernel(LayArgs a)
 {
-    __shared__ float table[kNF4Codes];
-    if (threadIdx.x < kNF4Codes) table[threadIdx.x] = kNF4Values[threadIdx.x];
-    __syncthreads();
-    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x, per_row = a.columns / 8;
-    if (i >= a.rows * per_row) return;
-    const uint64_t row = i / per_row, c = (i - row * per_row) * 8;
-    float x[8] = {};
-    if (c < a.k) {
-        const uint64_t e = a.first + row * a.k + c, top = (a.last - 1) / kNF4Block;
-        const uint32_t d = eight_codes(a.from, e, a.last);
-        const uint64_t b0 = e / kNF4Block, b1 = b0 < top ? b0 + 1 : top;
-        const float s0 = reinterpret_cast<const gfloat_t*>(a.absmax)[b0], s1 = reinterpret_cast<const gfloat_t*>(a.absmax)[b1];
-        const uint32_t left = kNF4Block - uint32_t(e % kNF4Block);
+    uint32_t table = 0;
 #pragma unroll
-        for (uint32_t j = 0; j < 8; ++j)
-            if (c + j < a.k) x[j] = table[d >> (4 * j) & 15u] * (j < left ? s0 : s1);
+    for (uint32_t i = 0; i < kNF4Codes; ++i)
+        table = (threadIdx.x & 15u) == i ? __builtin_bit_cast(uint32_t, kNF4Values[i]) : table;
+    const uint64_t i0 = uint64_t(blockIdx.x) * (256 * kExpandUnits) + threadIdx.x, all = a.rows * (a.columns / 8);
+    [[maybe_unused]] const uint64_t top = (a.last - 1) / kNF4Block;
+    uint32_t codes[kExpandUnits], valid[kExpandUnits];
+    float s0[kExpandUnits];
+    [[maybe_unused]] uint32_t left[kExpandUnits];
+    [[maybe_unused]] float s1[kExpandUnits];
+#pragma unroll
+    for (uint32_t u = 0; u < kExpandUnits; ++u) {
+        const uint64_t i = i0 + u * 256;
+        const Unit at = unit_of(a, i < all ? i : all - 1);
+        valid[u] = at.col >= a.k ? 0u : (a.k - at.col < 8 ? uint32_t(a.k - at.col) : 8u);
+        const uint64_t e = a.first + at.row * a.k + (valid[u] ? at.col : 0), b = e / kNF4Block;
+        s0[u] = reinterpret_cast<const gfloat_t*>(a.absmax)[b];
+        if constexpr (kWhole) {
+            codes[u] = __builtin_nontemporal_load(reinterpret_cast<const gu32_t*>(a.from) + e / 8);
+        } else {
+            codes[u] = eight_codes(a.from, e, a.last);
+            left[u] = kNF4Block - uint32_t(e % kNF4Block);
+            s1[u] = left[u] >= 8 ? s0[u] : reinterpret_cast<const gfloat_t*>(a.absmax)[b < top ? b + 1 : top];
+        }
     }
-    store_planes<kWide>(a.to + i * 16, a.plane, x);
+#pragma unroll
+    for (uint32_t u = 0; u < kExpandUnits; ++u) {
+        const uint64_t i = i0 + u * 256;
+        float x[8];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)  // (by all lanes: any of them may be asked)
+            x[j] = __uint_as_float(uint32_t(__builtin_amdgcn_ds_bpermute(int((codes[u] >> (4 * j) & 15u) << 2), int(table))));
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+            if constexpr (kWhole)
+                x[j] = valid[u] ? x[j] * s0[u] : 0.0f;
+            else
+                x[j] = j < valid[u] ? x[j] * (j < left[u] ? s0[u] : s1[u]) : 0.0f;
+        }
+        if (i < all) store_planes<kWide>(a.to + i * 16, a.plane, x);
+    }
 }
 
 // ---- the product of what was laid out ------------------------------------------------
@@ -344,7 +389,6 @@ struct NF4ThinArgs {
     uint32_t splits;
 };
 
-typedef float v2f_t __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
 // A float as three bf16 by cutting, eight at a time.
@@ -655,8 +699,9 @@ hipError_t launch_tiled(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t s
     for (uint64_t n0 = 0; n0 < a.n; n0 += cut.slab) {
         lay.rows = a.n - n0 < cut.slab ? a.n - n0 : cut.slab;
         lay.first = n0 * a.k;
-        hipError_t e = run(reinterpret_cast<const void*>(nf4_expand_kernel<kWide>),
-                           dim3(uint32_t((lay.rows * (columns / 8) + 255) / 256)), 256, lay, stream);
+        hipError_t e = run(a.k % 8 ? reinterpret_cast<const void*>(nf4_expand_kernel<kWide, false>)
+                                   : reinterpret_cast<const void*>(nf4_expand_kernel<kWide, true>),
+                           dim3(uint32_t((lay.rows * (columns / 8) + 256 * kExpandUnits - 1) / (256 * kExpandUnits))), 256, lay, stream);
         if (e != hipSuccess) return e;
         g.n = uint32_t(lay.rows);
         g.c = a.c + n0 * (kWideOut ? 4 : 2);
