@@ -428,6 +428,11 @@ __device__ __forceinline__ v4f_t product(const Planes& w, const Planes& x, v4f_t
 
 constexpr uint32_t kThinWaves = 16;
 
+// fp32: the table holds the three parts of each value, and a block's sum is scaled as a whole.
+// The values are kept 2^-7 of themselves, so that no sum of 64 products of finite activations
+// overflows where its scaled value does not.
+constexpr float kThinScale = 0x1p-7f;
+
 template <bool kF, uint32_t kRowWaves, uint32_t kRG, uint32_t kXRows, uint32_t kDepth, uint32_t kCopies, bool kWideOut>
 __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a)
 {
@@ -444,7 +449,7 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
     static_assert(kRows * kCodeChunks % 64 == 0 && kXRows * kXChunks % 64 == 0 && kRows * kKWaves % 64 == 0);
     constexpr uint32_t kLoads = kCodeLoads + kXLoads + kScaleLoads, kPerWave = (kLoads + kThinWaves - 1) / kThinWaves;
     // (one object, the table first: its addresses then need no base)
-    constexpr uint32_t kTable = kNF4Pairs * kCopies * sizeof(v2f_t);
+    constexpr uint32_t kTable = kF ? kNF4Pairs * 256 : kNF4Pairs * kCopies * sizeof(v2f_t);
     __shared__ __attribute__((aligned(1024))) uint8_t memory[kTable + kDepth * kStage];
     uint8_t* const lds = memory + kTable;
     static_assert(kKWaves * kRows * kFM * 16 * 4 <= sizeof(memory), "the waves' sums fit");
@@ -519,15 +524,28 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
             v.x = (byte & 15u) == i ? kNF4Values[i] : v.x;
             v.y = (byte >> 4) == i ? kNF4Values[i] : v.y;
         }
-        const v4f_t twice = {v.x, v.y, v.x, v.y};
+        if constexpr (kF) {
+            // a row of 256 bytes: the pair's first and second parts 16 times, its third 32 times
+            const float lo[8] = {v.x * kThinScale, v.y * kThinScale, 0, 0, 0, 0, 0, 0};
+            const Planes p = planes_of(lo);
+            const u32x4_t a0 = __builtin_bit_cast(u32x4_t, p.p[0]), a1 = __builtin_bit_cast(u32x4_t, p.p[1]),
+                          a2 = __builtin_bit_cast(u32x4_t, p.p[2]);
+            const u32x4_t w = threadIdx.x % 4 < 2 ? u32x4_t{a0[0], a1[0], a0[0], a1[0]} : u32x4_t{a2[0], a2[0], a2[0], a2[0]};
 #pragma unroll
-        for (uint32_t i = 0; i < kCopies / 2 / kEach; ++i)
-            *reinterpret_cast<v4f_t*>(memory + (byte * (kCopies / 2) + i * kEach + threadIdx.x % kEach) * 16) = twice;
+            for (uint32_t i = 0; i < 4; ++i)
+                *reinterpret_cast<u32x4_t*>(memory + byte * 256 + threadIdx.x % 4 * 64 + i * 16) = w;
+        } else {
+            const v4f_t twice = {v.x, v.y, v.x, v.y};
+#pragma unroll
+            for (uint32_t i = 0; i < kCopies / 2 / kEach; ++i)
+                *reinterpret_cast<v4f_t*>(memory + (byte * (kCopies / 2) + i * kEach + threadIdx.x % kEach) * 16) = twice;
+        }
     }
 
     const uint32_t fr = l & 15u, fg = l >> 4;
     const uint32_t rw = wave / kKWaves, q = wave % kKWaves;
-    const uint32_t mine = (l % kCopies) * 8;  // this lane's copy
+    const uint32_t mine = kF ? (l & 15u) * 8 : (l % kCopies) * 8;  // this lane's copy
+    [[maybe_unused]] const uint32_t third = 128 + (l & 31u) * 4;   // and of third parts
     // where this lane reads in a stage: of each of its groups of 16 rows, and of the activations
     const uint32_t xr = kXRows < 16 ? fr % kXRows : fr;
     uint32_t code_at[kRG], scale_at[kRG], x_at[2];
@@ -535,7 +553,7 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
     for (uint32_t g = 0; g < kRG; ++g) {
         const uint32_t r = (rw * kRG + g) * 16 + fr;
         code_at[g] = (r * kCodeChunks + ((2 * q + (fg >> 1)) ^ code_swizzle(r))) * 16 + (fg & 1u) * 8;
-        scale_at[g] = kScaleAt + (r * kKWaves + q) * 4;
+        scale_at[g] = kScaleAt + ((kF ? (rw * kRG + g) * 16 + fg * 4 : r) * kKWaves + q) * 4;
     }
 #pragma unroll
     for (uint32_t h = 0; h < 2; ++h)
@@ -557,32 +575,35 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
         const uint8_t* t = lds + (s - s0) % kDepth * kStage;
         // 16 weights of a row for each group, all lookups under way before the first is used
         u32x2_t code[kRG];
-        float scale[kRG];
-        v2f_t w[kRG][2][4];
 #pragma unroll
-        for (uint32_t g = 0; g < kRG; ++g) {
-            code[g] = *reinterpret_cast<const u32x2_t*>(t + code_at[g]);
-            scale[g] = *reinterpret_cast<const float*>(t + scale_at[g]);
-        }
+        for (uint32_t g = 0; g < kRG; ++g) code[g] = *reinterpret_cast<const u32x2_t*>(t + code_at[g]);
+        if constexpr (kF) {
+            u32x2_t w[kRG][2][4];
+            uint32_t w3[kRG][2][4];
 #pragma unroll
-        for (uint32_t g = 0; g < kRG; ++g)
+            for (uint32_t g = 0; g < kRG; ++g)
 #pragma unroll
-            for (uint32_t h = 0; h < 2; ++h)
+                for (uint32_t h = 0; h < 2; ++h)
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    const uint32_t at = kCopies == 32 ? __builtin_amdgcn_perm(code[g][h], mine, 0x0C0C0000u | (4 + i) << 8)
-                                                      : (code[g][h] >> (8 * i) & 255u) * (kCopies * 8) | mine;
-                    w[g][h][i] = *reinterpret_cast<const v2f_t*>(memory + at);
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        const uint32_t byte = 0x0C0C0000u | (4 + i) << 8;
+                        w[g][h][i] = *reinterpret_cast<const u32x2_t*>(memory + __builtin_amdgcn_perm(code[g][h], mine, byte));
+                        w3[g][h][i] = *reinterpret_cast<const uint32_t*>(memory + __builtin_amdgcn_perm(code[g][h], third, byte));
+                    }
+            __builtin_amdgcn_sched_barrier(0);
+            v4f_t sum[kRG][kFM] = {};  // of this block, unscaled
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) {
+                Planes p[kRG];
+#pragma unroll
+                for (uint32_t g = 0; g < kRG; ++g) {
+                    p[g].p[0] = __builtin_bit_cast(v8bf_t, u32x4_t{w[g][h][0].x, w[g][h][1].x, w[g][h][2].x, w[g][h][3].x});
+                    p[g].p[1] = __builtin_bit_cast(v8bf_t, u32x4_t{w[g][h][0].y, w[g][h][1].y, w[g][h][2].y, w[g][h][3].y});
+                    p[g].p[2] = __builtin_bit_cast(v8bf_t, u32x4_t{w3[g][h][0], w3[g][h][1], w3[g][h][2], w3[g][h][3]});
                 }
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (uint32_t h = 0; h < 2; ++h) {  // 32 of the block's 64 columns: 8 of each lane
-            std::conditional_t<kF, Planes, v8bf_t> x[kFM];
-#pragma unroll
-            for (uint32_t f = 0; f < kFM; ++f) {
-                const uint8_t* at = t + x_at[h] + f * 16 * kXChunks * 16;
-                if constexpr (kF) {
-                    const u32x4_t lo = *reinterpret_cast<const u32x4_t*>(at);
+                for (uint32_t f = 0; f < kFM; ++f) {
+                    const u32x4_t lo = *reinterpret_cast<const u32x4_t*>(t + x_at[h] + f * 16 * kXChunks * 16);
                     const u32x4_t hi = *reinterpret_cast<const u32x4_t*>(t + (x_at[h] ^ 16u) + f * 16 * kXChunks * 16);
                     float v[8];
 #pragma unroll
@@ -590,32 +611,52 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
                         v[i] = __uint_as_float(lo[i]);
                         v[i + 4] = __uint_as_float(hi[i]);
                     }
-                    x[f] = planes_of(v);
-                } else {
-                    x[f] = *reinterpret_cast<const v8bf_t*>(at);
+                    const Planes x = planes_of(v);
+#pragma unroll
+                    for (uint32_t g = 0; g < kRG; ++g) sum[g][f] = product(p[g], x, sum[g][f]);
                 }
             }
 #pragma unroll
-            for (uint32_t g = 0; g < kRG; ++g) {
-                float v[8];
+            for (uint32_t g = 0; g < kRG; ++g)
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    v[2 * i] = w[g][h][i].x * scale[g];
-                    v[2 * i + 1] = w[g][h][i].y * scale[g];
+                for (uint32_t i = 0; i < 4; ++i) {  // a lane's results are rows 4 fg .. + 3
+                    const float scale = *reinterpret_cast<const float*>(t + scale_at[g] + i * kKWaves * 4);
+#pragma unroll
+                    for (uint32_t f = 0; f < kFM; ++f) acc[g][f][i] = __builtin_fmaf(sum[g][f][i], scale, acc[g][f][i]);
                 }
-                std::conditional_t<kF, Planes, v8bf_t> wide;
-                if constexpr (kF) {
-                    wide = planes_of(v);
-                } else {
+        } else {
+            float scale[kRG];
+            v2f_t w[kRG][2][4];
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) wide[i] = static_cast<__bf16>(v[i]);
-                }
+            for (uint32_t g = 0; g < kRG; ++g) scale[g] = *reinterpret_cast<const float*>(t + scale_at[g]);
 #pragma unroll
-                for (uint32_t f = 0; f < kFM; ++f) {
-                    if constexpr (kF)
-                        acc[g][f] = product(wide, x[f], acc[g][f]);
-                    else
-                        acc[g][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide, x[f], acc[g][f], 0, 0, 0);
+            for (uint32_t g = 0; g < kRG; ++g)
+#pragma unroll
+                for (uint32_t h = 0; h < 2; ++h)
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        const uint32_t at = kCopies == 32 ? __builtin_amdgcn_perm(code[g][h], mine, 0x0C0C0000u | (4 + i) << 8)
+                                                          : (code[g][h] >> (8 * i) & 255u) * (kCopies * 8) | mine;
+                        w[g][h][i] = *reinterpret_cast<const v2f_t*>(memory + at);
+                    }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) {  // 32 of the block's 64 columns: 8 of each lane
+                v8bf_t x[kFM];
+#pragma unroll
+                for (uint32_t f = 0; f < kFM; ++f)
+                    x[f] = *reinterpret_cast<const v8bf_t*>(t + x_at[h] + f * 16 * kXChunks * 16);
+#pragma unroll
+                for (uint32_t g = 0; g < kRG; ++g) {
+                    v8bf_t b;
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        b[2 * i] = static_cast<__bf16>(w[g][h][i].x * scale[g]);
+                        b[2 * i + 1] = static_cast<__bf16>(w[g][h][i].y * scale[g]);
+                    }
+#pragma unroll
+                    for (uint32_t f = 0; f < kFM; ++f)
+                        acc[g][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, x[f], acc[g][f], 0, 0, 0);
                 }
             }
         }
@@ -641,6 +682,7 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
         v4f_t sum = room[t * 64 + l];
 #pragma unroll
         for (uint32_t w = 1; w < kKWaves; ++w) sum += room[(w * kTiles + t) * 64 + l];
+        if constexpr (kF) sum *= 1.0f / kThinScale;
         const uint32_t row = m0 + t % kFM * 16 + fr, column = n0 + t / kFM * 16 + fg * 4;
         if ((kXRows < 16 && fr >= kXRows) || row >= a.m || column >= a.n) continue;
         if (a.splits == 1)
@@ -764,7 +806,9 @@ hipError_t launch_thin(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t st
     switch (cut.thin_rows) {
     case 16: e = go(nf4_thin_kernel<kWide, 1, 1, 4, kWide ? 3 : 4, 32, kWideOut>, 16, 4); break;
     case 128:
-        if constexpr (!kWide) {
+        if constexpr (kWide) {
+            e = go(nf4_thin_kernel<true, 4, 2, 16, 2, 32, kWideOut>, 128, 16);
+        } else {
             if (a.m <= 4)
                 e = go(nf4_thin_kernel<false, 2, 4, 4, 2, 32, kWideOut>, 128, 4);
             else
@@ -773,7 +817,7 @@ hipError_t launch_thin(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t st
         break;
     default:
         if (a.m <= 4)
-            e = go(nf4_thin_kernel<kWide, 2, 2, 4, 3, kWide ? 16 : 32, kWideOut>, 64, 4);
+            e = go(nf4_thin_kernel<kWide, 2, 2, 4, 3, 32, kWideOut>, 64, 4);
         else if (a.m <= 16 || kWide)
             e = go(nf4_thin_kernel<kWide, 4, 1, 16, kWide ? 3 : 4, 32, kWideOut>, 64, 16);
         else if constexpr (!kWide) {

@@ -34,17 +34,18 @@ inline NF4Cut cut_nf4(uint64_t m, uint64_t n, uint64_t k, bool wide_x)
     uint64_t slab = kNF4SlabBytes / row / 256 * 256;
     if (slab < 256) slab = 256;
     if (slab > n) slab = n;
-    if (m <= 64 && k % 64 == 0) {
+    if (m <= (wide_x ? 128 : 256) && k % 64 == 0) {
         // A workgroup a CU. One to four activations and few weights: 16 rows each and all of k
         // (4096 x 4096 8.4 us, 64 rows and k in four 10). Many rows: 128 each where that saves
         // rounds over the CUs; one takes 1.6 times as long as with 64 (1 x 50272 x 4096 36.6 us
         // in two rounds of 128, 43.7 in four of 64; 1 x 16384 x 4096 18.1 and 12.6 in one).
         const uint64_t rounds64 = ((n + 63) / 64 + 255) / 256, rounds128 = ((n + 127) / 128 + 255) / 256;
         const uint64_t rows = m <= 4 && n <= 4096                                     ? 16
-                              : m <= 32 && !wide_x && 8 * rounds128 < 5 * rounds64 ? 128
+                              : wide_x ? (m > 16 ? 128 : 64)
+                              : m <= 32 && 8 * rounds128 < 5 * rounds64 ? 128
                                                                                      : 64;
         // k split where the rows leave CUs without work, in parts of 16 blocks at least
-        const uint64_t groups = (n + rows - 1) / rows * (wide_x && m > 4 ? (m + 15) / 16 : 1);
+        const uint64_t groups = (n + rows - 1) / rows * (wide_x ? (m + 15) / 16 : (m + 63) / 64);
         const uint64_t want = groups >= 160 ? 1 : 256 / groups, most = k / 64 / 16;
         const uint64_t splits = want < most ? want : most;
         return {kThin, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits)), 0, uint32_t(rows)};
