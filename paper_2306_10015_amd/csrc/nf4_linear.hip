@@ -332,18 +332,43 @@ __global__ void __launch_bounds__(kWM* kWN * 64) nf4_matmul_kernel(NF4MatmulArgs
         }
     }
     const bool whole = whole_groups<kWideOut>(a);
+    if (whole || a.splits > 1) {
+#pragma unroll
+        for (uint32_t i = 0; i < kFM; ++i) {
+            const uint32_t row = m0 + wm + i * 16 + fr;
+            if (row >= a.m) continue;
+#pragma unroll
+            for (uint32_t j = 0; j < kFN; ++j) {
+                const uint32_t col = n0 + wn + j * 16 + fg * 4;
+                if (a.splits == 1)
+                    store4<kWideOut>(a, whole, row, col, acc[i][j]);
+                else if (col < a.n)
+                    *reinterpret_cast<MEZO_GLOBAL v4f_t*>(partial_at(a, blockIdx.y, row, col)) = acc[i][j];
+            }
+        }
+        return;
+    }
+    // Where rows of c do not lie on the alignment of four columns, a wave's part of the tile goes
+    // through LDS, 16 rows at a time, and out with neighbouring lanes on neighbouring columns (lanes
+    // would store one by one, 4 columns apart).
+    using Out = std::conditional_t<kWideOut, float, __bf16>;
+    constexpr uint32_t kCols = kFN * 16;
+    static_assert(kWaves * 16 * (kCols + 4) * 4 <= sizeof(lds), "the rows fit");
+    lds_barrier();  // the last stage is read
+    float* room = reinterpret_cast<float*>(&lds[0][0]) + wave * 16 * (kCols + 4);
+    const uint32_t col = l % kCols, n = n0 + wn + col;
+    MEZO_GLOBAL Out* c = reinterpret_cast<MEZO_GLOBAL Out*>(a.c) + n;
 #pragma unroll
     for (uint32_t i = 0; i < kFM; ++i) {
-        const uint32_t row = m0 + wm + i * 16 + fr;
-        if (row >= a.m) continue;
 #pragma unroll
-        for (uint32_t j = 0; j < kFN; ++j) {
-            const uint32_t col = n0 + wn + j * 16 + fg * 4;
-            if (a.splits == 1)
-                store4<kWideOut>(a, whole, row, col, acc[i][j]);
-            else if (col < a.n)
-                *reinterpret_cast<MEZO_GLOBAL v4f_t*>(partial_at(a, blockIdx.y, row, col)) = acc[i][j];
+        for (uint32_t j = 0; j < kFN; ++j)
+            *reinterpret_cast<v4f_t*>(room + fr * (kCols + 4) + j * 16 + fg * 4) = acc[i][j];
+        lds_wait();  // (the wave's own room)
+        for (uint32_t r = l / kCols; r < 16; r += 64 / kCols) {
+            const uint32_t row = m0 + wm + i * 16 + r;
+            if (row < a.m && n < a.n) c[row * a.ldc] = static_cast<Out>(room[r * (kCols + 4) + col]);
         }
+        lds_wait();
     }
 }
 
@@ -358,7 +383,21 @@ __global__ void __launch_bounds__(256) nf4_join_kernel(NF4MatmulArgs a)
     v4f_t sum = {};
     for (uint32_t s = 0; s < a.splits; ++s)
         sum += *reinterpret_cast<const MEZO_GLOBAL v4f_t*>(partial_at(a, s, row, col));
-    store4<kWideOut>(a, whole_groups<kWideOut>(a), row, col, sum);
+    store4<kWideOut>(a, true, row, col, sum);
+}
+
+// The same where rows of c do not lie on the alignment of four columns: a lane a column.
+template <bool kWideOut>
+__global__ void __launch_bounds__(256) nf4_join_columns_kernel(NF4MatmulArgs a)
+{
+    using Out = std::conditional_t<kWideOut, float, __bf16>;
+    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= uint64_t(a.m) * a.n) return;
+    const uint32_t row = uint32_t(i / a.n), col = uint32_t(i - uint64_t(row) * a.n);
+    float sum = 0.0f;
+    for (uint32_t s = 0; s < a.splits; ++s)
+        sum += reinterpret_cast<const gfloat_t*>(partial_at(a, s, row, col))[col & 3u];
+    (reinterpret_cast<MEZO_GLOBAL Out*>(a.c) + row * a.ldc)[col] = static_cast<Out>(sum);
 }
 
 // ---- few rows -----------------------------------------------------------------------
@@ -701,6 +740,17 @@ hipError_t run(const void* f, dim3 grid, uint32_t lanes, Args& a, hipStream_t st
     return hipLaunchKernel(f, grid, dim3(lanes), params, 0, stream);
 }
 
+template <bool kWideOut>
+hipError_t join(NF4MatmulArgs& a, hipStream_t stream)
+{
+    constexpr uint64_t kBytes = kWideOut ? 4 : 2;
+    const bool whole = ((a.c | (a.ldc * kBytes)) & (4 * kBytes - 1)) == 0;
+    const uint64_t lanes = a.m * uint64_t(whole ? (a.n + 3) / 4 : a.n);
+    return run(whole ? reinterpret_cast<const void*>(nf4_join_kernel<kWideOut>)
+                     : reinterpret_cast<const void*>(nf4_join_columns_kernel<kWideOut>),
+               dim3(uint32_t((lanes + 255) / 256)), 256, a, stream);
+}
+
 template <bool kWide, bool kWideOut>
 hipError_t launch_tiled(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t stream)
 {
@@ -758,9 +808,7 @@ hipError_t launch_tiled(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t s
         }
         if (e != hipSuccess) return e;
         if (cut.splits > 1) {
-            const uint64_t groups = a.m * ((lay.rows + 3) / 4);
-            e = run(reinterpret_cast<const void*>(nf4_join_kernel<kWideOut>), dim3(uint32_t((groups + 255) / 256)), 256, g,
-                    stream);
+            e = join<kWideOut>(g, stream);
             if (e != hipSuccess) return e;
         }
     }
@@ -835,8 +883,7 @@ hipError_t launch_thin(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t st
     j.m = g.m;
     j.n = g.n;
     j.splits = cut.splits;
-    const uint64_t groups = a.m * ((a.n + 3) / 4);
-    return run(reinterpret_cast<const void*>(nf4_join_kernel<kWideOut>), dim3(uint32_t((groups + 255) / 256)), 256, j, stream);
+    return join<kWideOut>(j, stream);
 }
 
 template <bool kWide, bool kWideOut>

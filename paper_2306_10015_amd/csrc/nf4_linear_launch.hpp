@@ -34,7 +34,10 @@ inline NF4Cut cut_nf4(uint64_t m, uint64_t n, uint64_t k, bool wide_x)
     uint64_t slab = kNF4SlabBytes / row / 256 * 256;
     if (slab < 256) slab = 256;
     if (slab > n) slab = n;
-    if (m <= (wide_x ? 128 : 256) && k % 64 == 0) {
+    // Up to so many rows the expanding does not pay: 256 x 16384 x 4096 bf16 75 us both ways, 128 41
+    // and 64; fp32, where a slice of 16 rows takes as long as its products, 1024 x 4096 x 4096 275
+    // and 278, 256 78 and 129.
+    if (m <= (wide_x ? 1024 : 256) && k % 64 == 0) {
         // A workgroup a CU. One to four activations and few weights: 16 rows each and all of k
         // (4096 x 4096 8.4 us, 64 rows and k in four 10). Many rows: 128 each where that saves
         // rounds over the CUs; one takes 1.6 times as long as with 64 (1 x 50272 x 4096 36.6 us
@@ -50,15 +53,30 @@ inline NF4Cut cut_nf4(uint64_t m, uint64_t n, uint64_t k, bool wide_x)
         const uint64_t splits = want < most ? want : most;
         return {kThin, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits)), 0, uint32_t(rows)};
     }
-    // as the 8-bit product is cut
-    const uint64_t t128 = tiles_of(m, slab, 128, 128);
-    const uint64_t rounds128 = (t128 + 511) / 512, rounds256 = (tiles_of(m, slab, 256, 256) + 255) / 256;
-    if (9 * rounds256 <= 5 * rounds128) return {k256x256, 1, slab, 0};
-    if (t128 >= 200) return {k128x128, 1, slab, 0};
+    // The tile and the split of k that take the least time by what was measured: a stage of 64
+    // columns takes a round of workgroups over the CUs 1640 ns with one tile of 256 x 256 a CU,
+    // 900 with two of 128 x 128, 750 with four of 64 x 64; a
+    // split's sums go out and back at 4 TB/s, and their join is a launch of 4 us.
+    struct Kind {
+        F8Tile tile;
+        uint64_t size, slots, stage;
+    };
+    constexpr Kind kinds[3] = {{k256x256, 256, 256, 1640}, {k128x128, 128, 512, 900}, {k64x64, 64, 1024, 750}};
     const uint64_t stages = nf4_columns(k) / 64 * (wide_x ? 6 : 1);
-    const uint64_t want = 512 / tiles_of(m, slab, 64, 64), most = stages / 16;
-    const uint64_t splits = want < most ? want : most;
-    return {k64x64, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits)), slab, 0};
+    NF4Cut best = {k64x64, 1, slab, 0};
+    uint64_t least = ~0ull;
+    for (const Kind& t : kinds)
+        for (uint64_t splits = 1; splits <= 16 && (splits == 1 || stages / splits >= 8); ++splits) {
+            const uint64_t rounds = (tiles_of(m, slab, t.size, t.size) * splits + t.slots - 1) / t.slots;
+            const uint64_t join = splits == 1 ? 0 : 4000 + splits * m * slab / 500;
+            const uint64_t time = rounds * ((stages + splits - 1) / splits) * t.stage + join;
+            if (time < least) {
+                least = time;
+                best.tile = t.tile;
+                best.splits = uint32_t(splits);
+            }
+        }
+    return best;
 }
 
 // The parts of a call's workspace, from its start: activations laid out, weights expanded,
