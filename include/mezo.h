@@ -570,9 +570,10 @@ MEZO_API int mezo_paged_attention(const mezo_attention_t* a, const mezo_pages_t*
  * they run over the ends of rows), c [m, n] of storage c_dtype (rows ldc apart;
  * MEZO_F32 or MEZO_BF16 both). w has the values that mezo_nf4_dequantize gives in
  * x_dtype: v[code] * absmax rounded to fp32, and for MEZO_BF16 to bf16. The products are
- * summed in fp32 (for MEZO_F32 but for parts below 2^-24 of a product, and what lies
- * below 2^-133 of values below 2^-110) and the sum is rounded once. A row of x that holds NaN or
- * an infinity, and a block whose absmax is one, give results that are not finite. 1 <= m, n <=
+ * summed in fp32 and the sum is rounded once; for MEZO_F32 each product is within 2^-22 of
+ * itself (v[code] * absmax may then stand unrounded), of values of x below 2^-100 and in results below
+ * 2^-110 within as much of 2^-100 and 2^-110. A row of x that holds NaN or an infinity, and a
+ * block whose absmax is one, give results that are not finite. 1 <= m, n <=
  * MEZO_F8_MAX_ROWS, 1 <= k <= MEZO_F8_MAX_COLS, m * k, n * k and m * n <= MEZO_MAX_NUMEL,
  * ldx >= k and ldc >= n where m > 1, codes and absmax 16-byte aligned (MEZO_EINVAL); c and the workspace
  * must not overlap anything else (MEZO_EOVERLAP). */

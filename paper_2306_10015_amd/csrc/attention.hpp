@@ -1075,11 +1075,37 @@ template <bool kF, class Args = AttentionArgs>
 __global__ void __launch_bounds__(256) attention_join_kernel(Args a)
 {
     const uint32_t l = threadIdx.x & 63u;
-    const uint64_t row = uint64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (row >= uint64_t(a.docs) * a.max_q * a.heads) return;
-    const uint32_t h = uint32_t(row % a.heads);
-    const int i = int(row / a.heads % a.max_q);
-    const uint32_t doc = uint32_t(row / a.heads / a.max_q);
+    const uint64_t row = uint64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint64_t rows = uint64_t(a.docs) * a.max_q * a.heads;
+    if (row >= rows) return;
+    uint32_t h, doc;
+    int i;
+    if (rows <= 0xFFFFFFFFu) {  // (divisions in 64 bits are long)
+        const uint32_t query = uint32_t(row) / a.heads;
+        h = uint32_t(row) - query * a.heads;
+        doc = query / a.max_q;
+        i = int(query - doc * a.max_q);
+    } else {
+        h = uint32_t(row % a.heads);
+        i = int(row / a.heads % a.max_q);
+        doc = uint32_t(row / a.heads / a.max_q);
+    }
+    // Everything is under way at once: the document's row, which says how many of the splits
+    // there are, and of as many as the call has the statistics and the first accumulators.
+    constexpr uint32_t kAhead = 8;  // loads in flight
+    float part[kAhead][2];
+    auto fetch = [&](uint32_t s0, uint32_t splits) {
+#pragma unroll
+        for (uint32_t s = 0; s < kAhead; ++s) {
+            const uint64_t at = partial_row(a, s0 + s < splits ? s0 + s : splits - 1, doc, i, h).acc;
+#pragma unroll
+            for (uint32_t c = 0; c < 2; ++c)
+                part[s][c] = l + 64 * c < a.dim ? reinterpret_cast<const gfloat_t*>(at)[l + 64 * c] : 0.0f;
+        }
+    };
+    const v2f_t stats = *reinterpret_cast<const MEZO_GLOBAL v2f_t*>(
+        partial_row(a, l < a.splits ? l : a.splits - 1, doc, i, h).stats);
+    fetch(0, a.splits);
     const Document d = read_document(a, doc);
     if (i >= d.nq) return;
     const int limit0 = visible(a, d, i);
@@ -1087,9 +1113,8 @@ __global__ void __launch_bounds__(256) attention_join_kernel(Args a)
     const uint32_t most = (limit + a.chunk - 1) / a.chunk, splits = most < a.splits ? most : a.splits;
     float m = -__builtin_inff(), sum = 0.0f;
     if (l < splits) {
-        const v2f_t s = *reinterpret_cast<const MEZO_GLOBAL v2f_t*>(partial_row(a, l, doc, i, h).stats);
-        m = s.x;
-        sum = s.y;
+        m = stats.x;
+        sum = stats.y;
     }
     float top = m;
 #pragma unroll
@@ -1103,16 +1128,8 @@ __global__ void __launch_bounds__(256) attention_join_kernel(Args a)
     // (at most 1 in all: the accumulator does not overflow)
     weight *= (sum == 0.0f ? 0.0f : 1.0f / sum) * (part_sum < 0.0f ? -part_sum : 1.0f);
     float acc[2] = {0.0f, 0.0f};
-    constexpr uint32_t kAhead = 8;  // loads in flight
     for (uint32_t s0 = 0; s0 < splits; s0 += kAhead) {
-        float part[kAhead][2];
-#pragma unroll
-        for (uint32_t s = 0; s < kAhead; ++s) {
-            const uint64_t at = partial_row(a, s0 + s < splits ? s0 + s : splits - 1, doc, i, h).acc;
-#pragma unroll
-            for (uint32_t c = 0; c < 2; ++c)
-                part[s][c] = l + 64 * c < a.dim ? reinterpret_cast<const gfloat_t*>(at)[l + 64 * c] : 0.0f;
-        }
+        if (s0) fetch(s0, splits);
 #pragma unroll
         for (uint32_t s = 0; s < kAhead; ++s) {
             if (s0 + s >= splits) break;
