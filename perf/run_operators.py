@@ -1,12 +1,13 @@
-"""Runs cases of the forward pass's operators for a profiler, and summarises what
-it wrote.
+"""Runs cases of the forward pass's operators, or of those of generation, for a
+profiler, and summarises what it wrote.
 
-    python3 perf/run_operators.py run CASE [PASSES]     # under rocprofv3, one case a run
-    python3 perf/run_operators.py commands OUT          # the commands of all cases, runs into OUT/<case>/<what>
-    python3 perf/run_operators.py summary OUT           # the tables, from those runs
+    python3 perf/run_operators.py run CASE [PASSES]          # under rocprofv3, one case a run
+    python3 perf/run_operators.py commands OUT [generation]  # the commands of all cases, runs into OUT/<case>/<what>
+    python3 perf/run_operators.py summary OUT [generation]   # the tables, from those runs
 
-CASE is a listed case of perf/operators.py or one of FORMS below: forms of the
-operators with code of their own that no listed case reaches.
+CASE is a listed case of perf/operators.py or perf/more_operators.py (those of
+generation), or one of FORMS or MORE_FORMS below: forms of the operators with code of
+their own that no listed case reaches.
 """
 from __future__ import annotations
 
@@ -17,7 +18,7 @@ import os
 import sys
 
 sys.path.insert(0, os.path.join(os.path.dirname(os.path.abspath(__file__)), ".."))
-from perf import operators  # noqa: E402
+from perf import more_operators, operators  # noqa: E402
 
 _ATTEND = {"op": "attend", "dtype": "bf16", "docs": 1, "lo": 8192, "hi": 8192, "new": 0, "capacity": 0, "heads": 32,
            "kv_heads": 32, "dim": 128, "prefix": False, "softcap": 0.0, "bias": False, "lens": 5}
@@ -47,6 +48,29 @@ FORMS = [
      "name": "linear_128_bf16"},
 ]
 
+_PAGED = {"op": "attend", "dtype": "bf16", "docs": 4, "lo": 600, "hi": 8192, "new": 1000, "tree": False, "page": 32,
+          "heads": 32, "kv_heads": 32, "dim": 128, "prefix": False, "softcap": 0.0, "bias": False, "lens": 6}
+_PRODUCT = {"op": "product", "dtype": "bf16", "out": "bf16", "m": 1, "k": 4096, "n": 16384, "pad": 0}
+
+MORE_FORMS = [
+    # full precision: a tree, and single tokens over long caches
+    {**_PAGED, "name": "trees_128_f32", "dtype": "f32", "docs": 8, "lo": 500, "new": 61, "tree": True, "kv_heads": 8,
+     "lens": 5},
+    {**_PAGED, "name": "tokens_128_f32", "dtype": "f32", "docs": 12, "lo": 500, "hi": 16384, "new": 1, "page": 16,
+     "kv_heads": 8, "lens": 2},
+    # a chunk with capped scores; small pages
+    {**_PAGED, "name": "chunks_capped_128_bf16", "softcap": 30.0},
+    {**_PAGED, "name": "chunks_page8_128_bf16", "page": 8},
+    # few activations: full precision, a vocabulary's rows, a batch of 24 and of 64; a few hundred
+    {**_PRODUCT, "name": "product_1_f32", "dtype": "f32", "out": "f32"},
+    {**_PRODUCT, "name": "product_vocabulary_bf16", "n": 50272},
+    {**_PRODUCT, "name": "product_64_bf16", "m": 64},
+    {**_PRODUCT, "name": "product_192_bf16", "m": 192},
+    # full precision on whole blocks; tiles of 128
+    {**_PRODUCT, "name": "product_2048_f32", "dtype": "f32", "out": "f32", "m": 2048, "n": 4096},
+    {**_PRODUCT, "name": "product_2048_bf16", "m": 2048, "n": 4096},
+]
+
 COUNTERS = {
     "fetch": "FETCH_SIZE",
     "write": "WRITE_SIZE",
@@ -55,25 +79,27 @@ COUNTERS = {
 }
 
 
-def cases():
-    return {c["name"]: c for c in operators.listed() + FORMS}
+def cases(generation=False):
+    return {c["name"]: c for c in (more_operators.listed() + MORE_FORMS if generation else operators.listed() + FORMS)}
 
 
 def run(name, passes):
     """`passes` passes over three states in turn, after one over each."""
     import torch
-    operators.own = True
-    states = [operators.prepare(cases()[name], seed) for seed in range(3)]
+    generation = name not in cases()
+    module = more_operators if generation else operators
+    module.own = True
+    states = [module.prepare(cases(generation)[name], seed) for seed in range(3)]
     for s in states:
-        operators.run(s)
+        module.run(s)
     torch.cuda.synchronize()
     for i in range(passes):
-        operators.run(states[i % 3])
+        module.run(states[i % 3])
     torch.cuda.synchronize()
 
 
-def commands(out):
-    for name in cases():
+def commands(out, generation=False):
+    for name in cases(generation):
         print(f"rocprofv3 --kernel-trace --stats -f csv -d {out}/{name}/trace -o p -- "
               f"python3 perf/run_operators.py run {name} 30")
         for what, counters in COUNTERS.items():
@@ -88,7 +114,9 @@ def _rows(out, name, what, file):
 
 
 def _short(kernel):
-    return kernel.replace("(mezo::Mode)", "").split("(mezo::")[0].split("mezo::")[1]
+    for long, short in (("(mezo::Mode)", ""), (", mezo::AttentionArgs", ""), (", mezo::PagedArgs", ", pages")):
+        kernel = kernel.replace(long, short)
+    return kernel.split("(mezo::")[0].split("mezo::")[1]
 
 
 def _counters(out, name):
@@ -99,13 +127,13 @@ def _counters(out, name):
     return {k: {c: sum(v) / len(v) for c, v in d.items()} for k, d in sums.items()}
 
 
-def summary(out):
+def summary(out, generation=False):
     """One line a case and kernel, averages over its dispatches (of all states)."""
     from paper_2306_10015_amd import profile_summary
     print("| case | kernel | µs (min) | read MB | written MB | VALU % | matrix % | CU busy % | LDS conflicts "
           "| VALU instr a unit |")
     print("|---|---|---|---|---|---|---|---|---|---|")
-    for name, case in cases().items():
+    for name, case in cases(generation).items():
         counted = _counters(out, name)
         trace = sorted(_rows(out, name, "trace", "p_kernel_stats.csv"), key=lambda r: -float(r["AverageNs"]))
         for r in trace:
@@ -123,15 +151,20 @@ def summary(out):
                          f"{64 * c['SQ_INSTS_VALU'] / unit:.1f}" if unit else ""]
             print("| " + " | ".join(line + [""] * (10 - len(line))) + " |")
     print()
-    for unit in ("attention.hip", "f8.hip", "token_loss.hip"):
+    for unit in (("paged_attention.hip", "cache_append.hip", "nf4_linear.hip") if generation
+                 else ("attention.hip", "f8.hip", "token_loss.hip")):
         print(f"Sources of `{unit}` ({', '.join(f'`{os.path.basename(s)}`' for s in profile_summary.unit_sources(unit))}) "
               f"sha256: `{profile_summary.source_hash(unit)}`  ")
 
 
 def units(case, kernel):
-    """What a case's kernel works through: scores that count, values quantized, logits."""
+    """What a case's kernel works through: scores that count, values quantized, logits,
+    weights decoded."""
     if kernel.startswith("attention_kernel"):
-        return operators.work(case)["flops"] // (4 * case["dim"])
+        module = more_operators if "page" in case else operators
+        return module.work(case)["flops"] // (4 * case["dim"])
+    if kernel.startswith(("nf4_thin", "nf4_expand")):
+        return case["n"] * case["k"]
     if kernel.startswith("loss_rows"):
         return (case["t"] - case["skip"]) * case["v"]
     if kernel.startswith("f8_quantize") and not case["fresh"]:
@@ -143,4 +176,4 @@ if __name__ == "__main__":
     if sys.argv[1] == "run":
         run(sys.argv[2], int(sys.argv[3]) if len(sys.argv) > 3 else 30)
     else:
-        {"commands": commands, "summary": summary}[sys.argv[1]](sys.argv[2])
+        {"commands": commands, "summary": summary}[sys.argv[1]](sys.argv[2], "generation" in sys.argv[3:])
