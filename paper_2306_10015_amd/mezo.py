@@ -481,7 +481,7 @@ def nf4_linear(x, w: NF4Tensor, dtype=None, out=None, stream=None):
     n, x_code = w.numel() // k, _dtype_code(x)
     with _on(x.device, stream):
         if out is None:
-            out = torch.empty(m, n, dtype=dtype or x.dtype, device=x.device)
+            out = x.new_empty((m, n), dtype=dtype or x.dtype)
             ldc = n
         else:
             if dtype is not None and out.dtype != dtype:
@@ -639,13 +639,15 @@ class PagedCache:
             raise ValueError("pages: a contiguous CUDA tensor [documents, entries] or [entries]")
         _same_device(k, v, pages)
         self.k, self.v, self.pages, self.n_pages, self.rows = k, v, pages, n_pages, rows
-        self._k, self._v = self._strides(k, "k"), self._strides(v, "v")
+        k_strides, v_strides = k.stride(), v.stride()
+        self._k = self._strides(shape, k_strides, "k")
+        self._v = self._k if v_strides == k_strides else self._strides(shape, v_strides, "v")
 
     @staticmethod
-    def _strides(t, what):
+    def _strides(shape, strides, what):
         """Elements from one page, one row and one head to the next."""
-        n_pages, rows, heads, dim = t.shape
-        sp, sr, sh, sd = t.stride()
+        n_pages, rows, heads, dim = shape
+        sp, sr, sh, sd = strides
         if dim > 1 and sd != 1:
             raise ValueError(f"{what}: the elements of a head must be contiguous")
         if min(sp, sr, sh) < 0:
@@ -738,7 +740,7 @@ def cache_append(k, v, cache: PagedCache, docs: Documents, q=None, freqs=None, p
         if q is not None:
             if out is None:
                 bare = docs.covered is not None and docs.covered < tk
-                out = (torch.zeros if bare else torch.empty)(q.shape, dtype=q.dtype, device=q.device)
+                out = (torch.zeros_like if bare else torch.empty_like)(q, memory_format=torch.contiguous_format)
                 o_token, o_head = heads * dim, dim
             else:
                 if out.dtype != q.dtype or out.shape != q.shape:
@@ -786,14 +788,14 @@ def paged_attention(q, cache: PagedCache, docs: Documents, tree=None, causal: bo
     with _on(q.device, stream):
         bare = docs.covered is not None and docs.covered < tq  # some tokens are of no document
         if out is None:
-            out = (torch.zeros if bare else torch.empty)((tq, heads, dim), dtype=q.dtype, device=q.device)
+            out = (torch.zeros_like if bare else torch.empty_like)(q, memory_format=torch.contiguous_format)
             o_token, o_head = heads * dim, dim
         else:
             if out.dtype != q.dtype or out.shape != q.shape:
                 raise ValueError("out must be like q")
             _, _, _, o_token, o_head = _heads_of(out, "out")
         _same_device(q, cache.k, out, slopes, tree, docs.table)
-        lse = torch.empty((tq, heads), dtype=torch.float32, device=q.device) if return_lse else None
+        lse = q.new_empty((tq, heads), dtype=torch.float32) if return_lse else None
         if bare and return_lse:
             lse.fill_(-math.inf)
         (k_page, k_row, k_head), (v_page, v_row, v_head) = cache._k, cache._v
