@@ -361,3 +361,19 @@ def test_no_backward(mz):
     for t in (out, lse):
         with pytest.raises(RuntimeError, match="no backward pass"):
             t.float().sum().backward(retain_graph=True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("docs", [2, 63, 64, 65])
+def test_order_of_documents(mz, docs, dtype):
+    """Of up to 64 documents the longest goes first: equal lengths, none at all, and queries of
+    no document's order; a table that says more keys than there are."""
+    r = np.random.default_rng(docs)
+    k_lens = [int(n) for n in r.choice([0, 1, 40, 40, 129, 250], docs)]
+    q_lens = [int(n) for n in r.choice([0, 1, 33, 70, 150], docs)]
+    q_lens[-1], k_lens[-1] = 150, 250
+    c = Case(mz, q_lens, k_lens, heads=3, kv_heads=3, dtype=dtype)
+    out, lse = c.check()
+    c.docs.table[:-1, 3][c.docs.table[:-1, 1] == 0] = 1 << 62
+    again, lse_again = mz.paged_attention(c.q, c.cache, c.docs, return_lse=True)
+    assert torch.equal(out, again) and torch.equal(lse, lse_again)
