@@ -71,6 +71,7 @@ typedef float v16f_t __attribute__((ext_vector_type(16)));
 typedef float v4f_t __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf_t __attribute__((ext_vector_type(8)));
 typedef __bf16 v4bf_t __attribute__((ext_vector_type(4)));
+typedef __bf16 v2bf_t __attribute__((ext_vector_type(2)));
 typedef short v4s_t __attribute__((ext_vector_type(4)));
 typedef float v2f_t __attribute__((ext_vector_type(2)));
 
@@ -1119,14 +1120,13 @@ __global__ void __launch_bounds__(256) attention_join_kernel(Args a)
     // Everything is under way at once: the document's row, which says how many of the splits
     // there are, and of as many as the call has the statistics and the first accumulators.
     constexpr uint32_t kAhead = 8;  // loads in flight
-    float part[kAhead][2];
+    v2f_t part[kAhead];
     auto fetch = [&](uint32_t s0, uint32_t splits) {
+        if (2 * l >= a.dim) return;
 #pragma unroll
         for (uint32_t s = 0; s < kAhead; ++s) {
-            const uint64_t at = partial_row(a, s0 + s < splits ? s0 + s : splits - 1, doc, i, h).acc;
-#pragma unroll
-            for (uint32_t c = 0; c < 2; ++c)
-                part[s][c] = l + 64 * c < a.dim ? reinterpret_cast<const gfloat_t*>(at)[l + 64 * c] : 0.0f;
+            if (s0 + s >= splits) break;
+            part[s] = reinterpret_cast<const MEZO_GLOBAL v2f_t*>(partial_row(a, s0 + s, doc, i, h).acc)[l];
         }
     };
     const v2f_t stats = *reinterpret_cast<const MEZO_GLOBAL v2f_t*>(
@@ -1153,7 +1153,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(Args a)
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
     // (at most 1 in all: the accumulator does not overflow)
     weight *= (sum == 0.0f ? 0.0f : 1.0f / sum) * (part_sum < 0.0f ? -part_sum : 1.0f);
-    float acc[2] = {0.0f, 0.0f};
+    v2f_t acc = {0.0f, 0.0f};
     for (uint32_t s0 = 0; s0 < splits; s0 += kAhead) {
         if (s0) fetch(s0, splits);
 #pragma unroll
@@ -1164,9 +1164,13 @@ __global__ void __launch_bounds__(256) attention_join_kernel(Args a)
             for (uint32_t c = 0; c < 2; ++c) acc[c] += part[s][c] * w;
         }
     }
-    const uint64_t token = d.q_first + uint64_t(i);
-    for (uint32_t c = 0; c < 2; ++c)
-        if (l + 64 * c < a.dim) store_element<kF>(a.out + token * a.o_token + h * a.o_head, l + 64 * c, acc[c]);
+    const uint64_t token = d.q_first + uint64_t(i), o = a.out + token * a.o_token + h * a.o_head;
+    if (2 * l < a.dim) {
+        if constexpr (kF)
+            reinterpret_cast<MEZO_GLOBAL v2f_t*>(o)[l] = acc;
+        else
+            reinterpret_cast<MEZO_GLOBAL v2bf_t*>(o)[l] = __builtin_convertvector(acc, v2bf_t);
+    }
     if (l == 0) store_lse(a, token, h, top, logf(sum));
 }
 
