@@ -83,10 +83,9 @@ def cases(generation=False):
     return {c["name"]: c for c in (more_operators.listed() + MORE_FORMS if generation else operators.listed() + FORMS)}
 
 
-def run(name, passes):
+def run(name, passes, generation=False):
     """`passes` passes over three states in turn, after one over each."""
     import torch
-    generation = name not in cases()
     module = more_operators if generation else operators
     module.own = True
     states = [module.prepare(cases(generation)[name], seed) for seed in range(3)]
@@ -99,12 +98,13 @@ def run(name, passes):
 
 
 def commands(out, generation=False):
+    kind = " generation" if generation else ""
     for name in cases(generation):
         print(f"rocprofv3 --kernel-trace --stats -f csv -d {out}/{name}/trace -o p -- "
-              f"python3 perf/run_operators.py run {name} 30")
+              f"python3 perf/run_operators.py run {name} 30{kind}")
         for what, counters in COUNTERS.items():
             print(f"rocprofv3 --pmc {counters} --kernel-trace -f csv -d {out}/{name}/{what} -o p -- "
-                  f"python3 perf/run_operators.py run {name} 2")
+                  f"python3 perf/run_operators.py run {name} 2{kind}")
 
 
 def _rows(out, name, what, file):
@@ -174,6 +174,6 @@ def units(case, kernel):
 
 if __name__ == "__main__":
     if sys.argv[1] == "run":
-        run(sys.argv[2], int(sys.argv[3]) if len(sys.argv) > 3 else 30)
+        run(sys.argv[2], int(sys.argv[3]) if len(sys.argv) > 3 else 30, "generation" in sys.argv[4:])
     else:
         {"commands": commands, "summary": summary}[sys.argv[1]](sys.argv[2], "generation" in sys.argv[3:])
