@@ -1,5 +1,6 @@
-// attention.hpp — the kernels of attention.hip and paged_attention.hip: attention of a packed batch of documents, the middle of a
-// decoder layer's forward pass. For query i of a document with nq queries and nk
+// attention.hpp — the kernels of attention.hip and paged_attention.hip: attention of a
+// packed batch of documents, the middle of a decoder layer's forward pass, over keys
+// that lie together or in the pages of a cache. For query i of a document with nq queries and nk
 // keys (its queries are the last of its tokens, pos = i + nk - nq), per head:
 //   s_j = scale q_i . k_j,  s_j = cap tanh(s_j / cap) if capped,
 //   s_j = s_j - slope |pos - j| if biased,
@@ -48,9 +49,13 @@
 // by 2^16 before the split would do as well, for 2 to 4% of the time of all calls.
 //
 // Keys of a paged cache (PagedArgs): key j of a document is row j % R of the page that entry
-// j / R of its list names, R a power of two from 8 on. A load of a wave is at most 8 keys, so
-// it stays within a page: its page's entry is one scalar load, the rest of its address scalar
-// arithmetic, and the loads, stages and sums are those of contiguous keys.
+// j / R of its list names, R a power of two from 8 on. A wave loads a stage's keys in groups
+// of 16 (of 8 where pages have 8 rows), each within a page: its address is one scalar load of
+// the page's entry, a stage ahead, and scalar arithmetic; the loads, stages and sums are those
+// of contiguous keys. bf16, 32 heads on 8 of 128: 24 tokens over 500 to 16384 keys in pages of
+// 16 take 163 us, 5.3 TB/s (the same keys in one piece 158), bound by memory; 8 trees of 61
+// tokens over 500 to 8192 keys 70 and 10 for the join, the vector units busy for 35% of it and
+// the matrix units for 33.
 //
 // A tree of drafted tokens (PagedArgs with `tree`) is the one mask that is not "the first so
 // many keys": query i sees the context, the first nk - nq keys, and of the document's own new
@@ -636,7 +641,9 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys, !k
     // Documents of a cache differ most in their keys. Where they are not split, the workgroups
     // go by their documents' keys, most first: the last to start are short (4 chunks of 1000
     // tokens over 600 to 8192 keys, 32 heads of 128, 418 -> 376 us; 12 chunks of 200, 306 ->
-    // 252; 20 trees of 61 tokens, whose workgroups all run at once, 188 -> 195).
+    // 252; 20 trees of 61 tokens, whose workgroups all run at once, 188 -> 195). Cutting
+    // documents into equal parts by their table instead gains nothing: 8 trees 80 us with 512
+    // workgroups wanted, 92 to 150 with other numbers; 24 tokens 165 -> 171.
     if constexpr (kPaged && !kKeys) {
         if (a.splits == 1 && a.docs > 1 && a.docs <= 64 && uint64_t(gridDim.x) * gridDim.y <= 0xFFFFFFFFu) {
             const uint32_t group = (blockIdx.y * gridDim.x + blockIdx.x) / a.kv_heads;

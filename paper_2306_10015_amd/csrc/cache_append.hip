@@ -15,7 +15,9 @@
 // (16 bytes where half of `rot` is a multiple of them, which the usual sizes are; else the
 // largest power of two that divides it): a vector of a pair's first columns and the one of
 // their partners, or a vector of whole pairs. Neighbouring lanes take neighbouring vectors of
-// a head, then heads, then tokens.
+// a head, then heads, then tokens. Packed prompts on the 6.7B shapes, 842 MB read and written:
+// 151 us, 5.6 TB/s (a copy of 1 GiB 5.2); 24 tokens of 32 heads on 8 of 128 take 8 us, one 5:
+// the chain from the table to the list to the page's row.
 #include <type_traits>
 
 #include "cache_append_launch.hpp"
