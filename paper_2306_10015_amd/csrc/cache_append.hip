@@ -146,8 +146,9 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(AppendArgs
     __shared__ float2 turn[kMostAngles];  // (cos, sin) of [token, pair]
     __shared__ Slot slots[kMostTile];
 
-    const uint32_t tiles = (a.max_q + a.tile - 1) / a.tile, work = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
-    const uint32_t doc = work / tiles, first = (work % tiles) * a.tile;
+    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x, work = id / a.parts, part = id % a.parts;
+    const uint32_t tiles = (a.max_q + a.tile - 1) / a.tile, doc = work / tiles, first = (work % tiles) * a.tile;
+    if (doc >= a.docs) return;
     // the document's row of the table, cut to the arrays: no table makes the kernel leave them
     const MEZO_GLOBAL int64_t* row = reinterpret_cast<const MEZO_GLOBAL int64_t*>(a.table) + uint64_t(doc) * 5;
     auto within = [](int64_t x, uint64_t top) { return x < 0 ? 0 : (uint64_t(x) > top ? top : uint64_t(x)); };
@@ -296,7 +297,11 @@ hipError_t launch(AppendArgs& a, hipStream_t stream)
         return reinterpret_cast<const void*>(cache_append_kernel<kF, kW, false, kStream>);
     };
     const void* f = stream_out ? pick(std::integral_constant<bool, true>{}) : pick(std::integral_constant<bool, false>{});
-    return hipLaunchKernel(f, dim3(uint32_t(groups * a.parts)), dim3(kAppendThreads), params, 0, stream);
+    // (a dimension of the grid holds less than 2^32 lanes)
+    constexpr uint64_t kMostGroups = 1u << 22;
+    const uint64_t all = groups * a.parts, across = all < kMostGroups ? all : kMostGroups;
+    return hipLaunchKernel(f, dim3(uint32_t(across), uint32_t((all + across - 1) / across)), dim3(kAppendThreads), params, 0,
+                           stream);
 }
 
 hipError_t launch_cache_append(const AppendArgs& args, hipStream_t stream)

@@ -253,3 +253,23 @@ def test_no_backward(mz):
             t.float().sum().backward(retain_graph=True)
     with torch.no_grad():
         assert not mz.cache_append(k, c.v, Case(mz, [2], [2]).cache, c.docs, q=q).requires_grad
+
+
+def test_more_workgroups_than_a_row_of_a_grid(mz):
+    """A padded batch: 2^16 documents of up to 512 tokens, nearly all of them without any."""
+    heads, dim, rows, tokens = 64, 128, 16, 512
+    docs = 1 << 16
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn(tokens, heads, dim, generator=g).cuda() for _ in range(3))
+    table = torch.zeros(docs, 5, dtype=torch.int64)
+    table[0] = torch.tensor([0, 5, 0, 5, 0])
+    table[-1] = torch.tensor([5, 507, 1, 507, 0])
+    pages = torch.randperm(33, generator=g).int()
+    cache = mz.PagedCache(torch.zeros(33, rows, heads, dim, device="cuda"), torch.zeros(33, rows, heads, dim, device="cuda"),
+                          pages.cuda())
+    out = mz.cache_append(k, v, cache, mz.Documents(table.cuda(), tokens, tokens), q=q)
+    assert torch.equal(out, q)
+    for new, where in ((k, cache.k), (v, cache.v)):
+        flat = where[pages.long().cuda()].reshape(33 * rows, heads, dim)
+        assert torch.equal(flat[:5], new[:5]) and torch.equal(flat[rows:rows + 507], new[5:])
+        assert not flat[5:rows].any() and not flat[rows + 507:].any()
