@@ -573,8 +573,8 @@ MEZO_API int mezo_paged_attention(const mezo_attention_t* a, const mezo_pages_t*
  * summed in fp32 and the sum is rounded once; for MEZO_F32 each product is within 2^-22 of
  * itself (v[code] * absmax may then stand unrounded), of values of x below 2^-100 and in results below
  * 2^-110 within as much of 2^-100 and 2^-110. A row of x that holds NaN or an infinity, and a
- * block whose absmax is one, give results that are not finite. 1 <= m, n <=
- * MEZO_F8_MAX_ROWS, 1 <= k <= MEZO_F8_MAX_COLS, m * k, n * k and m * n <= MEZO_MAX_NUMEL,
+ * block whose absmax is one, give results that are not finite. m, n >= 1, 1 <= k <=
+ * MEZO_F8_MAX_COLS, m * n <= MEZO_MAX_NUMEL, m and n times k rounded up to 64 too,
  * ldx >= k and ldc >= n where m > 1, codes and absmax 16-byte aligned (MEZO_EINVAL); c and the workspace
  * must not overlap anything else (MEZO_EOVERLAP). */
 MEZO_API uint64_t mezo_nf4_linear_workspace(uint64_t m, uint64_t n, uint64_t k, uint32_t x_dtype, uint32_t c_dtype);

@@ -313,8 +313,10 @@ int paged_attention(const mezo_attention_t* pa, const mezo_pages_t* pc, void* wo
 
 bool nf4_sizes(uint64_t m, uint64_t n, uint64_t k)
 {
-    return m >= 1 && n >= 1 && k >= 1 && m <= MEZO_F8_MAX_ROWS && n <= MEZO_F8_MAX_ROWS && k <= MEZO_F8_MAX_COLS &&
-           n <= MEZO_MAX_NUMEL / k && m <= MEZO_MAX_NUMEL / k && m <= MEZO_MAX_NUMEL / n;
+    // (rows as they are laid out, so that no launch is larger than a grid)
+    const uint64_t columns = k <= MEZO_F8_MAX_COLS ? nf4_columns(k) : 0;
+    return m >= 1 && n >= 1 && k >= 1 && columns && n <= MEZO_MAX_NUMEL / columns && m <= MEZO_MAX_NUMEL / columns &&
+           m <= MEZO_MAX_NUMEL / n;
 }
 
 int nf4_linear(const void* x, uint32_t x_dtype, uint64_t ldx, const void* codes, const float* absmax, uint64_t m,

@@ -43,7 +43,8 @@ inline NF4Cut cut_nf4(uint64_t m, uint64_t n, uint64_t k, bool wide_x)
         // rounds over the CUs; one takes 1.6 times as long as with 64 (1 x 50272 x 4096 36.6 us
         // in two rounds of 128, 43.7 in four of 64; 1 x 16384 x 4096 18.1 and 12.6 in one).
         const uint64_t rounds64 = ((n + 63) / 64 + 255) / 256, rounds128 = ((n + 127) / 128 + 255) / 256;
-        const bool wide_group = wide_x ? m > 16 : m <= 32 && 8 * rounds128 < 5 * rounds64;
+        // (and past 2^27 rows, of which 64 a workgroup are more lanes than a grid holds)
+        const bool wide_group = (wide_x ? m > 16 : m <= 32 && 8 * rounds128 < 5 * rounds64) || n > 1ull << 27;
         const uint64_t rows = m <= 4 && n <= 4096 ? 16 : (wide_group ? 128 : 64);
         // k split where the rows leave CUs without work, in parts of 16 blocks at least
         const uint64_t groups = (n + rows - 1) / rows * (wide_x ? (m + 15) / 16 : (m + 63) / 64);

@@ -205,6 +205,16 @@ hipError_t launch_nf4_linear(const NF4LinearArgs& a, hipStream_t)
         CHECK((m * (columns / 8) + 255) / 256 < (u128(1) << 31) && (u128(cut.slab) * (columns / 8) + 255) / 256 < (u128(1) << 31));
         CHECK(((m + 63) / 64) * ((u128(cut.slab) + 63) / 64) < (u128(1) << 31));
     }
+    // lanes of a launch's first dimension, 32 bits
+    const u128 most = u128(1) << 32, lanes = m * (columns / 8) + 255;
+    CHECK(lanes < most);
+    if (cut.tile == kThin) {
+        CHECK((n + cut.thin_rows - 1) / cut.thin_rows * 1024 < most && (m + 3) / 4 <= 65535);
+    } else {
+        const u128 size = cut.tile == k256x256 ? 256 : (cut.tile == k128x128 ? 128 : 64);
+        CHECK((m + size - 1) / size * ((u128(cut.slab) + size - 1) / size) * (size == 256 ? 512 : 256) < most);
+    }
+    if (cut.splits > 1) CHECK(m * (cut.tile == kThin ? n : u128(cut.slab)) + 255 < most);
     CHECK(u128(s.bytes) <= g_workspace.to - g_workspace.from);
     return hipSuccess;
 }

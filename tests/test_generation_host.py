@@ -191,3 +191,13 @@ def test_linear_workspace():
         assert L.mezo_nf4_linear_workspace(*bad) == 0
     # a matrix of any size is expanded a slab at a time
     assert L.mezo_nf4_linear_workspace(100, 50272, 16384, mezo.BF16, mezo.BF16) < 300 << 20
+
+
+def test_linear_of_more_rows_than_a_grid():
+    """Rows are laid out in whole blocks of 64 columns: what fits in MAX_NUMEL so, and no more."""
+    size = L.mezo_nf4_linear_workspace
+    for m, n, k in ((1 << 30, 1, 16), ((1 << 28) + 1, 1, 1), (1, 1 << 30, 16), (4, (1 << 28) + 1, 64)):
+        assert size(m, n, k, mezo.BF16, mezo.BF16) == 0
+        assert linear(m=m, n=n, k=k, ldx=k, ldc=n, size=1 << 40) == mezo.EINVAL
+    for m, n, k in ((1 << 28, 1, 1), (1 << 28, 64, 64), (255, (1 << 26) - 1, 63)):
+        assert size(m, n, k, mezo.F32, mezo.BF16) > 0
