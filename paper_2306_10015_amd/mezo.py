@@ -637,7 +637,8 @@ class PagedCache:
             raise TypeError(f"pages must be int32, got {pages.dtype}")
         if pages.dim() not in (1, 2) or not pages.is_cuda or not pages.is_contiguous():
             raise ValueError("pages: a contiguous CUDA tensor [documents, entries] or [entries]")
-        _same_device(k, v, pages)
+        if _DEVICES != 1:  # (with one they are on it)
+            _same_device(k, v, pages)
         self.k, self.v, self.pages, self.n_pages, self.rows = k, v, pages, n_pages, rows
         k_strides, v_strides = k.stride(), v.stride()
         self._k = self._strides(shape, k_strides, "k")
@@ -650,7 +651,7 @@ class PagedCache:
         sp, sr, sh, sd = strides
         if dim > 1 and sd != 1:
             raise ValueError(f"{what}: the elements of a head must be contiguous")
-        if min(sp, sr, sh) < 0:
+        if sp < 0 or sr < 0 or sh < 0:
             raise ValueError(f"{what}: negative strides")
         sh = sh if heads > 1 else dim
         return sp if n_pages > 1 else rows * sr, sr, sh
@@ -721,9 +722,9 @@ def cache_append(k, v, cache: PagedCache, docs: Documents, q=None, freqs=None, p
         raise TypeError(f"k and v are {k.dtype} and {v.dtype}, the cache {cache.k.dtype}")
     rot = 0
     if freqs is not None:
-        if freqs.dtype != torch.float32 or freqs.dim() != 1 or not freqs.is_contiguous() or 2 * len(freqs) > dim:
+        rot = 2 * freqs.numel()  # (len of a tensor takes 0.4 us)
+        if freqs.dtype != torch.float32 or freqs.dim() != 1 or not freqs.is_contiguous() or rot > dim:
             raise ValueError(f"freqs: a contiguous float32 tensor of at most {dim // 2}")
-        rot = 2 * len(freqs)
     if positions is not None and (positions.dtype != torch.int64 or positions.shape != (tk,)
                                   or not positions.is_contiguous()):
         raise ValueError(f"positions: a contiguous int64 tensor of {tk}")
@@ -746,7 +747,9 @@ def cache_append(k, v, cache: PagedCache, docs: Documents, q=None, freqs=None, p
                 if out.dtype != q.dtype or out.shape != q.shape:
                     raise ValueError("out must be like q")
                 _, _, _, o_token, o_head = _heads_of(out, "out")
-        _same_device(k, v, q, out, cache.k, freqs, positions, docs.table)
+        if _DEVICES != 1:  # (with one, heads, caches and tables are on it)
+            _same_device(k, v, q, out, cache.k, docs.table)
+        _same_device(k, freqs, positions)
         a = _APPEND.pack(_ptr(q) or 0, k.data_ptr(), v.data_ptr(), _ptr(out) or 0, cache.k.data_ptr(),
                          cache.v.data_ptr(), docs.table.data_ptr(), cache.pages.data_ptr(), _ptr(freqs) or 0,
                          _ptr(positions) or 0, tk, cache.n_pages, cache.pages.numel(), docs.max_q, q_token, q_head,
@@ -794,7 +797,9 @@ def paged_attention(q, cache: PagedCache, docs: Documents, tree=None, causal: bo
             if out.dtype != q.dtype or out.shape != q.shape:
                 raise ValueError("out must be like q")
             _, _, _, o_token, o_head = _heads_of(out, "out")
-        _same_device(q, cache.k, out, slopes, tree, docs.table)
+        if _DEVICES != 1:
+            _same_device(q, cache.k, out, docs.table)
+        _same_device(q, slopes, tree)
         lse = q.new_empty((tq, heads), dtype=torch.float32) if return_lse else None
         if bare and return_lse:
             lse.fill_(-math.inf)
