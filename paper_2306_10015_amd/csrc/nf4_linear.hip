@@ -12,6 +12,7 @@
 // front of the matrix instructions that use them (nf4_thin_kernel, below). The lookups bound
 // it, and the loads of the codes under them: one row by 16384 x 4096 weights 11 us (37 MB, 3.4
 // TB/s), 24 rows by 4096 x 16384 17, 64 rows by 16384 x 4096 20.
+// Few rows where k is no multiple of 64: codes go straight into registers (nf4_ragged_kernel).
 // Many rows: a slab of the weights is expanded into the workspace (2 bytes an element, 6 for
 // fp32), and a tiled product reads it. Expanding costs 2.5 bytes an element once, the product
 // 2 m operations: from a few hundred rows on it does not show (8192 x 16384 x 4096: 31 us of
@@ -736,6 +737,167 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
     }
 }
 
+// ---- few rows, and blocks that run over the ends of the weights' -------------------------
+
+// Where k is no multiple of 64 a row begins anywhere in a block, or within a byte. A workgroup
+// takes kRG groups of 16 rows of weights, its waves every kRaggedWaves-th 64 columns of them. A lane
+// has 16 weights next to each other, as above: of its row's three words of codes it shifts out two,
+// by the same shift in every stage, since 64 columns are whole words; the weights before and behind
+// the end of a block are the same ones in every stage too, so that it takes two scales and selects.
+// A code's value comes from the lane that holds it. Codes and scales are read a stage ahead, straight
+// into registers: rows lie on no alignment that loads into LDS could use.
+// What bounds it are those loads, of 16 rows each, and the activations' (1 x 16384 x 4100 bf16 31
+// us, 16 rows 36, 64 rows 58, in fp32 39, 51 and 133; expanded and through tiles 69, 69, 72 and
+// 220, 221, 250). Values by pairs out of LDS took as long; 64 weights a lane 28 us for one row and
+// 37, 89 for 16 and 64; groups of 16 rows alone 33, 41 and 83.
+constexpr uint32_t kRaggedWaves = 8;
+
+struct NF4RaggedArgs {
+    uint64_t x, x_plane, x_row;  // laid out in planes, zeros behind column k
+    uint64_t codes, absmax, c, ldc, partial;
+    uint64_t k;
+    uint32_t m, n, splits;
+};
+
+template <bool kF, uint32_t kRG, uint32_t kFM, bool kWideOut>
+__global__ void __launch_bounds__(kRaggedWaves * 64) nf4_ragged_kernel(NF4RaggedArgs a)
+{
+    __shared__ v4f_t room[kRaggedWaves][kRG * kFM][64];
+    const uint32_t l = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t fr = l & 15u, fg = l >> 4, n0 = blockIdx.x * kRG * 16, m0 = blockIdx.z * kFM * 16;
+    uint32_t table = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kNF4Codes; ++i) table = fr == i ? __builtin_bit_cast(uint32_t, kNF4Values[i]) : table;
+    const uint32_t stages = uint32_t((a.k + 63) / 64);
+    const uint32_t s0 = uint32_t(uint64_t(stages) * blockIdx.y / a.splits),
+                   s1 = uint32_t(uint64_t(stages) * (blockIdx.y + 1) / a.splits);
+
+    // this lane's first weights of stage 0, rows past the end: the last one's
+    const uint64_t all = a.n * a.k, words = (all + 1) / 2 / 4, top = (all - 1) / kNF4Block;
+    uint64_t e0[kRG];
+    uint32_t shift[kRG], left[kRG];
+#pragma unroll
+    for (uint32_t g = 0; g < kRG; ++g) {
+        const uint32_t row = n0 + g * 16 + fr;
+        e0[g] = (row < a.n ? row : a.n - 1) * a.k + 16 * fg;
+        shift[g] = uint32_t(e0[g] & 7u) * 4;
+        left[g] = kNF4Block - uint32_t(e0[g] % kNF4Block);
+    }
+    // the stages whose three words are whole words of the codes, by all lanes
+    const uint32_t last_row = n0 + kRG * 16 - 1 < a.n ? n0 + kRG * 16 - 1 : a.n - 1;
+    const uint64_t furthest = (last_row * a.k + 48) / 8 + 3;
+    const uint32_t safe = words < furthest ? 0u : uint32_t((words - furthest) / 8 < stages ? (words - furthest) / 8 + 1 : stages);
+
+    struct Codes {
+        uint32_t w[3];
+        float scale[2];
+    };
+    auto fetch = [&](uint32_t g, uint32_t s) {
+        Codes c;
+        const uint64_t e = e0[g] + uint64_t(s) * 64, b = e / kNF4Block;
+        if (s < safe) {
+#pragma unroll
+            for (uint32_t i = 0; i < 3; ++i) c.w[i] = reinterpret_cast<const gu32_t*>(a.codes)[e / 8 + i];
+        } else {
+            const uint64_t at = e & ~uint64_t(7);
+            c.w[0] = eight_codes(a.codes, at, all);
+            c.w[1] = eight_codes(a.codes, at + 8, all);
+            c.w[2] = eight_codes(a.codes, at + 16, all);
+        }
+        c.scale[0] = reinterpret_cast<const gfloat_t*>(a.absmax)[b < top ? b : top];
+        c.scale[1] = reinterpret_cast<const gfloat_t*>(a.absmax)[left[g] >= 16 || b >= top ? (b < top ? b : top) : b + 1];
+        return c;
+    };
+
+    uint64_t xs[kFM];
+#pragma unroll
+    for (uint32_t f = 0; f < kFM; ++f) {
+        const uint32_t r = m0 + f * 16 + fr;
+        xs[f] = a.x + (r < a.m ? r : a.m - 1) * a.x_row + fg * 32;
+    }
+    constexpr uint32_t kPlanes = kF ? 3 : 1;
+    v4f_t acc[kRG][kFM] = {};
+    Codes next[kRG] = {}, now[kRG];
+    uint32_t s = s0 + wave;
+    if (s < s1)
+#pragma unroll
+        for (uint32_t g = 0; g < kRG; ++g) next[g] = fetch(g, s);
+    for (; s < s1; s += kRaggedWaves) {
+#pragma unroll
+        for (uint32_t g = 0; g < kRG; ++g) now[g] = next[g];
+        v8bf_t x[kFM][2][kPlanes];
+#pragma unroll
+        for (uint32_t f = 0; f < kFM; ++f)
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h)
+#pragma unroll
+                for (uint32_t p = 0; p < kPlanes; ++p)
+                    x[f][h][p] = *reinterpret_cast<const MEZO_GLOBAL v8bf_t*>(xs[f] + p * a.x_plane + uint64_t(s) * 128 + h * 16);
+        if (s + kRaggedWaves < s1)
+#pragma unroll
+            for (uint32_t g = 0; g < kRG; ++g) next[g] = fetch(g, s + kRaggedWaves);
+        const uint64_t column = uint64_t(s) * 64 + 16 * fg;
+        const uint32_t valid = column >= a.k ? 0u : (a.k - column < 16 ? uint32_t(a.k - column) : 16u);
+#pragma unroll
+        for (uint32_t g = 0; g < kRG; ++g) {
+            const uint32_t codes[2] = {__builtin_amdgcn_alignbit(now[g].w[1], now[g].w[0], shift[g]),
+                                       __builtin_amdgcn_alignbit(now[g].w[2], now[g].w[1], shift[g])};
+            float w[16];
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i)
+                w[i] = __uint_as_float(uint32_t(
+                    __builtin_amdgcn_ds_bpermute(int((codes[i / 8] >> (4 * (i % 8)) & 15u) << 2), int(table))));
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) w[i] *= i < left[g] ? now[g].scale[0] : now[g].scale[1];
+            if (s + 1 == stages) {  // (what follows the row is not its own, and may not be finite)
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i) w[i] = i < valid ? w[i] : 0.0f;
+            }
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) {
+                if constexpr (kF) {
+                    const float v[8] = {w[8 * h], w[8 * h + 1], w[8 * h + 2], w[8 * h + 3], w[8 * h + 4], w[8 * h + 5],
+                                        w[8 * h + 6], w[8 * h + 7]};
+                    const Planes p = planes_of(v);
+#pragma unroll
+                    for (uint32_t f = 0; f < kFM; ++f)
+                        acc[g][f] = product(p, Planes{{x[f][h][0], x[f][h][1], x[f][h][2]}}, acc[g][f]);
+                } else {
+                    v8bf_t b;
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) b[i] = static_cast<__bf16>(w[8 * h + i]);
+#pragma unroll
+                    for (uint32_t f = 0; f < kFM; ++f)
+                        acc[g][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, x[f][h][0], acc[g][f], 0, 0, 0);
+                }
+            }
+        }
+    }
+
+    // the waves' sums, joined in their order
+#pragma unroll
+    for (uint32_t t = 0; t < kRG * kFM; ++t) room[wave][t][l] = acc[t / kFM][t % kFM];
+    __syncthreads();
+    NF4MatmulArgs o;
+    o.c = a.c;
+    o.ldc = a.ldc;
+    o.partial = a.partial;
+    o.m = a.m;
+    o.n = a.n;
+    const bool whole = whole_groups<kWideOut>(o);
+    for (uint32_t t = wave; t < kRG * kFM; t += kRaggedWaves) {
+        v4f_t sum = room[0][t][l];
+#pragma unroll
+        for (uint32_t w = 1; w < kRaggedWaves; ++w) sum += room[w][t][l];
+        const uint32_t out = m0 + t % kFM * 16 + fr, column = n0 + t / kFM * 16 + fg * 4;
+        if (out >= a.m || column >= a.n) continue;
+        if (a.splits == 1)
+            store4<kWideOut>(o, whole, out, column, sum);
+        else
+            *reinterpret_cast<MEZO_GLOBAL v4f_t*>(partial_at(o, blockIdx.y, out, column)) = sum;
+    }
+}
+
 // ---- launches ---------------------------------------------------------------------
 
 template <class Args>
@@ -892,9 +1054,63 @@ hipError_t launch_thin(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t st
 }
 
 template <bool kWide, bool kWideOut>
+hipError_t launch_ragged(const NF4LinearArgs& a, const NF4Cut& cut, hipStream_t stream)
+{
+    const uint64_t columns = nf4_columns(a.k), row = columns * 2;
+    LayArgs lay = {};
+    lay.k = a.k;
+    lay.columns = columns;
+    lay.from = a.x;
+    lay.ld = a.ldx;
+    lay.to = a.workspace;
+    lay.plane = a.m * row;
+    lay.rows = a.m;
+    hipError_t e = run(reinterpret_cast<const void*>(nf4_lay_values_kernel<kWide>),
+                       dim3(uint32_t((a.m * (columns / 8) + 255) / 256)), 256, lay, stream);
+    if (e != hipSuccess) return e;
+    NF4RaggedArgs g = {};
+    g.x = a.workspace;
+    g.x_plane = a.m * row;
+    g.x_row = row;
+    g.codes = a.codes;
+    g.absmax = a.absmax;
+    g.c = a.c;
+    g.ldc = a.ldc;
+    g.partial = a.workspace + nf4_space(a.m, a.n, a.k, kWide).partial;
+    g.k = a.k;
+    g.m = uint32_t(a.m);
+    g.n = uint32_t(a.n);
+    g.splits = cut.splits;
+    auto go = [&](auto* f, uint64_t rows, uint64_t x_rows) {
+        return run(reinterpret_cast<const void*>(f),
+                   dim3(uint32_t((a.n + rows - 1) / rows), cut.splits, uint32_t((a.m + x_rows - 1) / x_rows)), kRaggedWaves * 64, g,
+                   stream);
+    };
+    auto by_groups = [&](auto groups) {
+        constexpr uint32_t kRG = decltype(groups)::value;
+        if (a.m <= 16) return go(nf4_ragged_kernel<kWide, kRG, 1, kWideOut>, 16 * kRG, 16);
+        if constexpr (!kWide)
+            if (a.m > 32) return go(nf4_ragged_kernel<kWide, kRG, 4, kWideOut>, 16 * kRG, 64);
+        return go(nf4_ragged_kernel<kWide, kRG, 2, kWideOut>, 16 * kRG, 32);
+    };
+    // (32 rows share the activations' reads where that leaves a workgroup for every two CUs)
+    e = a.n <= 4096 ? by_groups(std::integral_constant<uint32_t, 1>{}) : by_groups(std::integral_constant<uint32_t, 2>{});
+    if (e != hipSuccess || cut.splits == 1) return e;
+    NF4MatmulArgs j = {};
+    j.c = a.c;
+    j.ldc = a.ldc;
+    j.partial = g.partial;
+    j.m = g.m;
+    j.n = g.n;
+    j.splits = cut.splits;
+    return join<kWideOut>(j, stream);
+}
+
+template <bool kWide, bool kWideOut>
 hipError_t launch_any(const NF4LinearArgs& a, hipStream_t stream)
 {
     const NF4Cut cut = cut_nf4(a.m, a.n, a.k, kWide);
+    if (cut.tile == kThin && !cut.thin_rows) return launch_ragged<kWide, kWideOut>(a, cut, stream);
     return cut.tile == kThin ? launch_thin<kWide, kWideOut>(a, cut, stream) : launch_tiled<kWide, kWideOut>(a, cut, stream);
 }
 

@@ -19,7 +19,7 @@ constexpr uint64_t nf4_planes(bool wide_x) { return wide_x ? 3 : 1; }
 // A product's cut: its tile, the workgroups that share out k, and the weights' rows that are
 // expanded at a time.
 struct NF4Cut {
-    F8Tile tile;  // kThin: weights read as they are, thin_rows rows of them a workgroup
+    F8Tile tile;  // kThin: weights read as they are, thin_rows rows of them a workgroup (0: in any order)
     uint32_t splits;
     uint64_t slab;
     uint32_t thin_rows;
@@ -27,6 +27,10 @@ struct NF4Cut {
 
 // Bytes of expanded weights at a time: what the last-level cache holds.
 constexpr uint64_t kNF4SlabBytes = 1ull << 28;
+
+// The most activations for which weights whose rows do not end with a block are decoded where they
+// are used (64 x 16384 x 4100 bf16 58 us, expanded 72; past 64 they would be decoded twice).
+constexpr uint64_t kNF4Ragged = 64;
 
 inline NF4Cut cut_nf4(uint64_t m, uint64_t n, uint64_t k, bool wide_x)
 {
@@ -51,6 +55,12 @@ inline NF4Cut cut_nf4(uint64_t m, uint64_t n, uint64_t k, bool wide_x)
         const uint64_t want = groups >= 160 ? 1 : 256 / groups, most = k / 64 / 16;
         const uint64_t splits = want < most ? want : most;
         return {kThin, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits)), 0, uint32_t(rows)};
+    }
+    // Rows that do not end with a block: 16 or 32 of them a workgroup, k split as above.
+    if (m <= kNF4Ragged && k % 64 && n <= 1ull << 26) {
+        const uint64_t groups = (n + 15) / 16 * ((m + 63) / 64), want = groups >= 160 ? 1 : 256 / groups,
+                       most = nf4_columns(k) / 64 / 16, splits = want < most ? want : most;
+        return {kThin, uint32_t(splits < 1 ? 1 : (splits > 16 ? 16 : splits)), 0, 0};
     }
     // The tile and the split of k that take the least time by what was measured: a stage of 64
     // columns takes a round of workgroups over the CUs 1640 ns with one tile of 256 x 256 a CU,
@@ -90,7 +100,7 @@ inline NF4Space nf4_space(uint64_t m, uint64_t n, uint64_t k, bool wide_x)
     const uint64_t row = nf4_columns(k) * 2 * nf4_planes(wide_x);
     NF4Space s;
     // (few rows are laid out in their own type where they do not lie on 16 bytes)
-    s.weights = c.tile == kThin ? m * k * (wide_x ? 4 : 2) : m * row;
+    s.weights = c.tile == kThin && c.thin_rows ? m * k * (wide_x ? 4 : 2) : m * row;
     s.partial = s.weights + c.slab * row;
     s.bytes = s.partial + (c.splits > 1 ? c.splits * m * (((c.tile == kThin ? n : c.slab) + 3) / 4 * 16) : 0);
     return s;

@@ -66,6 +66,9 @@ MORE_FORMS = [
     {**_PRODUCT, "name": "product_vocabulary_bf16", "n": 50272},
     {**_PRODUCT, "name": "product_64_bf16", "m": 64},
     {**_PRODUCT, "name": "product_192_bf16", "m": 192},
+    # rows of weights that end within a block
+    {**_PRODUCT, "name": "product_ragged_bf16", "k": 4100},
+    {**_PRODUCT, "name": "product_ragged_16_f32", "dtype": "f32", "out": "f32", "m": 16, "k": 4100},
     # full precision on whole blocks; tiles of 128
     {**_PRODUCT, "name": "product_2048_f32", "dtype": "f32", "out": "f32", "m": 2048, "n": 4096},
     {**_PRODUCT, "name": "product_2048_bf16", "m": 2048, "n": 4096},
@@ -163,7 +166,7 @@ def units(case, kernel):
     if kernel.startswith("attention_kernel"):
         module = more_operators if "page" in case else operators
         return module.work(case)["flops"] // (4 * case["dim"])
-    if kernel.startswith(("nf4_thin", "nf4_expand")):
+    if kernel.startswith(("nf4_thin", "nf4_ragged", "nf4_expand")):
         return case["n"] * case["k"]
     if kernel.startswith("loss_rows"):
         return (case["t"] - case["skip"]) * case["v"]

@@ -192,8 +192,9 @@ hipError_t launch_nf4_linear(const NF4LinearArgs& a, hipStream_t)
     const u128 columns = (k + 63) / 64 * 64, planes = wide ? 3 : 1;
     CHECK(cut.splits >= 1 && cut.splits <= 16 && s.weights % 16 == 0 && s.partial % 16 == 0);
     if (cut.tile == kThin) {
-        CHECK(k % 64 == 0 && u128(s.weights) >= m * k * xe);
-        CHECK(cut.thin_rows == 16 || cut.thin_rows == 64 || cut.thin_rows == 128);
+        CHECK(cut.thin_rows == 0 || cut.thin_rows == 16 || cut.thin_rows == 64 || cut.thin_rows == 128);
+        if (cut.thin_rows) CHECK(k % 64 == 0 && u128(s.weights) >= m * k * xe);
+        if (!cut.thin_rows) CHECK(u128(s.weights) >= m * columns * 2 * planes);
         CHECK(cut.thin_rows != 16 || m <= 4);
         if (cut.splits > 1) CHECK(u128(s.bytes) >= s.partial + cut.splits * m * ((n + 3) / 4) * 16);
     } else {
@@ -209,7 +210,8 @@ hipError_t launch_nf4_linear(const NF4LinearArgs& a, hipStream_t)
     const u128 most = u128(1) << 32, lanes = m * (columns / 8) + 255;
     CHECK(lanes < most);
     if (cut.tile == kThin) {
-        CHECK((n + cut.thin_rows - 1) / cut.thin_rows * 1024 < most && (m + 3) / 4 <= 65535);
+        const u128 rows = cut.thin_rows ? cut.thin_rows : 16;
+        CHECK((n + rows - 1) / rows * (cut.thin_rows ? 1024 : 512) < most && (m + 3) / 4 <= 65535);
     } else {
         const u128 size = cut.tile == k256x256 ? 256 : (cut.tile == k128x128 ? 128 : 64);
         CHECK((m + size - 1) / size * ((u128(cut.slab) + size - 1) / size) * (size == 256 ? 512 : 256) < most);

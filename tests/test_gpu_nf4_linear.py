@@ -1,6 +1,8 @@
 """Products with 4-bit weights on the GPU, through the binding, against a plain
 product in 64 bits of the values that the storage holds. The bars come from the
 arithmetic (bound)."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -274,3 +276,29 @@ def test_no_backward(mz):
     with pytest.raises(RuntimeError, match="no backward pass"):
         mz.nf4_linear(x, w).sum().backward()
     assert np.isfinite(float(mz.nf4_linear(x.detach(), w).sum()))
+
+
+@pytest.mark.parametrize("dtype,out", FORMS)
+@pytest.mark.parametrize("m", [1, 5, 16, 17, 32, 33, 64, 65])
+@pytest.mark.parametrize("n,k", [(33, 100), (4097, 77), (5000, 30), (100, 5001)])
+def test_rows_that_end_within_a_block(mz, n, k, m, dtype, out):
+    check(mz, m, n, k, dtype, out)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("k", [50, 100, 131])
+def test_blocks_that_are_not_finite_reach_their_own_rows(mz, k, dtype):
+    """A block of the next row alone changes nothing, though it is read with the last columns."""
+    n, m = 40, 3
+    w, code, absmax = weights(mz, n, k)
+    x = activations(m, k, dtype)
+    want = mz.nf4_linear(x, w)
+    for b in (1, 17, absmax.numel() - 1):
+        own = torch.zeros(n, dtype=torch.bool)
+        own[b * 64 // k:min(n, (min(b * 64 + 63, n * k - 1)) // k + 1)] = True
+        for bad in (math.nan, math.inf):
+            w.absmax[b] = bad
+            got = mz.nf4_linear(x, w).cpu()
+            assert torch.equal(got[:, ~own], want.cpu()[:, ~own])
+            assert not bool(torch.isfinite(got[:, own]).any())
+        w.absmax[b] = absmax[b]
