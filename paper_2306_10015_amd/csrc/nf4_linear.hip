@@ -746,10 +746,11 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
 // the end of a block are the same ones in every stage too, so that it takes two scales and selects.
 // A code's value comes from the lane that holds it. Codes and scales are read a stage ahead, straight
 // into registers: rows lie on no alignment that loads into LDS could use.
-// What bounds it are those loads, of 16 rows each, and the activations' (1 x 16384 x 4100 bf16 31
-// us, 16 rows 36, 64 rows 58, in fp32 39, 51 and 133; expanded and through tiles 69, 69, 72 and
-// 220, 221, 250). Values by pairs out of LDS took as long; 64 weights a lane 28 us for one row and
-// 37, 89 for 16 and 64; groups of 16 rows alone 33, 41 and 83.
+// What bounds it is the number of those loads, each of 16 rows, and of the activations' (1 x 16384
+// x 4100 bf16 26 us, 16 rows 31, 64 rows 53, in fp32 33, 45 and 130; expanded and through tiles 69,
+// 69, 72 and 220, 221, 250). So both scales are one load; with a load each it took 31, 36 and 58 us,
+// and then values by pairs out of LDS took as long, 64 weights a lane 28, 37 and 89, groups of 16
+// rows alone 33, 41 and 83.
 constexpr uint32_t kRaggedWaves = 8;
 
 struct NF4RaggedArgs {
@@ -774,19 +775,26 @@ __global__ void __launch_bounds__(kRaggedWaves * 64) nf4_ragged_kernel(NF4Ragged
 
     // this lane's first weights of stage 0, rows past the end: the last one's
     const uint64_t all = a.n * a.k, words = (all + 1) / 2 / 4, top = (all - 1) / kNF4Block;
+    // (bytes from the workgroup's first row: 32 rows of up to 2^23 weights)
+    const uint64_t first = n0 * a.k, code0 = a.codes + first / 8 * 4, scale0 = a.absmax + first / kNF4Block * 4;
     uint64_t e0[kRG];
-    uint32_t shift[kRG], left[kRG];
+    uint32_t shift[kRG], left[kRG], code_at[kRG], scale_at[kRG];
 #pragma unroll
     for (uint32_t g = 0; g < kRG; ++g) {
         const uint32_t row = n0 + g * 16 + fr;
         e0[g] = (row < a.n ? row : a.n - 1) * a.k + 16 * fg;
         shift[g] = uint32_t(e0[g] & 7u) * 4;
         left[g] = kNF4Block - uint32_t(e0[g] % kNF4Block);
+        code_at[g] = uint32_t(e0[g] / 8 - first / 8) * 4;
+        scale_at[g] = uint32_t(e0[g] / kNF4Block - first / kNF4Block) * 4;
     }
-    // the stages whose three words are whole words of the codes, by all lanes
+    // the stages whose three words are whole words of the codes and whose blocks have a next one,
+    // by all lanes
     const uint32_t last_row = n0 + kRG * 16 - 1 < a.n ? n0 + kRG * 16 - 1 : a.n - 1;
-    const uint64_t furthest = (last_row * a.k + 48) / 8 + 3;
-    const uint32_t safe = words < furthest ? 0u : uint32_t((words - furthest) / 8 < stages ? (words - furthest) / 8 + 1 : stages);
+    const uint64_t furthest = last_row * a.k + 48, word = furthest / 8 + 3, block = furthest / kNF4Block + 1;
+    uint64_t most = words < word || top < block ? 0 : (words - word) / 8 + 1;
+    if (most > top - block + 1) most = top - block + 1;
+    const uint32_t safe = most < stages ? uint32_t(most) : stages;
 
     struct Codes {
         uint32_t w[3];
@@ -794,48 +802,49 @@ __global__ void __launch_bounds__(kRaggedWaves * 64) nf4_ragged_kernel(NF4Ragged
     };
     auto fetch = [&](uint32_t g, uint32_t s) {
         Codes c;
-        const uint64_t e = e0[g] + uint64_t(s) * 64, b = e / kNF4Block;
-        if (s < safe) {
+        const uint64_t from = code0 + uint64_t(s) * 32, scales = scale0 + uint64_t(s) * 4;
 #pragma unroll
-            for (uint32_t i = 0; i < 3; ++i) c.w[i] = reinterpret_cast<const gu32_t*>(a.codes)[e / 8 + i];
-        } else {
-            const uint64_t at = e & ~uint64_t(7);
-            c.w[0] = eight_codes(a.codes, at, all);
-            c.w[1] = eight_codes(a.codes, at + 8, all);
-            c.w[2] = eight_codes(a.codes, at + 16, all);
-        }
-        c.scale[0] = reinterpret_cast<const gfloat_t*>(a.absmax)[b < top ? b : top];
-        c.scale[1] = reinterpret_cast<const gfloat_t*>(a.absmax)[left[g] >= 16 || b >= top ? (b < top ? b : top) : b + 1];
+        for (uint32_t i = 0; i < 3; ++i) c.w[i] = *reinterpret_cast<const gu32_t*>(from + code_at[g] + 4 * i);
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i) c.scale[i] = reinterpret_cast<const gfloat_t*>(scales + scale_at[g])[i];
+        return c;
+    };
+    auto fetch_last = [&](uint32_t g, uint32_t s) {
+        Codes c;
+        const uint64_t e = e0[g] + uint64_t(s) * 64, b = e / kNF4Block, at = e & ~uint64_t(7);
+        c.w[0] = eight_codes(a.codes, at, all);
+        c.w[1] = eight_codes(a.codes, at + 8, all);
+        c.w[2] = eight_codes(a.codes, at + 16, all);
+        const gfloat_t* scales = reinterpret_cast<const gfloat_t*>(a.absmax);
+        c.scale[0] = scales[b < top ? b : top];
+        c.scale[1] = scales[left[g] >= 16 || b >= top ? (b < top ? b : top) : b + 1];
         return c;
     };
 
-    uint64_t xs[kFM];
+    uint32_t x_at[kFM];  // (up to 64 rows of 2^24 bytes)
 #pragma unroll
     for (uint32_t f = 0; f < kFM; ++f) {
         const uint32_t r = m0 + f * 16 + fr;
-        xs[f] = a.x + (r < a.m ? r : a.m - 1) * a.x_row + fg * 32;
+        x_at[f] = (r < a.m ? r : a.m - 1) * uint32_t(a.x_row) + fg * 32;
     }
     constexpr uint32_t kPlanes = kF ? 3 : 1;
     v4f_t acc[kRG][kFM] = {};
-    Codes next[kRG] = {}, now[kRG];
-    uint32_t s = s0 + wave;
-    if (s < s1)
-#pragma unroll
-        for (uint32_t g = 0; g < kRG; ++g) next[g] = fetch(g, s);
-    for (; s < s1; s += kRaggedWaves) {
-#pragma unroll
-        for (uint32_t g = 0; g < kRG; ++g) now[g] = next[g];
+    struct Activations {
         v8bf_t x[kFM][2][kPlanes];
+    };
+    auto activations = [&](uint32_t s) {
+        Activations o;
 #pragma unroll
         for (uint32_t f = 0; f < kFM; ++f)
 #pragma unroll
             for (uint32_t h = 0; h < 2; ++h)
 #pragma unroll
                 for (uint32_t p = 0; p < kPlanes; ++p)
-                    x[f][h][p] = *reinterpret_cast<const MEZO_GLOBAL v8bf_t*>(xs[f] + p * a.x_plane + uint64_t(s) * 128 + h * 16);
-        if (s + kRaggedWaves < s1)
-#pragma unroll
-            for (uint32_t g = 0; g < kRG; ++g) next[g] = fetch(g, s + kRaggedWaves);
+                    o.x[f][h][p] = *reinterpret_cast<const MEZO_GLOBAL v8bf_t*>(a.x + p * a.x_plane + uint64_t(s) * 128 + x_at[f] + h * 16);
+        return o;
+    };
+    auto step = [&](uint32_t s, const Codes (&now)[kRG], const Activations& in) {
+        const auto& x = in.x;
         const uint64_t column = uint64_t(s) * 64 + 16 * fg;
         const uint32_t valid = column >= a.k ? 0u : (a.k - column < 16 ? uint32_t(a.k - column) : 16u);
 #pragma unroll
@@ -845,8 +854,9 @@ __global__ void __launch_bounds__(kRaggedWaves * 64) nf4_ragged_kernel(NF4Ragged
             float w[16];
 #pragma unroll
             for (uint32_t i = 0; i < 16; ++i)
-                w[i] = __uint_as_float(uint32_t(
-                    __builtin_amdgcn_ds_bpermute(int((codes[i / 8] >> (4 * (i % 8)) & 15u) << 2), int(table))));
+                // (the lane by bits 2 to 7: of four lanes that hold a value any will do)
+                w[i] = __uint_as_float(uint32_t(__builtin_amdgcn_ds_bpermute(
+                    int(i % 8 ? codes[i / 8] >> (4 * (i % 8) - 2) : codes[i / 8] << 2), int(table))));
 #pragma unroll
             for (uint32_t i = 0; i < 16; ++i) w[i] *= i < left[g] ? now[g].scale[0] : now[g].scale[1];
             if (s + 1 == stages) {  // (what follows the row is not its own, and may not be finite)
@@ -872,6 +882,28 @@ __global__ void __launch_bounds__(kRaggedWaves * 64) nf4_ragged_kernel(NF4Ragged
                 }
             }
         }
+    };
+    // The stages whose words are all there, then the others, by code of their own: where the two
+    // ways to read meet, the compiler waits for the loads.
+    Codes now[kRG], next[kRG] = {};
+    const uint32_t end = s1 < safe ? s1 : safe;
+    uint32_t s = s0 + wave;
+    if (s < end)
+#pragma unroll
+        for (uint32_t g = 0; g < kRG; ++g) next[g] = fetch(g, s);
+    for (; s < end; s += kRaggedWaves) {
+#pragma unroll
+        for (uint32_t g = 0; g < kRG; ++g) now[g] = next[g];
+        const Activations x = activations(s);
+        if (s + kRaggedWaves < end)
+#pragma unroll
+            for (uint32_t g = 0; g < kRG; ++g) next[g] = fetch(g, s + kRaggedWaves);
+        step(s, now, x);
+    }
+    for (; s < s1; s += kRaggedWaves) {
+#pragma unroll
+        for (uint32_t g = 0; g < kRG; ++g) now[g] = fetch_last(g, s);
+        step(s, now, activations(s));
     }
 
     // the waves' sums, joined in their order

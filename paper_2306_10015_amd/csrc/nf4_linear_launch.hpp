@@ -29,7 +29,7 @@ struct NF4Cut {
 constexpr uint64_t kNF4SlabBytes = 1ull << 28;
 
 // The most activations for which weights whose rows do not end with a block are decoded where they
-// are used (64 x 16384 x 4100 bf16 58 us, expanded 72; past 64 they would be decoded twice).
+// are used (64 x 16384 x 4100 bf16 53 us, expanded 72; past 64 they would be decoded twice).
 constexpr uint64_t kNF4Ragged = 64;
 
 inline NF4Cut cut_nf4(uint64_t m, uint64_t n, uint64_t k, bool wide_x)
