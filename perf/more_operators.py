@@ -25,9 +25,9 @@ import torch
 own = False
 
 #: NF4's values, and the elements that share a scale.
-NF4 = [-1.0, -0.6961928009986877, -0.5250729322433472, -0.39491742849349976, -0.2844413220882416,
-       -0.18477340042591095, -0.09104997664690018, 0.0, 0.07958031445741653, 0.16093014180660248,
-       0.24611225724220276, 0.3379151225090027, 0.4407097399234772, 0.5626168847084045, 0.722956657409668, 1.0]
+NF4 = [-1.0, -0.6961928009986877, -0.5250730514526367, -0.39491748809814453, -0.28444138169288635, -0.18477343022823334,
+       -0.09105003625154495, 0.0, 0.07958029955625534, 0.16093020141124725, 0.24611230194568634, 0.33791524171829224,
+       0.44070982933044434, 0.5626170039176941, 0.7229568362236023, 1.0]
 BLOCK = 64
 
 
