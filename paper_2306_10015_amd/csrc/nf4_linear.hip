@@ -4,8 +4,11 @@
 // is rounded once.
 //
 // bf16: the products of bf16 are exact in v_mfma_f32_16x16x32_bf16. fp32: each operand is
-// three bf16, its 24 bits in 8 and 8 and 8 by cutting (so that the largest floats stay finite),
-// and six of the nine products are summed, all above 2^-24 of the whole. The parts of a value
+// three bf16, its 24 bits in 8 and 8 and 8, and six of the nine products are summed: all but the
+// second part by the third and the third by itself. Parts are rounded to nearest where operands are
+// laid out, and what is left out is at most 2^-24 of the product; the kernels of few rows cut those of
+// one operand, where they use it (rounding there costs 6%: 1 x 16384 x 4096 23.0 -> 24.5 us), and
+// leave out up to 3 2^-24. With both operands cut it would be 2^-21, and always towards 0. The parts of a value
 // below 2^-110 end at bf16's last bit, 2^-133; one that is infinite or NaN makes its row NaN.
 //
 // Few rows: codes go to LDS as they are and are looked up in a table of all pairs there, in
@@ -41,12 +44,39 @@ __device__ __forceinline__ uint32_t upper_halves(float lo, float hi)
     return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
 }
 
-// What is left of a float after its first 8 bits; 0 where it is not finite (its first part
-// says all there is).
-__device__ __forceinline__ float after_first(float x)
+// Floats as three bf16 each, eight at a time, their parts cut or rounded to nearest. Cutting
+// keeps the largest floats finite by itself; where rounding would not, the first part is the
+// largest bf16. A part of what is not finite is not finite.
+struct Planes {
+    v8bf_t p[3];
+};
+
+template <bool kCut>
+__device__ __forceinline__ Planes planes_of(const float (&x)[8])
 {
-    const float r = x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
-    return r == r ? r : 0.0f;
+    constexpr float kLargest = 0x1.FEp127f;
+    Planes o;
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+        if constexpr (kCut) {
+            uint32_t u[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = upper_halves(r[2 * i], r[2 * i + 1]);
+            o.p[p] = __builtin_bit_cast(v8bf_t, u32x4_t{u[0], u[1], u[2], u[3]});
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                o.p[p][i] = static_cast<__bf16>(p ? r[i] : __builtin_amdgcn_fmed3f(r[i], -kLargest, kLargest));
+        }
+        if (p < 2)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                r[i] -= kCut ? __uint_as_float(__float_as_uint(r[i]) & 0xFFFF0000u) : static_cast<float>(o.p[p][i]);
+    }
+    return o;
 }
 
 // Eight values as one or three planes of bf16, 16 bytes each.
@@ -54,18 +84,9 @@ template <bool kWide>
 __device__ __forceinline__ void store_planes(uint64_t at, uint64_t plane, const float (&x)[8])
 {
     if constexpr (kWide) {
-        float r[8];
+        const Planes o = planes_of<false>(x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r[i] = x[i] == x[i] ? x[i] : __builtin_nanf("");  // (cut, a NaN's bits must not be an infinity's)
-#pragma unroll
-        for (int p = 0; p < 3; ++p) {
-            uint32_t u[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) u[i] = upper_halves(r[2 * i], r[2 * i + 1]);
-            *reinterpret_cast<gu32x4_t*>(at + p * plane) = u32x4_t{u[0], u[1], u[2], u[3]};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] = after_first(r[i]);
-        }
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<gu32x4_t*>(at + p * plane) = __builtin_bit_cast(u32x4_t, o.p[p]);
     } else {
         v8bf_t b;
 #pragma unroll
@@ -436,30 +457,6 @@ struct NF4ThinArgs {
 
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
-// A float as three bf16 by cutting, eight at a time.
-struct Planes {
-    v8bf_t p[3];
-};
-
-__device__ __forceinline__ Planes planes_of(const float (&x)[8])
-{
-    Planes o;
-    float r[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = x[i];
-#pragma unroll
-    for (int p = 0; p < 3; ++p) {
-        uint32_t u[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = upper_halves(r[2 * i], r[2 * i + 1]);
-        o.p[p] = __builtin_bit_cast(v8bf_t, u32x4_t{u[0], u[1], u[2], u[3]});
-        if (p < 2)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] -= __uint_as_float(__float_as_uint(r[i]) & 0xFFFF0000u);
-    }
-    return o;
-}
-
 // c + w x of split operands, the smallest products first.
 __device__ __forceinline__ v4f_t product(const Planes& w, const Planes& x, v4f_t c)
 {
@@ -572,7 +569,7 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
         if constexpr (kF) {
             // a row of 256 bytes: the pair's first and second parts 16 times, its third 32 times
             const float lo[8] = {v.x * kThinScale, v.y * kThinScale, 0, 0, 0, 0, 0, 0};
-            const Planes p = planes_of(lo);
+            const Planes p = planes_of<false>(lo);
             const u32x4_t a0 = __builtin_bit_cast(u32x4_t, p.p[0]), a1 = __builtin_bit_cast(u32x4_t, p.p[1]),
                           a2 = __builtin_bit_cast(u32x4_t, p.p[2]);
             const u32x4_t w = threadIdx.x % 4 < 2 ? u32x4_t{a0[0], a1[0], a0[0], a1[0]} : u32x4_t{a2[0], a2[0], a2[0], a2[0]};
@@ -656,7 +653,7 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
                         v[i] = __uint_as_float(lo[i]);
                         v[i + 4] = __uint_as_float(hi[i]);
                     }
-                    const Planes x = planes_of(v);
+                    const Planes x = planes_of<true>(v);
 #pragma unroll
                     for (uint32_t g = 0; g < kRG; ++g) sum[g][f] = product(p[g], x, sum[g][f]);
                 }
@@ -868,7 +865,7 @@ __global__ void __launch_bounds__(kRaggedWaves * 64) nf4_ragged_kernel(NF4Ragged
                 if constexpr (kF) {
                     const float v[8] = {w[8 * h], w[8 * h + 1], w[8 * h + 2], w[8 * h + 3], w[8 * h + 4], w[8 * h + 5],
                                         w[8 * h + 6], w[8 * h + 7]};
-                    const Planes p = planes_of(v);
+                    const Planes p = planes_of<true>(v);
 #pragma unroll
                     for (uint32_t f = 0; f < kFM; ++f)
                         acc[g][f] = product(p, Planes{{x[f][h][0], x[f][h][1], x[f][h][2]}}, acc[g][f]);

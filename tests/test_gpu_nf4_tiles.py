@@ -8,7 +8,8 @@ Bars, from the arithmetic, with u = 2^-24:
   / 4 additions (a matrix instruction adds at least four products before it rounds) each is off by
   u / sqrt(3) of the sum so far in the mean, which is at most S = sqrt(sum (x w)^2) in the mean: errors have a
   mean square of at most (sqrt(k / 2) + 4 + 1)^2 u^2 S^2, the 1 for the result's rounding. At k = 600 that is
-  22 u S; a product that lacked the last 8 of an operand's 24 bits would be off by 40 u S or more."""
+  22 u S; a product that lacked the last 8 of an operand's 24 bits would be off by 40 u S or more;
+- fp32, of single products: 2^-22 for the product, u for the sum of its parts and u for a scale or the result."""
 import math
 
 import numpy as np
@@ -70,3 +71,29 @@ def test_product_of_every_kernel(mz, m, n, k, dtype, kernel, splits, slab, wide)
             mean_square = (xv ** 2) @ (wv ** 2).t().contiguous()
             off = float(((got - want) ** 2 / mean_square).mean().sqrt())
             assert off <= (math.sqrt(k / 2) + 5) * U, off / U
+
+
+@pytest.mark.parametrize("m,n,k,kernel,splits,slab,wide",
+                         [p[:3] + p[4:] for p in PRODUCTS if p[3] == "f32" and p[0] * p[1] < 10 ** 7 and p[2] < 10 ** 4])
+def test_single_products_of_fp32(mz, m, n, k, kernel, splits, slab, wide):
+    """One activation that is not 0 a row: each result is one product of two floats with all their bits."""
+    g = torch.Generator("cuda").manual_seed(m + n + k)
+
+    def floats(count):
+        """Random ones, and those whose parts after the first are as large as they get."""
+        x = 1 + torch.rand(count, generator=g, device="cuda")
+        hard = torch.tensor([1 + 2.0 ** -7 - 2.0 ** -23, 1 + 2.0 ** -8 - 2.0 ** -16 - 2.0 ** -23, 1 + 2.0 ** -8 + 2.0 ** -17,
+                             1 + 2.0 ** -7 - 2.0 ** -16 + 2.0 ** -17], device="cuda")
+        pick = torch.randint(0, 8, (count,), generator=g, device="cuda")
+        x = torch.where(pick < 4, hard[pick.clamp(max=3)], x)
+        return x * torch.exp2(torch.randint(-3, 4, (count,), generator=g, device="cuda").float())
+
+    code = torch.randint(0, 16, (n * k + 1,), generator=g, device="cuda", dtype=torch.uint8)
+    code = torch.where(torch.rand(n * k + 1, generator=g, device="cuda") < 0.3, torch.full_like(code, 15), code)
+    w, wv = weights(mz, n, k, floats((n * k + 63) // 64), g, code)
+    at = torch.randint(0, k, (m,), generator=g, device="cuda")
+    x = torch.zeros(m, k, device="cuda")
+    x[torch.arange(m, device="cuda"), at] = floats(m)
+    want = x.sum(1).double()[:, None] * wv.double()[:, at].t()
+    off = (products(mz, x, w, n, wide, "f32").double() - want).abs()
+    assert bool((off <= (2.0 ** -22 + 2 * U) * want.abs()).all()), float((off / want.abs().clamp(min=1e-30)).max()) / U
