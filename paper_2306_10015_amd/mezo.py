@@ -353,10 +353,10 @@ class _NoBackward(torch.autograd.Function):
     an error, not a gradient left out."""
 
     @staticmethod
-    def forward(ctx, name, count, *tensors):
+    def forward(ctx, name, out, *inputs):
         ctx.name = name
-        ctx.mark_dirty(*tensors[:count])  # (the operator wrote them)
-        return tensors[:count]
+        ctx.mark_dirty(out)  # (the operator wrote it)
+        return out
 
     @staticmethod
     def backward(ctx, *grads):
@@ -367,7 +367,8 @@ class _NoBackward(torch.autograd.Function):
 def _no_backward(name, outputs, *inputs):
     """Outputs of inputs that require a gradient require one too."""
     if any(t is not None and t.requires_grad for t in inputs) and torch.is_grad_enabled():
-        _NoBackward.apply(name, len(outputs), *outputs, *inputs)
+        for out in outputs:  # (one at a time: of several none may be a part of a wider array)
+            _NoBackward.apply(name, out, *inputs)
 
 
 class F8Matrix:
@@ -757,9 +758,7 @@ def cache_append(k, v, cache: PagedCache, docs: Documents, q=None, freqs=None, p
                          kv_heads, dim, cache.rows, rot, 1 if interleaved else 0, cache.dtype)
         _check(lib.mezo_cache_append(a, _stream_ptr(None)), "mezo_cache_append")
     if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad):
-        for t in (out, cache.k, cache.v):
-            if t is not None:
-                _no_backward("cache_append", (t,), q, k, v)
+        _no_backward("cache_append", (cache.k, cache.v) if out is None else (out, cache.k, cache.v), q, k, v)
     return out
 
 

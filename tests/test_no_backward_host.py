@@ -34,3 +34,18 @@ def test_a_part_of_a_wider_array_may_be_the_output():
     mezo._no_backward("f8_linear", (out,), w)
     with pytest.raises(RuntimeError, match="no backward pass"):
         wide.sum().backward()
+
+
+def test_outputs_may_be_parts_of_wider_arrays_one_beside_another():
+    x, wide, lse = torch.ones(3, requires_grad=True), torch.zeros(2, 5), torch.zeros(2)
+    out = wide[:, 1:4]
+    mezo._no_backward("paged_attention", (out, lse), x, None)
+    for t in (wide, out, lse):
+        with pytest.raises(RuntimeError, match="mezo.paged_attention has no backward pass"):
+            t.sum().backward()
+    cache = torch.zeros(4, 2, 8)
+    k, v = cache[:, 0], cache[:, 1]
+    mezo._no_backward("cache_append", (k, v), x)
+    for t in (k, v, cache):
+        with pytest.raises(RuntimeError, match="mezo.cache_append has no backward pass"):
+            t.sum().backward()
