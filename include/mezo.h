@@ -571,7 +571,7 @@ MEZO_API int mezo_paged_attention(const mezo_attention_t* a, const mezo_pages_t*
  * MEZO_F32 or MEZO_BF16 both). w has the values that mezo_nf4_dequantize gives in
  * x_dtype: v[code] * absmax rounded to fp32, and for MEZO_BF16 to bf16. The products are
  * summed in fp32 and the sum is rounded once; for MEZO_F32 each product is within 2^-22 of
- * itself (v[code] * absmax may then stand unrounded), of values of x below 2^-100 and in results below
+ * itself (v[code] * absmax may then stand unrounded), of values of x or w below 2^-100 and in results below
  * 2^-110 within as much of 2^-100 and 2^-110. A row of x that holds NaN or an infinity, and a
  * block whose absmax is one, give results that are not finite. m, n >= 1, 1 <= k <=
  * MEZO_F8_MAX_COLS, m * n <= MEZO_MAX_NUMEL, m and n times k rounded up to 64 too,

@@ -496,8 +496,8 @@ def nf4_linear(x, w: NF4Tensor, dtype=None, out=None, stream=None):
         ws = _scratch(nbytes, x.device)
         _check(lib.mezo_nf4_linear(x.data_ptr(), x_code, ldx, w.codes.data_ptr(), w.absmax.data_ptr(), m, n, k,
                                    out.data_ptr(), code, ldc, _ptr(ws), nbytes, _stream_ptr(None)), "mezo_nf4_linear")
-    if x.requires_grad:
-        _no_backward("nf4_linear", (out,), x)
+    if x.requires_grad or w.absmax.requires_grad:
+        _no_backward("nf4_linear", (out,), x, w.absmax)
     return out
 
 
@@ -757,8 +757,9 @@ def cache_append(k, v, cache: PagedCache, docs: Documents, q=None, freqs=None, p
                          k_token, k_head, v_token, v_head, o_token, o_head, *cache._k, *cache._v, docs.count, heads,
                          kv_heads, dim, cache.rows, rot, 1 if interleaved else 0, cache.dtype)
         _check(lib.mezo_cache_append(a, _stream_ptr(None)), "mezo_cache_append")
-    if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad):
-        _no_backward("cache_append", (cache.k, cache.v) if out is None else (out, cache.k, cache.v), q, k, v)
+    if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad) \
+            or (freqs is not None and freqs.requires_grad):
+        _no_backward("cache_append", (cache.k, cache.v) if out is None else (out, cache.k, cache.v), q, k, v, freqs)
     return out
 
 

@@ -23,6 +23,31 @@ def cache_of(mz):
     return both, mz.PagedCache(both[:, 0], both[:, 1], torch.arange(3, dtype=torch.int32, device="cuda").view(1, 3))
 
 
+def test_frequencies(mz):
+    """Learned ones."""
+    both, cache = cache_of(mz)
+    qkv = torch.randn(5, 6, 64, device="cuda")
+    freqs = torch.rand(32, device="cuda", requires_grad=True)
+    docs = cache.documents([5], [5])
+    out = mz.cache_append(qkv[:, 2:4], qkv[:, 4:], cache, docs, q=qkv[:, :2], freqs=freqs)
+    for t in (out, cache.k):
+        raises(t)
+    both2, cache2 = cache_of(mz)
+    with torch.no_grad():
+        same = mz.cache_append(qkv[:, 2:4], qkv[:, 4:], cache2, docs, q=qkv[:, :2], freqs=freqs)
+    assert torch.equal(same, out) and torch.equal(both, both2) and not same.requires_grad and not both2.requires_grad
+
+
+def test_scales(mz):
+    w = mz.nf4_quantize(torch.randn(10, 64, device="cuda"))
+    x = torch.randn(4, 64, device="cuda")
+    want = mz.nf4_linear(x, w)
+    w.absmax.requires_grad_(True)
+    got = mz.nf4_linear(x, w)
+    assert torch.equal(got, want)
+    raises(got)
+
+
 @pytest.mark.parametrize("paged", [True, False])
 def test_outputs_in_a_wider_array_with_their_lse(mz, paged):
     q = torch.randn(5, 4, 64, device="cuda", requires_grad=True)
