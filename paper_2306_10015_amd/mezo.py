@@ -234,22 +234,27 @@ class NF4Tensor:
     """A tensor of ``numel`` elements in 4-bit NormalFloat storage (the 4-bit
     forward-only variant): ``codes`` (uint8, ceil(numel / 2) bytes, element
     2i in the low nibble of byte i) and ``absmax`` (float32, one per block of
-    64 elements), both contiguous device tensors owned by torch."""
+    64 elements), both contiguous device tensors owned by torch. ``shape``:
+    that of the elements, None where it is not known; nf4_quantize takes it from
+    the values, and nf4_linear refuses activations that do not fit it."""
 
-    def __init__(self, codes, absmax, numel: int):
+    def __init__(self, codes, absmax, numel: int, shape=None):
         if codes.dtype != torch.uint8 or absmax.dtype != torch.float32:
             raise TypeError("codes must be uint8 and absmax float32")
         if not (codes.is_cuda and absmax.is_cuda and codes.is_contiguous() and absmax.is_contiguous()):
             raise ValueError("codes and absmax must be contiguous CUDA tensors")
         if codes.numel() < (numel + 1) // 2 or absmax.numel() < (numel + NF4_BLOCK - 1) // NF4_BLOCK:
             raise ValueError("codes / absmax too small for numel")
+        if shape is not None and math.prod(shape) != numel:
+            raise ValueError(f"shape {tuple(shape)} is not one of {numel} elements")
         self.codes, self.absmax, self._numel = codes, absmax, int(numel)
+        self.shape = None if shape is None else tuple(shape)
 
     @classmethod
-    def empty(cls, numel: int, device="cuda") -> "NF4Tensor":
+    def empty(cls, numel: int, device="cuda", shape=None) -> "NF4Tensor":
         return cls(torch.empty((numel + 1) // 2, dtype=torch.uint8, device=device),
                    torch.empty((numel + NF4_BLOCK - 1) // NF4_BLOCK, dtype=torch.float32, device=device),
-                   numel)
+                   numel, shape)
 
     def numel(self) -> int:
         return self._numel
@@ -264,7 +269,8 @@ class NF4Tensor:
 
 
 def nf4_quantize(values, out: NF4Tensor | None = None, stream=None) -> NF4Tensor:
-    """values (contiguous fp32/bf16 device tensor) -> NF4 storage."""
+    """values (contiguous fp32/bf16 device tensor) -> NF4 storage of their shape
+    (``out`` keeps a shape of two or more dimensions that it has)."""
     n = values.numel()
     out = NF4Tensor.empty(n, values.device) if out is None else out
     if out.numel() != n or not values.is_contiguous():
@@ -272,6 +278,8 @@ def nf4_quantize(values, out: NF4Tensor | None = None, stream=None) -> NF4Tensor
     with torch.cuda.device(values.device):
         _check(lib.mezo_nf4_quantize(values.data_ptr(), _dtype_code(values), n, out.codes.data_ptr(),
                                      out.absmax.data_ptr(), _stream_ptr(stream)), "mezo_nf4_quantize")
+    if out.shape is None or len(out.shape) < 2:
+        out.shape = tuple(values.shape)
     return out
 
 
@@ -475,10 +483,12 @@ def nf4_linear(x, w: NF4Tensor, dtype=None, out=None, stream=None):
     """A layer's product with 4-bit weights: the activations x (fp32/bf16 [m, k],
     contiguous rows) times w, an NF4 tensor of a [n, k] matrix: [m, n] of dtype (x's by
     default). The values of w are those of nf4_dequantize(w, x.dtype), summed in
-    fp32 (mezo_nf4_linear)."""
+    fp32 (mezo_nf4_linear). Where w's shape is not known, or a flat one, it is a matrix
+    of as many columns as x has."""
     m, k, ldx = _rows_of(x, "x")
-    if w.numel() == 0 or w.numel() % k:
-        raise ValueError(f"x has {k} columns, w {w.numel()} elements")
+    shape = w.shape
+    if w.numel() == 0 or w.numel() % k or (shape is not None and len(shape) > 1 and shape[0] * k != w.numel()):
+        raise ValueError(f"x has {k} columns, w " + (f"{w.numel()} elements" if shape is None else f"is {shape}"))
     n, x_code = w.numel() // k, _dtype_code(x)
     with _on(x.device, stream):
         if out is None:
