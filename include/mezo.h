@@ -515,7 +515,8 @@ MEZO_API int mezo_attention(const mezo_attention_t* a, void* workspace, uint64_t
  * taken as at most tokens (MEZO_EINVAL). What is written must not overlap
  * itself or anything else (MEZO_EOVERLAP), but q_out may be q with its strides,
  * arrays of one stride may lie in each other's gaps (parts of one projection's
- * output), and so may the keys' and the values' pages (not their rows).
+ * output), and so may the keys' and the values' pages, and their rows of all heads
+ * where pages begin a multiple of a row's stride apart.
  * n_docs = 0, max_q = 0 and tokens = 0 enqueue nothing. */
 typedef struct {
     const void* q; /* or NULL */

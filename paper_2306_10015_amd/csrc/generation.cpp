@@ -94,6 +94,18 @@ bool cache_parts(const void* at, uint64_t n_pages, uint64_t page, uint32_t rows,
     return stretch(s, r);
 }
 
+// Whether the rows of the keys' pages lie in the gaps of the values' rows, or the other way round
+// (as where each row of an array holds a token's keys and then its values): rows of all heads
+// together, the same distance apart, also from page to page.
+bool rows_apart(uint64_t k, uint64_t v, uint64_t n_pages, uint64_t k_page, uint64_t v_page, uint64_t k_row, uint64_t v_row,
+                uint64_t heads, uint64_t k_head, uint64_t v_head, uint64_t dim, uint64_t e)
+{
+    if (k_row != v_row || k_row == 0 || (n_pages > 1 && (k_page % k_row || v_page % k_row))) return false;
+    const uint64_t stride = k_row * e, k_bytes = ((heads - 1) * k_head + dim) * e, v_bytes = ((heads - 1) * v_head + dim) * e;
+    const uint64_t d = (v >= k ? v - k : stride - (k - v) % stride) % stride;
+    return k_bytes <= d && d + v_bytes <= stride;
+}
+
 // ---- appending to a paged cache ----------------------------------------------------
 
 int cache_append(const mezo_append_t* p, void* stream)
@@ -141,7 +153,9 @@ int cache_append(const mezo_append_t* p, void* stream)
     // where they are
     if (!distinct(a.page_rows, a.kc_row, a.kv_heads, a.kc_head, a.dim) || (a.n_pages > 1 && kc.stride < kc.extent) ||
         !distinct(a.page_rows, a.vc_row, a.kv_heads, a.vc_head, a.dim) || (a.n_pages > 1 && vc.stride < vc.extent) ||
-        !apart(kc, vc) || (a.q && !distinct(a.tokens, a.o_token, heads, a.o_head, a.dim)))
+        (!apart(kc, vc) && !rows_apart(kc.at, vc.at, a.n_pages, a.kc_page, a.vc_page, a.kc_row, a.vc_row, a.kv_heads,
+                                       a.kc_head, a.vc_head, a.dim, e)) ||
+        (a.q && !distinct(a.tokens, a.o_token, heads, a.o_head, a.dim)))
         return MEZO_EOVERLAP;
     const Strided in[3] = {q, k, v};
     const bool in_place = a.q && a.q == a.q_out && a.q_token == a.o_token && a.q_head == a.o_head;
