@@ -640,10 +640,11 @@ __global__ void __launch_bounds__(kWaves * 64, (waves_per_simd<kF, kD, kKeys, !k
     const uint32_t kvh = (blockIdx.x + (kKeys ? doc + blockIdx.z : 0)) % a.kv_heads;
     // Documents of a cache differ most in their keys. Where they are not split, the workgroups
     // go by their documents' keys, most first: the last to start are short (4 chunks of 1000
-    // tokens over 600 to 8192 keys, 32 heads of 128, 418 -> 376 us; 12 chunks of 200, 306 ->
-    // 252; 20 trees of 61 tokens, whose workgroups all run at once, 188 -> 195). Cutting
-    // documents into equal parts by their table instead gains nothing: 8 trees 80 us with 512
-    // workgroups wanted, 92 to 150 with other numbers; 24 tokens 165 -> 171.
+    // tokens over 600 to 8192 keys, 32 heads of 128, 452 -> 408 us; 12 chunks of 200, 290 ->
+    // 251; 24 of 200, heads of 64, 498 -> 350; 24 trees of 61 tokens in fp32, 8 key/value heads
+    // of 64, 703 -> 524; 20 trees in bf16, heads of 128, 208 -> 213). Up to 64 documents: a lane
+    // of a wave has one. Cutting documents into equal parts by their table instead gains nothing: 8
+    // trees 80 us with 512 workgroups wanted, 92 to 150 with other numbers; 24 tokens 165 -> 171.
     if constexpr (kPaged && !kKeys) {
         if (a.splits == 1 && a.docs > 1 && a.docs <= 64 && uint64_t(gridDim.x) * gridDim.y <= 0xFFFFFFFFu) {
             const uint32_t group = (blockIdx.y * gridDim.x + blockIdx.x) / a.kv_heads;

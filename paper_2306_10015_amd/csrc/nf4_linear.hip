@@ -432,7 +432,8 @@ __global__ void __launch_bounds__(256) nf4_join_columns_kernel(NF4MatmulArgs a)
 // A product of few activations reads each weight once and is bound by that as long as decoding
 // stays cheap. A byte of codes is looked up whole: a table holds the two values of each byte,
 // 32 times over, a copy for each lane of a half wave, so that a lane's lookups never meet
-// another's bank; the address is the byte in bits 8 .. 15 and the lane below, one v_perm_b32.
+// another's bank (17 to 32 activations and the first two parts of fp32 have 16 copies, a
+// copy for two lanes); the address is the byte in bits 8 .. 15 and the lane below, one v_perm_b32.
 // Then a multiplication by the block's scale each and one conversion: 2 vector instructions a
 // weight in bf16 (selecting by v_perm_b32 out of registers takes 4).
 //
@@ -742,7 +743,8 @@ __global__ void __launch_bounds__(kThinWaves * 64) nf4_thin_kernel(NF4ThinArgs a
 // by the same shift in every stage, since 64 columns are whole words; the weights before and behind
 // the end of a block are the same ones in every stage too, so that it takes two scales and selects.
 // A code's value comes from the lane that holds it. Codes and scales are read a stage ahead, straight
-// into registers: rows lie on no alignment that loads into LDS could use.
+// into registers: rows lie on no alignment. (Loads into LDS would go from the 16 bytes that a row
+// begins in, a chunk more a row, and the shift would be one of LDS reads; not built.)
 // What bounds it is the number of those loads, each of 16 rows, and of the activations' (1 x 16384
 // x 4100 bf16 26 us, 16 rows 31, 64 rows 53, in fp32 33, 45 and 130; expanded and through tiles 69,
 // 69, 72 and 220, 221, 250). So both scales are one load; with a load each it took 31, 36 and 58 us,
