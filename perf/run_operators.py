@@ -50,22 +50,31 @@ FORMS = [
 
 _PAGED = {"op": "attend", "dtype": "bf16", "docs": 4, "lo": 600, "hi": 8192, "new": 1000, "tree": False, "page": 32,
           "heads": 32, "kv_heads": 32, "dim": 128, "prefix": False, "softcap": 0.0, "bias": False, "lens": 6}
+_APPEND = {"op": "append", "dtype": "f32", "docs": 16, "lo": 50, "hi": 2048, "new": 0, "tree": False, "page": 32,
+           "heads": 32, "kv_heads": 32, "dim": 128, "rot": 128, "interleaved": False, "lens": 3}
 _PRODUCT = {"op": "product", "dtype": "bf16", "out": "bf16", "m": 1, "k": 4096, "n": 16384, "pad": 0}
 
 MORE_FORMS = [
+    # prompts in full precision, and turned by vectors of two elements
+    {**_APPEND, "name": "append_prompts_f32"},
+    {**_APPEND, "name": "append_prompts_rot20_bf16", "dtype": "bf16", "rot": 20},
     # full precision: a tree, and single tokens over long caches
     {**_PAGED, "name": "trees_128_f32", "dtype": "f32", "docs": 8, "lo": 500, "new": 61, "tree": True, "kv_heads": 8,
      "lens": 5},
     {**_PAGED, "name": "tokens_128_f32", "dtype": "f32", "docs": 12, "lo": 500, "hi": 16384, "new": 1, "page": 16,
      "kv_heads": 8, "lens": 2},
+    # chunks in full precision
+    {**_PAGED, "name": "chunks_128_f32", "dtype": "f32"},
     # a chunk with capped scores; small pages
     {**_PAGED, "name": "chunks_capped_128_bf16", "softcap": 30.0},
     {**_PAGED, "name": "chunks_page8_128_bf16", "page": 8},
-    # few activations: full precision, a vocabulary's rows, a batch of 24 and of 64; a few hundred
+    # few activations: full precision, a vocabulary's rows, batches of 24 and 64; a few hundred
     {**_PRODUCT, "name": "product_1_f32", "dtype": "f32", "out": "f32"},
+    {**_PRODUCT, "name": "product_24_f32", "dtype": "f32", "out": "f32", "m": 24},
     {**_PRODUCT, "name": "product_vocabulary_bf16", "n": 50272},
     {**_PRODUCT, "name": "product_64_bf16", "m": 64},
     {**_PRODUCT, "name": "product_192_bf16", "m": 192},
+    {**_PRODUCT, "name": "product_256_bf16", "m": 256},
     # rows of weights that end within a block
     {**_PRODUCT, "name": "product_ragged_bf16", "k": 4100},
     {**_PRODUCT, "name": "product_ragged_16_f32", "dtype": "f32", "out": "f32", "m": 16, "k": 4100},
